@@ -254,6 +254,68 @@ int monarch_dense(const void *L, const void *R, void *M, int32_t n, int32_t m, i
 int monarch_project(const void *A, void *L, void *R, int32_t n, int32_t m, int dtype,
                     unsigned long long *rotation_count, void *stream);
 
+/* Softmax cross entropy of token rows against a vocabulary, without keeping the logits
+ * (the loss behind the language models of Section 5; the paper gives no text for it):
+ *   z[t][v] = sum_i x[t][i] W[v][i],   lse[t] = log sum_v exp z[t][v]   (natural logarithm),
+ *   loss[t] = lse[t] - z[t][targets[t]].
+ * x: [tokens][d], W: [vocab][d] in the storage dtype; targets: int64 [tokens]; loss, lse:
+ * float32 [tokens].  A token whose target equals ignore_index is left out: loss = lse = 0
+ * there, and its row of x is not used (it may hold anything).  A target outside
+ * [0, vocab) that is not ignore_index gives loss = NaN for its token.  ignore_index may be
+ * any value, one inside [0, vocab) included.  A row with a logit of +infinity or NaN gives
+ * loss = lse = NaN, and so does, in float32, an infinity among the operands of any of its
+ * logits (mask with the lowest finite value).  No reduction over tokens: a mean is dloss[t] = 1 / count below.
+ * targets need 8-byte, loss, lse and dloss 4-byte alignment (so that shifted labels can be
+ * passed in place); tokens and vocab up to 2^24, d up to 65536: beyond, MONARCH_ERR_UNSUPPORTED.
+ * Sums over d, the maximum and the sum of exponentials are fp32 in both dtypes (float32
+ * operands enter the tensor cores as three bf16 parts each, 24 bits).
+ * Workspace: monarch_xent_workspace_bytes (0 for invalid arguments). */
+int monarch_xent_fwd(const void *x, const void *W, const int64_t *targets, float *loss, float *lse,
+                     int64_t tokens, int32_t d, int32_t vocab, int64_t ignore_index, int dtype,
+                     void *workspace, size_t workspace_bytes, void *stream);
+size_t monarch_xent_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab, int dtype);
+
+/* Gradients of sum_t dloss[t] loss[t], with the lse of monarch_xent_fwd:
+ *   g[t][v] = dloss[t] (exp(z[t][v] - lse[t]) - [v == targets[t]]),
+ *   dx[t] = sum_v g[t][v] W[v],   dW[v] = sum_t g[t][v] x[t].
+ * The logits are formed again, a piece of the vocabulary at a time.  dx: [tokens][d] in the
+ * storage dtype; dW: float32 [vocab][d], accumulate == 0 overwrites it, 1 adds to it.
+ * lse, dloss: float32 [tokens].  Tokens left out (ignore_index) have dx = 0 and no part in dW;
+ * a target out of range makes the gradients that it enters NaN.  For float32 and for up to 64
+ * tokens g is held to 2^-24 (three bf16 parts), else to 2^-16 in dW and to bf16 in dx.  The
+ * order of all sums is fixed.
+ * Workspace: monarch_xent_bwd_workspace_bytes (0 for invalid arguments). */
+int monarch_xent_bwd(const void *x, const void *W, const int64_t *targets, const float *lse,
+                     const float *dloss, void *dx, float *dW, int accumulate,
+                     int64_t tokens, int32_t d, int32_t vocab, int64_t ignore_index, int dtype,
+                     void *workspace, size_t workspace_bytes, void *stream);
+size_t monarch_xent_bwd_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab, int dtype);
+
+/* Orthogonalisation of every block of a stack by Newton-Schulz products (for the gradients of the
+ * factors: M = P L P^T R with orthogonal blocks is orthogonal).  For each block X0 = G / (||G||_F + 1e-7),
+ * then `steps` times, with S = X X^T (rows <= cols) or X^T X:
+ *   X <- a X + (b S + c S^2) X   or   X (b S + c S^2),   a, b, c = 3.4445, -4.7750, 2.0315,
+ * which takes the singular values near 1 (five steps: to about 0.7 .. 1.2) and keeps the singular vectors.
+ * G, O: [blocks][rows][cols] in the storage dtype; a factor of monarch_fwd is [m][m][m], of monarch_rect_fwd
+ * [q][b][b1] or [b][r][q], a dense matrix one block.  A block of zeros gives zeros; one with an infinity
+ * or NaN gives NaN, in that block alone.  rows, cols up to 32768, blocks up to 2^20, steps 1 to 32.
+ * Products are held to fp32 (float32 O) or to 16 bits or more (bf16 O), sums are fp32, the norm is summed in fp64.
+ * Workspace: monarch_ortho_workspace_bytes (0 for invalid arguments). */
+int monarch_orthogonalize(const void *G, void *O, int64_t blocks, int32_t rows, int32_t cols, int32_t steps,
+                          int dtype, void *workspace, size_t workspace_bytes, void *stream);
+size_t monarch_ortho_workspace_bytes(int64_t blocks, int32_t rows, int32_t cols, int dtype);
+
+/* One optimiser step with the orthogonalised update, in place:
+ *   V <- beta V + dW;   U = dW + beta V (nesterov == 1) or V (0);
+ *   W <- (1 - lr weight_decay) W - lr scale O(U)
+ * with O as monarch_orthogonalize.  W: [blocks][rows][cols] in the storage dtype; dW (as monarch_bwd and
+ * monarch_rect_bwd return it) and the momentum V: float32.  scale is the caller's choice, commonly
+ * sqrt(max(1, rows / cols)).  W is read and rounded once.  Workspace: monarch_ortho_workspace_bytes with
+ * the dtype of W. */
+int monarch_muon_step(void *W, const float *dW, float *V, int64_t blocks, int32_t rows, int32_t cols,
+                      double lr, double weight_decay, double beta, int nesterov, double scale, int32_t steps,
+                      int dtype, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Bytes of workspace `op` (a monarch_op_t) needs for these sizes under the
  * current implementation choice; always >= MONARCH_STATUS_BYTES.  Returns 0
  * for invalid or unsupported arguments. */

@@ -12,5 +12,7 @@ from .binding import (  # noqa: F401
     monarch_rect_fwd, monarch_rect_workspace_bytes,
     monarch_rectw_fwd, monarch_rectw_bwd, monarch_rectw_workspace_bytes, monarch_rectw_bwd_workspace_bytes,
     monarch_set_impl, monarch_set_deterministic, monarch_debug_set_wait_limit, monarch_debug_skip_load,
+    monarch_xent_fwd, monarch_xent_bwd, monarch_xent_workspace_bytes, monarch_xent_bwd_workspace_bytes,
+    monarch_orthogonalize, monarch_muon_step, monarch_ortho_workspace_bytes,
     monarch_status_string, monarch_workspace_bytes, monarch_workspace_init,
 )

@@ -19,8 +19,8 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmonarch
 _lib = None
 _calls = {}         # name -> native call object, made on first use
 
-_vp, _i64, _i32, _int, _sz = (ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_int,
-                              ctypes.c_size_t)
+_vp, _i64, _i32, _int, _sz, _dbl = (ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_int,
+                                    ctypes.c_size_t, ctypes.c_double)
 _SIGNATURES = {
     "monarch_fwd": (_int, [_vp, _vp, _vp, _vp, _i64, _i32, _i32, _int, _vp, _sz, _vp]),
     "monarch_bwd_dx": (_int, [_vp, _vp, _vp, _vp, _i64, _i32, _i32, _int, _vp, _sz, _vp]),
@@ -41,6 +41,13 @@ _SIGNATURES = {
     "monarch_cplx_fwd": (_int, [_vp, _vp, _vp, _vp, _int, _i64, _i32, _i32, _int, _vp, _sz, _vp]),
     "monarch_dense": (_int, [_vp, _vp, _vp, _i32, _i32, _int, _vp]),
     "monarch_project": (_int, [_vp, _vp, _vp, _i32, _i32, _int, _vp, _vp]),
+    "monarch_xent_fwd": (_int, [_vp] * 5 + [_i64, _i32, _i32, _i64, _int, _vp, _sz, _vp]),
+    "monarch_xent_workspace_bytes": (_sz, [_i64, _i32, _i32, _int]),
+    "monarch_xent_bwd": (_int, [_vp] * 7 + [_int, _i64, _i32, _i32, _i64, _int, _vp, _sz, _vp]),
+    "monarch_xent_bwd_workspace_bytes": (_sz, [_i64, _i32, _i32, _int]),
+    "monarch_orthogonalize": (_int, [_vp, _vp, _i64, _i32, _i32, _i32, _int, _vp, _sz, _vp]),
+    "monarch_ortho_workspace_bytes": (_sz, [_i64, _i32, _i32, _int]),
+    "monarch_muon_step": (_int, [_vp] * 3 + [_i64, _i32, _i32, _dbl, _dbl, _dbl, _int, _dbl, _i32, _int, _vp, _sz, _vp]),
     "monarch_workspace_bytes": (_sz, [_int, _i64, _i32, _i32, _int]),
     "monarch_workspace_init": (_int, [_vp, _sz, _vp]),
     "monarch_last_device_status": (_int, [_vp, _vp]),
@@ -204,6 +211,11 @@ _SPECS = {
     "monarch_cplx_fwd": ("ttttiiiiDws", "x L R y adjoint tokens n m workspace stream"),
     "monarch_dense": ("tttiiDs", "L R M n m stream"),
     "monarch_project": ("tttiiDqs", "A L R n m rotation_count stream"),
+    "monarch_xent_fwd": ("ttqffiiiiDws", "x W targets loss lse tokens d vocab ignore_index workspace stream"),
+    "monarch_xent_bwd": ("ttqfftfiiiiiDws", "x W targets lse dloss dx dW accumulate tokens d vocab ignore_index workspace stream"),
+    "monarch_orthogonalize": ("ttiiiiDws", "G O blocks rows cols steps workspace stream"),
+    "monarch_muon_step": ("tffiiidddidiDws",
+                          "W dW V blocks rows cols lr weight_decay beta nesterov scale steps workspace stream"),
 }
 
 
@@ -282,6 +294,61 @@ def monarch_project(A, L, R, n, m, rotation_count=None, stream=None) -> None:
     """Algorithm 1: factors L, R of the Monarch matrix closest to the dense A in Frobenius norm.
     rotation_count: optional one-element int64 CUDA tensor, incremented by the number of Jacobi rotations."""
     (_calls.get("monarch_project") or _native("monarch_project"))(A, L, R, n, m, rotation_count, stream)
+
+
+def _sizes(call: str, **tensors) -> None:
+    """The tensors of a call, each with the number of values that the call touches: enough of them, on the current device, whose stream is used."""
+    import torch
+    device = torch.cuda.current_device() if torch.cuda.is_available() else 0
+    for name, (t, n) in tensors.items():
+        if t is None:
+            continue
+        if t.numel() < n:
+            raise ValueError(f"{call}: {name} must have at least {n} values, got {t.numel()}")
+        if t.is_cuda and t.get_device() != device:
+            raise ValueError(f"{call}: {name} is on device {t.get_device()}, the current one is {device}")
+
+
+def monarch_xent_workspace_bytes(tokens: int, d: int, vocab: int, dtype: int) -> int:
+    return int(lib().monarch_xent_workspace_bytes(tokens, d, vocab, dtype))
+
+
+def monarch_xent_bwd_workspace_bytes(tokens: int, d: int, vocab: int, dtype: int) -> int:
+    return int(lib().monarch_xent_bwd_workspace_bytes(tokens, d, vocab, dtype))
+
+
+def monarch_xent_fwd(x, W, targets, loss, lse, tokens, d, vocab, ignore_index, workspace, stream=None) -> None:
+    """loss[t] = lse[t] - x[t] . W[targets[t]], lse[t] = log sum_v exp(x[t] . W[v]); targets int64, loss and lse float32."""
+    _sizes("monarch_xent_fwd", x=(x, tokens * d), W=(W, vocab * d), targets=(targets, tokens), loss=(loss, tokens), lse=(lse, tokens))
+    (_calls.get("monarch_xent_fwd") or _native("monarch_xent_fwd"))(x, W, targets, loss, lse, tokens, d, vocab, ignore_index,
+                                                                    workspace, stream)
+
+
+def monarch_xent_bwd(x, W, targets, lse, dloss, dx, dW, accumulate, tokens, d, vocab, ignore_index, workspace, stream=None) -> None:
+    """Gradients of sum_t dloss[t] loss[t]: dx like x, dW [vocab, d] in float32 (accumulate=1 adds to it)."""
+    _sizes("monarch_xent_bwd", x=(x, tokens * d), W=(W, vocab * d), targets=(targets, tokens), lse=(lse, tokens),
+           dloss=(dloss, tokens), dx=(dx, tokens * d), dW=(dW, vocab * d))
+    (_calls.get("monarch_xent_bwd") or _native("monarch_xent_bwd"))(x, W, targets, lse, dloss, dx, dW, int(accumulate), tokens, d,
+                                                                    vocab, ignore_index, workspace, stream)
+
+
+def monarch_ortho_workspace_bytes(blocks: int, rows: int, cols: int, dtype: int) -> int:
+    return int(lib().monarch_ortho_workspace_bytes(blocks, rows, cols, dtype))
+
+
+def monarch_orthogonalize(G, O, blocks, rows, cols, steps, workspace, stream=None) -> None:
+    """O = G with the singular values of every [rows, cols] block taken near 1 by ``steps`` Newton-Schulz products."""
+    n = blocks * rows * cols
+    _sizes("monarch_orthogonalize", G=(G, n), O=(O, n))
+    (_calls.get("monarch_orthogonalize") or _native("monarch_orthogonalize"))(G, O, blocks, rows, cols, steps, workspace, stream)
+
+
+def monarch_muon_step(W, dW, V, blocks, rows, cols, lr, weight_decay, beta, nesterov, scale, steps, workspace, stream=None) -> None:
+    """V <- beta V + dW; W <- (1 - lr weight_decay) W - lr scale orthogonalised(dW + beta V, or V without nesterov), in place."""
+    n = blocks * rows * cols
+    _sizes("monarch_muon_step", W=(W, n), dW=(dW, n), V=(V, n))
+    (_calls.get("monarch_muon_step") or _native("monarch_muon_step"))(W, dW, V, blocks, rows, cols, lr, weight_decay, beta,
+                                                                      int(nesterov), scale, steps, workspace, stream)
 
 
 def monarch_rect_bwd_workspace_bytes(tokens: int, q: int, b1: int, b: int, r: int, dtype: int) -> int:

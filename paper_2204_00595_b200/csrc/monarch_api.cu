@@ -1,5 +1,6 @@
 // C-ABI entry points of libmonarch: argument validation and dispatch.  No arithmetic here.
 #include <atomic>
+#include <cmath>
 #include <cstdlib>
 
 #include "common.cuh"
@@ -38,6 +39,8 @@ size_t esize(int dtype) { return dtype == MONARCH_F32 ? 4 : 2; }
 struct Range {
     const void *p;
     size_t bytes;
+    size_t align = 16;
+    bool empty_ok = false;      // null where there are no bytes
 };
 
 bool overlap(const Range &a, const Range &b)
@@ -70,15 +73,15 @@ int check_rect(int64_t tokens, int32_t q, int32_t b1, int32_t b, int32_t r, int 
     return MONARCH_OK;
 }
 
-// Inputs and outputs: non-null, 16-byte aligned; no output overlaps an input, another
+// Inputs and outputs: non-null, aligned (16 bytes unless said otherwise); no output overlaps an input, another
 // output or the workspace.
 int check_buffers(const Range *in, int n_in, const Range *out, int n_out, const void *ws,
                   size_t ws_bytes, size_t ws_need)
 {
     for (int i = 0; i < n_in; ++i)
-        if (!in[i].p || !aligned(in[i].p, 16)) return MONARCH_ERR_INVALID_ARG;
+        if ((!in[i].p && !(in[i].empty_ok && in[i].bytes == 0)) || !aligned(in[i].p, in[i].align)) return MONARCH_ERR_INVALID_ARG;
     for (int i = 0; i < n_out; ++i)
-        if (!out[i].p || !aligned(out[i].p, 16)) return MONARCH_ERR_INVALID_ARG;
+        if ((!out[i].p && !(out[i].empty_ok && out[i].bytes == 0)) || !aligned(out[i].p, out[i].align)) return MONARCH_ERR_INVALID_ARG;
     if (!ws || !aligned(ws, 256) || ws_need == 0 || ws_bytes < ws_need) return MONARCH_ERR_WORKSPACE;
     const Range w = {ws, ws_bytes};
     for (int o = 0; o < n_out; ++o) {
@@ -90,6 +93,24 @@ int check_buffers(const Range *in, int n_in, const Range *out, int n_out, const 
     }
     for (int i = 0; i < n_in; ++i)
         if (overlap(in[i], w)) return MONARCH_ERR_INVALID_ARG;
+    return MONARCH_OK;
+}
+
+// Sizes of the vocabulary loss: what 32-bit tile coordinates and the preparation's counters hold with room to spare.
+int check_xent(int64_t tokens, int32_t d, int32_t vocab, int dtype)
+{
+    if (tokens < 0 || d <= 0 || vocab <= 0) return MONARCH_ERR_INVALID_ARG;
+    if (dtype != MONARCH_F32 && dtype != MONARCH_BF16) return MONARCH_ERR_INVALID_ARG;
+    if (tokens > (1 << 24) || d > (1 << 16) || vocab > (1 << 24)) return MONARCH_ERR_UNSUPPORTED;
+    return MONARCH_OK;
+}
+
+// Sizes of the orthogonalised update.
+int check_ortho(int64_t blocks, int32_t rows, int32_t cols, int32_t steps, int dtype)
+{
+    if (blocks < 0 || rows <= 0 || cols <= 0 || steps < 1) return MONARCH_ERR_INVALID_ARG;
+    if (dtype != MONARCH_F32 && dtype != MONARCH_BF16) return MONARCH_ERR_INVALID_ARG;
+    if (rows > 32768 || cols > 32768 || blocks > (1 << 20) || steps > 32) return MONARCH_ERR_UNSUPPORTED;
     return MONARCH_OK;
 }
 
@@ -415,6 +436,71 @@ int monarch_mlp_bwd(const void *x, const void *dy, const void *L1, const void *R
     MONARCH_TRY(monarch_bwd(x, dh, L1, R1, ws_f, dx, dL1, dR1, accumulate, tokens, n, m, dtype, ws_b, lay.ws_b,
                             stream));
     return bias_in_a ? MONARCH_OK : merge_status((unsigned *)ws_b, (unsigned *)ws_f, s);
+}
+
+size_t monarch_xent_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab, int dtype)
+{
+    return check_xent(tokens, d, vocab, dtype) != MONARCH_OK ? 0 : xent_workspace_bytes(tokens, d, vocab, dtype, 0);
+}
+
+size_t monarch_xent_bwd_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab, int dtype)
+{
+    return check_xent(tokens, d, vocab, dtype) != MONARCH_OK ? 0 : xent_workspace_bytes(tokens, d, vocab, dtype, 1);
+}
+
+int monarch_xent_fwd(const void *x, const void *W, const int64_t *targets, float *loss, float *lse, int64_t tokens, int32_t d,
+                     int32_t vocab, int64_t ignore_index, int dtype, void *workspace, size_t workspace_bytes, void *stream)
+{
+    MONARCH_TRY(check_xent(tokens, d, vocab, dtype));
+    const size_t es = esize(dtype), t = (size_t)tokens;
+    const Range in[] = {{x, t * d * es, 16, true}, {W, (size_t)vocab * d * es}, {targets, t * 8, 8, true}};
+    const Range out[] = {{loss, t * 4, 4, true}, {lse, t * 4, 4, true}};
+    MONARCH_TRY(check_buffers(in, 3, out, 2, workspace, workspace_bytes, xent_workspace_bytes(tokens, d, vocab, dtype, 0)));
+    return xent_fwd(x, W, targets, loss, lse, tokens, d, vocab, ignore_index, dtype, workspace, (cudaStream_t)stream);
+}
+
+int monarch_xent_bwd(const void *x, const void *W, const int64_t *targets, const float *lse, const float *dloss, void *dx, float *dW,
+                     int accumulate, int64_t tokens, int32_t d, int32_t vocab, int64_t ignore_index, int dtype, void *workspace,
+                     size_t workspace_bytes, void *stream)
+{
+    MONARCH_TRY(check_xent(tokens, d, vocab, dtype));
+    if (accumulate != 0 && accumulate != 1) return MONARCH_ERR_INVALID_ARG;
+    const size_t es = esize(dtype), t = (size_t)tokens;
+    const Range in[] = {{x, t * d * es, 16, true}, {W, (size_t)vocab * d * es}, {targets, t * 8, 8, true}, {lse, t * 4, 4, true}, {dloss, t * 4, 4, true}};
+    const Range out[] = {{dx, t * d * es, 16, true}, {dW, (size_t)vocab * d * 4}};
+    MONARCH_TRY(check_buffers(in, 5, out, 2, workspace, workspace_bytes, xent_workspace_bytes(tokens, d, vocab, dtype, 1)));
+    return xent_bwd(x, W, targets, lse, dloss, dx, dW, accumulate, tokens, d, vocab, ignore_index, dtype, workspace, (cudaStream_t)stream);
+}
+
+size_t monarch_ortho_workspace_bytes(int64_t blocks, int32_t rows, int32_t cols, int dtype)
+{
+    return check_ortho(blocks, rows, cols, 1, dtype) != MONARCH_OK ? 0 : ortho_workspace_bytes(blocks, rows, cols, dtype);
+}
+
+int monarch_orthogonalize(const void *G, void *O, int64_t blocks, int32_t rows, int32_t cols, int32_t steps, int dtype, void *workspace,
+                          size_t workspace_bytes, void *stream)
+{
+    MONARCH_TRY(check_ortho(blocks, rows, cols, steps, dtype));
+    const size_t bytes = (size_t)blocks * rows * cols * esize(dtype);
+    const Range in[] = {{G, bytes, 16, true}};
+    const Range out[] = {{O, bytes, 16, true}};
+    MONARCH_TRY(check_buffers(in, 1, out, 1, workspace, workspace_bytes, ortho_workspace_bytes(blocks, rows, cols, dtype)));
+    return orthogonalize(G, O, blocks, rows, cols, steps, dtype, workspace, (cudaStream_t)stream);
+}
+
+int monarch_muon_step(void *W, const float *dW, float *V, int64_t blocks, int32_t rows, int32_t cols, double lr, double weight_decay,
+                      double beta, int nesterov, double scale, int32_t steps, int dtype, void *workspace, size_t workspace_bytes,
+                      void *stream)
+{
+    MONARCH_TRY(check_ortho(blocks, rows, cols, steps, dtype));
+    if (nesterov != 0 && nesterov != 1) return MONARCH_ERR_INVALID_ARG;
+    if (!std::isfinite(lr) || !std::isfinite(weight_decay) || !std::isfinite(beta) || !std::isfinite(scale)) return MONARCH_ERR_INVALID_ARG;
+    const size_t n = (size_t)blocks * rows * cols;
+    const Range in[] = {{dW, n * 4, 16, true}};
+    const Range out[] = {{W, n * esize(dtype), 16, true}, {V, n * 4, 16, true}};
+    MONARCH_TRY(check_buffers(in, 1, out, 2, workspace, workspace_bytes, ortho_workspace_bytes(blocks, rows, cols, dtype)));
+    return muon_step(W, dW, V, blocks, rows, cols, (float)(1.0 - lr * weight_decay), (float)(lr * scale), (float)beta, nesterov, steps, dtype,
+                     workspace, (cudaStream_t)stream);
 }
 
 size_t monarch_rect_workspace_bytes(int64_t tokens, int32_t q, int32_t b1, int32_t b, int32_t r, int dtype)

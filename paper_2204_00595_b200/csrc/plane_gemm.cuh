@@ -1,0 +1,403 @@
+// Matrix products on CTA pairs (tcgen05, cta_group::2) whose operands are held as one, two or three bf16 PLANES: a value is
+// hi + lo (+ lo2), each plane the bf16 rounding of what the ones before it leave: off by at most 2^-8, 2^-16 or 2^-24 of the
+// value.  A product of two such operands is a few plane products added up in the same fp32 accumulator:
+//   kP1    hi hi                                        operands that are bf16 themselves
+//   kP2x1  hi hi + lo hi                                first operand in two planes, second one bf16
+//   kP3x1  the same with three planes of the first
+//   kP2x2  hi hi + hi lo + lo hi                        both in two planes (left out: lo lo, at most 2^-16 of the product)
+//   kP3x3  the six with at most two orders of lo        fp32 operands (left out: 2^-23 of the product)
+// A tf32 product would keep 11 bits and fp32 FMA runs at a 25th of this rate.
+//
+//   C[m][n] = sum_k A(m, k) B(n, k)       A, B stored [rows][K] (K-major) or [K][rows] (MN-major), each with its own flag
+//
+// Persistent kernel on clusters of two CTAs, 256 x 256 output tiles: CTA r of a pair owns 128 rows of A and loads 128 of the
+// 256 rows of B; one MMA instruction of 256 x 256 x 16 runs on both SMs.  Shared memory is a ring of 16 KB operand tiles
+// (128 x 64, 128-byte swizzle), loaded in the order in which the plane products use them, so that a tile of a plane is loaded
+// once per K chunk however many products it enters.  Two accumulators of 256 columns in tensor memory alternate.
+//   warps 0-7  epilogue: warp w reads rows 32 (w % 4) .. of column half w / 4
+//   warp 8     lane 0: TMA loads;  warp 9  lane 0 of the even CTA: MMAs
+// Every wait is bounded (tc_common.cuh).
+#pragma once
+
+#include "mma_tiles.cuh"
+
+namespace monarch {
+namespace tc {
+
+enum PlaneScheme { kP1 = 0, kP2x1 = 1, kP2x2 = 2, kP3x3 = 3, kP3x1 = 4 };
+
+constexpr int kPgTile = 256, kPgChunk = 64;
+constexpr int kPgSlotBytes = 128 * kPgChunk * 2, kPgSlots = 13;
+constexpr int kPgThreads = 320, kPgEpiWarps = 8;
+constexpr int kPgSmem = kPgSlots * kPgSlotBytes + 1024;
+
+// loads per K chunk: bit 2 = operand B, bits 0-1 = plane
+__host__ __device__ constexpr int pg_loads(int s) { return s == kP1 ? 2 : s == kP2x1 ? 3 : s == kP2x2 || s == kP3x1 ? 4 : 6; }
+__host__ __device__ constexpr int pg_load(int s, int l)
+{
+    constexpr int kB = 4;
+    constexpr int t[5][6] = {{0, kB, 0, 0, 0, 0}, {kB, 0, 1, 0, 0, 0}, {0, kB, kB + 1, 1, 0, 0}, {0, kB, kB + 1, kB + 2, 1, 2}, {kB, 0, 1, 2, 0, 0}};
+    return t[s][l];
+}
+// products that become possible with load l: (load of A) | (load of B) << 4, up to two; 0xff: none
+__host__ __device__ constexpr int pg_mma(int s, int l, int i)
+{
+    constexpr int none = 0xff;
+    constexpr int t[5][6][2] = {{{none, none}, {0x10, none}, {none, none}, {none, none}, {none, none}, {none, none}},
+                                {{none, none}, {0x01, none}, {0x02, none}, {none, none}, {none, none}, {none, none}},
+                                {{none, none}, {0x10, none}, {0x20, none}, {0x13, none}, {none, none}, {none, none}},
+                                {{none, none}, {0x10, none}, {0x20, none}, {0x30, none}, {0x14, 0x24}, {0x15, none}},
+                                {{none, none}, {0x01, none}, {0x02, none}, {0x03, none}, {none, none}, {none, none}}};
+    return t[s][l][i];
+}
+// loads whose last use is among the products of load l (bit mask)
+__host__ __device__ constexpr int pg_done(int s, int l)
+{
+    constexpr int t[5][6] = {{0, 3, 0, 0, 0, 0}, {0, 2, 5, 0, 0, 0}, {0, 0, 5, 10, 0, 0}, {0, 0, 0, 9, 20, 34}, {0, 2, 4, 9, 0, 0}};
+    return t[s][l];
+}
+
+// The tensor cores add to an fp32 accumulator without rounding to nearest: sums of mixed signs shrink by some 2^-25 per step of 16
+// products (measured: a sum over 8192 tokens of two planes, 1024 steps, was 1.9e-5 off; 3e-5 over 1500 steps).  Where the result is
+// float32, a run in tensor memory ends after this many K chunks and the epilogue warps add the runs up in registers, while the
+// MMAs go on in the other accumulator.
+__host__ __device__ constexpr int pg_seg(int s) { return s == kP1 ? 16 : s == kP2x1 ? 8 : s == kP2x2 || s == kP3x1 ? 5 : 2; }
+
+struct PlaneGemm {
+    unsigned *status;
+    const int *count;          // device: rows that take part (token rows), or null
+    int count_is_k;            // count bounds K (else M)
+    int row0, rows;            // rows of M: row0 .. row0 + rows (rows clipped by *count - row0)
+    int cols;                  // columns of N
+    int kdim;                  // contraction length (clipped by *count)
+    int a_k0, b_k0;            // first K coordinate of the operands
+    int b_n0;                  // first N coordinate of B
+    int a_zstep, b_zstep;      // planes per matrix of a batch in the tensor maps
+    int batches, splits;       // matrices; parts of K, each a product of its own (output index batch * splits + split)
+    int n_fastest;             // neighbouring pairs take neighbouring column tiles (else row tiles)
+    int seg;                   // K chunks per accumulation in tensor memory (kernels with PROMOTE)
+};
+
+struct PgTile {
+    int z, row, col, zero;     // output matrix; this thread's row; first of this warp's 128 columns; nothing was accumulated
+};
+
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap *m, int x, int y, int z, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+        "l"(m), "r"(bar & 0xFEFFFFFFu), "r"(x), "r"(y), "r"(z)
+        : "memory");
+}
+
+// 32 consecutive columns of this thread's lane, waited for
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&f)[32])
+{
+    uint32_t *r = reinterpret_cast<uint32_t *>(f);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+    // the wait names the registers, so that nothing that reads them can move before it
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                   "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
+                   "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
+                   "+r"(r[25]), "+r"(r[26]), "+r"(r[27])
+                 :
+                 : "memory");
+    asm volatile("" : "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])::"memory");
+}
+
+// 32 bytes in one store: a full sector
+__device__ __forceinline__ void st_v8(void *p, uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t e, uint32_t f, uint32_t g, uint32_t h)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e), "r"(f), "r"(g), "r"(h) : "memory");
+}
+
+struct PgBars {
+    uint64_t full[kPgSlots], empty[kPgSlots];                           // full: used in the even CTA only
+    uint64_t acc_full[2], acc_empty[2];
+};
+
+// Epi: struct with  begin(const Epi::Args &, const PgTile &),  chunk(args, tile, c, float (&v)[32])  for c = 0, 32, 64, 96,
+// end(args, tile).  PROMOTE: at most p.seg chunks are accumulated in tensor memory, sums of those in fp32 registers.
+template <int AMN, int BMN, int SCHEME, bool PROMOTE, class Epi>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPgThreads, 1)
+plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const PlaneGemm p,
+                  const typename Epi::Args args)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) PgBars bars;
+    __shared__ uint32_t tmem_base_s;
+    __shared__ int dead_s;
+
+    const uint32_t ring0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+    volatile int *dead = &dead_s;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kPgSlots; ++s) {
+            mbar_init(smem_u32(&bars.full[s]), 1);                      // the even CTA's expect_tx arrival
+            mbar_init(smem_u32(&bars.empty[s]), 1);
+        }
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(smem_u32(&bars.acc_full[a]), 1);
+            mbar_init(smem_u32(&bars.acc_empty[a]), 2 * kPgEpiWarps);   // epilogue warps of both CTAs
+        }
+        fence_mbar_init();
+        dead_s = 0;
+        tma_prefetch_desc(&tm_a);
+        tma_prefetch_desc(&tm_b);
+    }
+    if (warp == 0) {
+        tmem_alloc_pair(smem_u32(&tmem_base_s), 512);
+        tmem_relinquish_pair();
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_arrive_release();                                           // both CTAs' barriers exist before any remote arrive
+    cluster_wait_acquire();
+    tc_fence_after();
+    const uint32_t tmem_base = tmem_base_s;
+    depend_launch();
+    depend_wait();
+
+    int rows = p.rows, kdim = p.kdim;
+    if (p.count != nullptr) {
+        const int n = *p.count;
+        if (p.count_is_k) kdim = min(kdim, n);
+        else rows = max(0, min(rows, n - p.row0));
+    }
+    const int mtiles = (rows + kPgTile - 1) / kPgTile, ntiles = (p.cols + kPgTile - 1) / kPgTile;
+    const int kchunks = (kdim + kPgChunk - 1) / kPgChunk;
+    const int per_split = (kchunks + p.splits - 1) / p.splits;
+    const long long plane_tiles = (long long)mtiles * ntiles, total = plane_tiles * p.batches * p.splits;
+    const uint32_t full0 = smem_u32(bars.full), empty0 = smem_u32(bars.empty);
+    const uint32_t accf0 = smem_u32(bars.acc_full), acce0 = smem_u32(bars.acc_empty);
+    constexpr int kLoads = pg_loads(SCHEME);
+    const int seg = PROMOTE ? p.seg : 0x7fffffff;
+
+    struct At {
+        int z, split, mt, nt, c0, c1;
+    };
+    auto locate = [&](long long tile) {
+        At a;
+        const int zz = (int)(tile / plane_tiles), t = (int)(tile % plane_tiles);
+        a.z = zz / p.splits;
+        a.split = zz % p.splits;
+        a.mt = p.n_fastest ? t / ntiles : t % mtiles;
+        a.nt = p.n_fastest ? t % ntiles : t / mtiles;
+        a.c0 = min(a.split * per_split, kchunks);
+        a.c1 = min(a.c0 + per_split, kchunks);
+        return a;
+    };
+
+    if (warp == 8) {
+        // ------------------------------------------------------------ loader (both CTAs)
+        if (lane == 0) {
+            uint32_t slot = 0, phase = 1;
+            bool ok = true;
+            for (long long tile = pair; ok && tile < total; tile += npairs) {
+                const At at = locate(tile);
+                const int m0 = p.row0 + at.mt * kPgTile + (int)rank * 128, n0 = p.b_n0 + at.nt * kPgTile + (int)rank * 128;
+                for (int c = at.c0; ok && c < at.c1; ++c) {
+                    const int ka = p.a_k0 + c * kPgChunk, kb = p.b_k0 + c * kPgChunk;
+#pragma unroll
+                    for (int l = 0; l < kLoads; ++l) {
+                        if (!mbar_wait(empty0 + slot * 8, phase, p.status, dead, kErrSlotWait)) { ok = false; break; }
+                        const uint32_t dst = ring0 + slot * kPgSlotBytes, full = full0 + slot * 8;
+                        // the even CTA announces the bytes of both halves; either CTA's may land first
+                        if (rank == 0) mbar_expect_tx(full, 2 * kPgSlotBytes);
+                        constexpr int tag[6] = {pg_load(SCHEME, 0), pg_load(SCHEME, 1), pg_load(SCHEME, 2), pg_load(SCHEME, 3),
+                                                pg_load(SCHEME, 4), pg_load(SCHEME, 5)};
+                        const int plane = tag[l] & 3;
+                        if (tag[l] & 4) {
+                            const int z = at.z * p.b_zstep + plane;
+                            if constexpr (BMN) {
+                                tma_load_3d_pair(dst, &tm_b, n0, kb, z, full);
+                                tma_load_3d_pair(dst + 8192, &tm_b, n0 + 64, kb, z, full);
+                            } else {
+                                tma_load_3d_pair(dst, &tm_b, kb, n0, z, full);
+                            }
+                        } else {
+                            const int z = at.z * p.a_zstep + plane;
+                            if constexpr (AMN) {
+                                tma_load_3d_pair(dst, &tm_a, m0, ka, z, full);
+                                tma_load_3d_pair(dst + 8192, &tm_a, m0 + 64, ka, z, full);
+                            } else {
+                                tma_load_3d_pair(dst, &tm_a, ka, m0, z, full);
+                            }
+                        }
+                        if (++slot == kPgSlots) { slot = 0; phase ^= 1; }
+                    }
+                }
+            }
+            let_copies_land(dead);
+        }
+    } else if (warp == 9) {
+        if (lane == 0 && rank == 0) {
+            // ------------------------------------------------------------ even CTA: MMA issuer for the pair
+            constexpr uint32_t idesc = make_idesc_bf16(256, 256, AMN, BMN);
+            constexpr uint32_t astep = AMN ? 128 : 2, bstep = BMN ? 128 : 2;
+            const uint64_t adesc = AMN ? make_smem_desc(0, 8192, 1024, kSwizzle128) : make_smem_desc(0, 16, 1024, kSwizzle128);
+            const uint64_t bdesc = BMN ? make_smem_desc(0, 8192, 1024, kSwizzle128) : make_smem_desc(0, 16, 1024, kSwizzle128);
+            uint32_t slot = 0, phase = 0, it = 0;
+            bool ok = true;
+            for (long long tile = pair; ok && tile < total; tile += npairs) {
+                const At at = locate(tile);
+                for (int c0 = at.c0; ok && c0 < at.c1; c0 = (at.c1 - c0 > seg) ? c0 + seg : at.c1, ++it) {
+                    const int c1 = (at.c1 - c0 > seg) ? c0 + seg : at.c1;
+                    const uint32_t buf = it & 1;
+                    if (!mbar_wait<true>(acce0 + buf * 8, ((it >> 1) & 1) ^ 1, p.status, dead, kErrTmemWait)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t d = tmem_base + buf * 256;
+                    for (int c = c0; ok && c < c1; ++c) {
+                        uint32_t at_slot[kLoads];
+#pragma unroll
+                        for (int l = 0; l < kLoads; ++l) {
+                            at_slot[l] = slot;
+                            if (!mbar_wait<true>(full0 + slot * 8, phase, p.status, dead, kErrTmaWait)) { ok = false; break; }
+                            if (++slot == kPgSlots) { slot = 0; phase ^= 1; }
+                            tc_fence_after();
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const int w = pg_mma(SCHEME, l, i);
+                                if (w == 0xff) continue;
+                                const uint64_t ad = adesc | (uint64_t)((ring0 + at_slot[w & 15] * kPgSlotBytes) >> 4);
+                                const uint64_t bd = bdesc | (uint64_t)((ring0 + at_slot[w >> 4] * kPgSlotBytes) >> 4);
+#pragma unroll
+                                for (int kk = 0; kk < 4; ++kk)
+                                    mma_f16_ss_pair(d, ad + astep * kk, bd + bstep * kk, idesc, (uint32_t)(c != c0 || l != 1 || kk != 0));
+                            }
+#pragma unroll
+                            for (int j = 0; j < kLoads; ++j)
+                                if ((pg_done(SCHEME, l) >> j) & 1) mma_commit_pair(empty0 + at_slot[j] * 8, 3);
+                        }
+                    }
+                    if (ok) mma_commit_pair(accf0 + buf * 8, 3);
+                }
+            }
+        }
+    } else {
+        // ------------------------------------------------------------ epilogue (both CTAs; own 128 rows)
+        const uint32_t acce_leader = map_to_cta(acce0, 0);
+        const uint32_t lane_base = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(warp >> 2) * 128;
+        uint32_t it = 0;
+        bool ok = true;
+        for (long long tile = pair; ok && tile < total; tile += npairs) {
+            const At at = locate(tile);
+            PgTile t;
+            t.z = at.z * p.splits + at.split;
+            t.row = p.row0 + at.mt * kPgTile + (int)rank * 128 + (warp & 3) * 32 + lane;
+            t.col = at.nt * kPgTile + (warp >> 2) * 128;
+            t.zero = at.c0 >= at.c1;
+            Epi e;
+            e.begin(args, t);
+            if constexpr (!PROMOTE) {
+                uint32_t buf = it & 1;
+                if (!t.zero) {
+                    if (!mbar_wait(accf0 + buf * 8, (it >> 1) & 1, p.status, dead, kErrMmaWait)) { ok = false; break; }
+                    tc_fence_after();
+                    ++it;
+                }
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    float v[32];
+                    if (!t.zero) {
+                        tmem_ld32(lane_base + buf * 256 + h * 32, v);
+                        if (h == 3) {
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive_remote(acce_leader + buf * 8);
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = 0.0f;
+                    }
+                    e.chunk(args, t, h * 32, v);
+                }
+            } else {
+                float acc[4][32];
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) acc[h][i] = 0.0f;
+                for (int c0 = at.c0; c0 < at.c1; c0 = (at.c1 - c0 > seg) ? c0 + seg : at.c1, ++it) {
+                    const uint32_t buf = it & 1;
+                    if (!mbar_wait(accf0 + buf * 8, (it >> 1) & 1, p.status, dead, kErrMmaWait)) { ok = false; break; }
+                    tc_fence_after();
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        float v[32];
+                        tmem_ld32(lane_base + buf * 256 + h * 32, v);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) acc[h][i] += v[i];
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_remote(acce_leader + buf * 8);
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int h = 0; h < 4; ++h) e.chunk(args, t, h * 32, acc[h]);
+            }
+            e.end(args, t);
+        }
+    }
+
+    // the even CTA's barriers receive arrivals from the odd CTA until it is done: leave together
+    tc_fence_before();
+    __syncthreads();
+    cluster_arrive_release();
+    cluster_wait_acquire();
+    if (warp == 0) tmem_dealloc_pair(tmem_base, 512);
+}
+
+// A stack of `z` matrices [rows][cols] (bf16, rows `ld` elements apart, matrices `zstride` elements apart) as an operand.
+// K-major: boxes of 64 columns x 128 rows; MN-major: 64 columns x 64 rows, two side by side.
+inline int plane_map(CUtensorMap *m, const void *base, int mn_major, int64_t rows, int64_t cols, int64_t ld, int64_t zstride, int64_t z)
+{
+    const uint64_t dims[3] = {(uint64_t)cols, (uint64_t)rows, (uint64_t)z};
+    const uint64_t strides[2] = {(uint64_t)ld * 2, (uint64_t)zstride * 2};
+    const uint32_t box[3] = {64, mn_major ? 64u : 128u, 1};
+    return encode_tmap_nd(m, base, 2, 3, dims, strides, box, 128);
+}
+
+template <int AMN, int BMN, int SCHEME, bool PROMOTE, class Epi>
+int launch_plane_gemm(const CUtensorMap &tm_a, const CUtensorMap &tm_b, const PlaneGemm &p, const typename Epi::Args &args, cudaStream_t s)
+{
+    const auto kern = plane_gemm_kernel<AMN, BMN, SCHEME, PROMOTE, Epi>;
+    static PerDeviceCache cache;
+    int pairs = cache.get();
+    if (pairs < 0) {
+        MONARCH_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kPgSmem));
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(2, 1, 1);
+        cfg.blockDim = dim3(kPgThreads, 1, 1);
+        cfg.dynamicSmemBytes = kPgSmem;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = 2; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        MONARCH_CUDA_TRY(cudaOccupancyMaxActiveClusters(&pairs, kern, &cfg));
+        cache.set(pairs);
+    }
+    if (pairs < 1) return MONARCH_ERR_CUDA;
+    const long long total = (long long)((p.rows + kPgTile - 1) / kPgTile) * ((p.cols + kPgTile - 1) / kPgTile) * p.batches * p.splits;
+    if (total <= 0) return MONARCH_OK;
+    const int grid = 2 * (int)(total < pairs ? total : pairs);
+    return launch_serialized(kern, dim3((unsigned)grid), kPgThreads, kPgSmem, s, tm_a, tm_b, p, args);
+}
+
+}  // namespace tc
+}  // namespace monarch

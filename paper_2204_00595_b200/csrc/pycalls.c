@@ -5,7 +5,7 @@
  * Call(name, address, spec, names, float_types, on_error, stream_of) is a callable object.  spec has one letter per
  * positional argument, in the order of the C function's parameters:
  *   t  tensor of the storage dtype (the first one decides which)      f  float32 tensor       q  int64 tensor
- *   i  integer     w  workspace: object with ptr and nbytes, or (ptr, nbytes); two C parameters
+ *   i  integer     d  float (double)     w  workspace: object with ptr and nbytes, or (ptr, nbytes); two C parameters
  *   v  workspace pointer, or None     s  stream: None (the current one), an integer, or an object with cuda_stream
  *   D  (no argument) the dtype code
  * None as a tensor is a null pointer.  A non-zero status is given to on_error(status, name). */
@@ -24,6 +24,14 @@ typedef int (*apply_fn)(void *, const uint64_t *);
 #define I(k) ((int32_t)a[k])
 #define L(k) ((int64_t)a[k])
 #define Z(k) ((size_t)a[k])
+#define Q(k) ((const int64_t *)(uintptr_t)a[k])
+static double as_double(uint64_t bits)
+{
+    double v;
+    memcpy(&v, &bits, sizeof v);
+    return v;
+}
+#define D(k) as_double(a[k])
 #define APPLY(name, ...) \
     static int apply_##name(void *fn, const uint64_t *a) { return ((__typeof__(name) *)fn)(__VA_ARGS__); }
 APPLY(monarch_fwd, P(0), P(1), P(2), P(3), L(4), I(5), I(6), I(7), P(8), Z(9), P(10))
@@ -39,6 +47,10 @@ APPLY(monarch_rect_bwd, P(0), P(1), P(2), P(3), P(4), P(5), F(6), F(7), I(8), L(
 APPLY(monarch_cplx_fwd, P(0), P(1), P(2), P(3), I(4), L(5), I(6), I(7), I(8), P(9), Z(10), P(11))
 APPLY(monarch_dense, P(0), P(1), P(2), I(3), I(4), I(5), P(6))
 APPLY(monarch_project, P(0), P(1), P(2), I(3), I(4), I(5), (unsigned long long *)P(6), P(7))
+APPLY(monarch_xent_fwd, P(0), P(1), Q(2), F(3), F(4), L(5), I(6), I(7), L(8), I(9), P(10), Z(11), P(12))
+APPLY(monarch_xent_bwd, P(0), P(1), Q(2), F(3), F(4), P(5), F(6), I(7), L(8), I(9), I(10), L(11), I(12), P(13), Z(14), P(15))
+APPLY(monarch_orthogonalize, P(0), P(1), L(2), I(3), I(4), I(5), I(6), P(7), Z(8), P(9))
+APPLY(monarch_muon_step, P(0), F(1), F(2), L(3), I(4), I(5), D(6), D(7), D(8), I(9), D(10), I(11), I(12), P(13), Z(14), P(15))
 
 static const struct { const char *name; apply_fn apply; int params; } kCalls[] = {
     {"monarch_fwd", apply_monarch_fwd, 11},         {"monarch_bwd_dx", apply_monarch_bwd_dx, 11},
@@ -46,7 +58,9 @@ static const struct { const char *name; apply_fn apply; int params; } kCalls[] =
     {"monarch_mlp_fwd", apply_monarch_mlp_fwd, 15}, {"monarch_mlp_bwd", apply_monarch_mlp_bwd, 22},
     {"monarch_rect_fwd", apply_monarch_rect_fwd, 13}, {"monarch_rect_bwd", apply_monarch_rect_bwd, 18},
     {"monarch_cplx_fwd", apply_monarch_cplx_fwd, 12}, {"monarch_dense", apply_monarch_dense, 7},
-    {"monarch_project", apply_monarch_project, 8},
+    {"monarch_project", apply_monarch_project, 8},  {"monarch_xent_fwd", apply_monarch_xent_fwd, 13},
+    {"monarch_xent_bwd", apply_monarch_xent_bwd, 16}, {"monarch_orthogonalize", apply_monarch_orthogonalize, 10},
+    {"monarch_muon_step", apply_monarch_muon_step, 16},
 };
 
 typedef struct {
@@ -146,6 +160,12 @@ static PyObject *call_it(PyObject *self, PyObject *const *args, size_t nargsf, P
         switch (kind) {
             case 'D': dtype_at = out++; break;
             case 'i': if (to_u64(v, &a[out++])) return NULL; break;
+            case 'd': {
+                const double f = PyFloat_AsDouble(v);
+                if (f == -1.0 && PyErr_Occurred()) return NULL;
+                memcpy(&a[out++], &f, sizeof f);
+                break;
+            }
             case 'w': if (workspace_of(v, &a[out], &a[out + 1])) return NULL; out += 2; break;
             case 'v':
                 a[out] = 0;
@@ -189,7 +209,7 @@ static PyObject *call_new(PyTypeObject *type, PyObject *args, PyObject *kw)
     if (len > MAX_ARGS || PyTuple_GET_SIZE(types) != 3) { PyErr_SetString(PyExc_ValueError, "bad spec"); return NULL; }
     int n_args = 0, params = 0;
     for (Py_ssize_t i = 0; i < len; ++i) {
-        if (strchr("tfqiwvsD", spec[i]) == NULL) { PyErr_SetString(PyExc_ValueError, "bad spec"); return NULL; }
+        if (strchr("tfqidwvsD", spec[i]) == NULL) { PyErr_SetString(PyExc_ValueError, "bad spec"); return NULL; }
         n_args += spec[i] != 'D';
         params += spec[i] == 'w' ? 2 : 1;
     }

@@ -1,0 +1,634 @@
+// Softmax cross entropy of token rows against a vocabulary matrix, without the logits in memory, and its gradient:
+//   z[t][v] = sum_i x[t][i] W[v][i],  lse[t] = log sum_v exp z[t][v],  loss[t] = lse[t] - z[t][target[t]]
+//   g[t][v] = dloss[t] (exp(z[t][v] - lse[t]) - [v == target[t]]),  dx = g W,  dW = g^T x
+// (the paper trains language models, Section 5; the loss itself has no counterpart in its text).
+//
+// All three products run on plane_gemm.cuh.  Tokens whose target is ignore_index are taken out first: a preparation kernel copies
+// the rows of x that count to the front of a buffer (fp32: split into three bf16 planes; rows whose length is no multiple of 8
+// padded, for TMA), so that nothing is computed for the others and what they hold (NaN, say) reaches no sum.
+//   forward   logits tile in tensor memory -> per row the maximum and the sum of exponentials of its 128 columns -> one pair per
+//             row and half tile in memory -> a warp per row joins them
+//   backward  per piece of the vocabulary: logits again, g as bf16 planes in memory, then dW = g^T x and dx += g W from them.
+// Planes of g.  fp32: three, all six plane products.  bf16: two for dW, a float32 result, whose terms of 2^-17 error each (rms
+// 4e-6) average out over the tokens (2.7e-6 of dW's norm at 2900 tokens, logits' errors included); up to kFewTokens tokens, where
+// they do not, three, which costs nothing there: the time goes into reading W and writing dW.  A bf16 dx takes the first plane
+// (2^-8 per term, as much as its own rounding), of few tokens two.
+#include "plane_gemm.cuh"
+
+namespace monarch {
+namespace tc {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kFewTokens = 64;
+constexpr int kTokenChunk = 32768;              // tokens whose partial sums are in memory at a time (forward)
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// ------------------------------------------------------------------------------------------------ preparation
+struct PrepArgs {
+    const void *x;
+    const int64_t *targets;
+    const float *lse_in, *dloss;      // backward
+    float *loss, *lse;                // forward: zeroed for the rows that are left out
+    void *dx;                         // backward: likewise
+    int *count, *map, *tgt;           // rows that count; compact row -> row; compact row -> target (-1: out of range)
+    float *clse, *cdl;                // backward: lse and dloss of the compact rows
+    __nv_bfloat16 *xp;                // planes [planes][tokens][dp]
+    int64_t ignore;
+    int tokens, d, dp, vocab, rows_per_cta;
+};
+
+// fp32 value -> bf16 planes.  The largest fp32 values round to infinity in bf16: they are cut instead.
+template <int PL> __device__ __forceinline__ void split(float v, __nv_bfloat16 (&o)[PL])
+{
+    const float inf = __int_as_float(0x7f800000);
+#pragma unroll
+    for (int i = 0; i < PL; ++i) {
+        o[i] = __float2bfloat16_rn(v);
+        if (PL > 1 && i == 0 && fabsf(__bfloat162float(o[0])) == inf) o[0] = __float2bfloat16_rz(v);
+        v -= __bfloat162float(o[i]);
+        if (i == 0 && !(fabsf(v) < inf)) v = 0.0f;             // infinite or NaN: all of it is in the first plane
+    }
+}
+
+template <typename T, int PL>
+__device__ __forceinline__ void copy_row(const T *__restrict__ src, __nv_bfloat16 *dst, size_t plane, int d, int dp, int lane)
+{
+    if constexpr (sizeof(T) == 2) {
+        if (d == dp) {
+            for (int c = lane * 8; c < dp; c += 256) *reinterpret_cast<uint4 *>(dst + c) = __ldg(reinterpret_cast<const uint4 *>(src + c));
+            return;
+        }
+    }
+    for (int c = lane * 2; c < dp; c += 64) {
+        __nv_bfloat16 a[PL], b[PL];
+        split<PL>(c < d ? elem<T>::load(src + c) : 0.0f, a);
+        split<PL>(c + 1 < d ? elem<T>::load(src + c + 1) : 0.0f, b);
+#pragma unroll
+        for (int i = 0; i < PL; ++i) *reinterpret_cast<__nv_bfloat162 *>(dst + i * plane + c) = __nv_bfloat162(a[i], b[i]);
+    }
+}
+
+template <typename T, int PL, bool BWD>
+__global__ void __launch_bounds__(256) xent_prep_kernel(const PrepArgs p)
+{
+    __shared__ int s_part[2][8], s_dst[256];
+    depend_wait();
+    depend_launch();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int first = blockIdx.x * p.rows_per_cta, last = min(p.tokens, first + p.rows_per_cta);
+    int before = 0, total = 0;
+    for (int t = tid; t < p.tokens; t += 256) {
+        const int keep = __ldg(p.targets + t) != p.ignore;
+        total += keep;
+        before += keep & (t < first);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        before += __shfl_xor_sync(~0u, before, o);
+        total += __shfl_xor_sync(~0u, total, o);
+    }
+    if (lane == 0) { s_part[0][warp] = before; s_part[1][warp] = total; }
+    __syncthreads();
+    before = total = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) { before += s_part[0][w]; total += s_part[1][w]; }
+    if (blockIdx.x == 0 && tid == 0) *p.count = total;
+
+    const T *x = (const T *)p.x;
+    const size_t plane = (size_t)p.tokens * p.dp;
+    for (int base = first; base < last; base += 256) {
+        const int t = base + tid;
+        int64_t y = p.ignore;
+        if (t < last) y = __ldg(p.targets + t);
+        const bool keep = t < last && y != p.ignore;
+        const unsigned mask = __ballot_sync(~0u, keep);
+        __syncthreads();                                     // s_part and s_dst of the rows before are read
+        if (lane == 0) s_part[0][warp] = __popc(mask);
+        __syncthreads();
+        int at = before + __popc(mask & ((1u << lane) - 1)), all = 0;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            all += s_part[0][w];
+            if (w < warp) at += s_part[0][w];
+        }
+        before += all;
+        s_dst[tid] = keep ? at : -1;
+        if (keep) {
+            const bool good = y >= 0 && y < p.vocab;
+            p.map[at] = t;
+            p.tgt[at] = good ? (int)y : -1;
+            if (BWD) {
+                p.clse[at] = p.lse_in[t];
+                p.cdl[at] = good ? p.dloss[t] : __int_as_float(0x7fffffff);
+            }
+        } else if (t < last && !BWD) {
+            p.loss[t] = 0.0f;
+            p.lse[t] = 0.0f;
+        }
+        __syncthreads();
+        for (int r = warp; r < 256 && base + r < last; r += 8) {
+            const int dst = s_dst[r];
+            if (dst >= 0)
+                copy_row<T, PL>(x + (size_t)(base + r) * p.d, p.xp + (size_t)dst * p.dp, plane, p.d, p.dp, lane);
+            else if (BWD)
+                for (int c = lane; c < p.d; c += 32) elem<T>::store((T *)p.dx + (size_t)(base + r) * p.d + c, 0.0f);
+            if (base + r >= total)                           // rows behind the last one that counts enter sums over tokens as zeros
+                for (int i = 0; i < PL; ++i)
+                    for (int c = lane * 8; c < p.dp; c += 256)
+                        *reinterpret_cast<uint4 *>(p.xp + i * plane + (size_t)(base + r) * p.dp + c) = make_uint4(0, 0, 0, 0);
+        }
+    }
+}
+
+// rows [rows][d] -> planes [PL][rows_max][dp]
+template <typename T, int PL>
+__global__ void __launch_bounds__(256) split_rows_kernel(const T *__restrict__ W, __nv_bfloat16 *wp, int rows, size_t plane, int d, int dp)
+{
+    depend_wait();
+    depend_launch();
+    for (int r = blockIdx.x * 8 + (threadIdx.x >> 5); r < rows; r += gridDim.x * 8)
+        copy_row<T, PL>(W + (size_t)r * d, wp + (size_t)r * dp, plane, d, dp, threadIdx.x & 31);
+}
+
+// ------------------------------------------------------------------------------------------------ epilogues
+// Per row and 128 columns: r = log2(e) times the maximum, rounded, and s = sum 2^(z log2 e - r).  Exponents are formed by one FMA
+// from z and r, so the rounding of r cancels in r + log2 s.
+struct EpiStats {
+    struct Args {
+        float2 *part;              // [rows of the chunk][2 * column tiles]
+        float *tlogit;             // logit of the target
+        const int *tgt, *count;
+        int row0, cols, v0, halves, half0;
+    };
+    float m, s;
+    int y;
+    bool live;
+    __device__ __forceinline__ void begin(const Args &a, const PgTile &t)
+    {
+        m = __int_as_float(0xff800000);
+        s = 0.0f;
+        live = t.row < *a.count;
+        y = live ? a.tgt[t.row] - a.v0 - t.col : -1;
+    }
+    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32])
+    {
+        const int left = a.cols - t.col - c;
+        if (left <= 0) return;
+        if (left < 32) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (i >= left) v[i] = __int_as_float(0xff800000);
+        }
+        float top[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+        for (int i = 4; i < 32; ++i) top[i & 3] = fmaxf(top[i & 3], v[i]);
+        const float cm = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * kLog2e;
+        const float nm = fmaxf(m, cm);
+        const float base = nm == __int_as_float(0xff800000) ? 0.0f : nm;
+        float sum[4] = {s * ex2(m - base), 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < 32; ++i) sum[i & 3] += ex2(fmaf(v[i], kLog2e, -base));
+        s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        m = nm;
+        const int at = y - c;
+        if (live && at >= 0 && at < 32) {
+            float z = v[0];
+#pragma unroll
+            for (int i = 1; i < 32; ++i)
+                if (at == i) z = v[i];
+            a.tlogit[t.row] = z;
+        }
+    }
+    __device__ __forceinline__ void end(const Args &a, const PgTile &t)
+    {
+        if (live) a.part[(size_t)(t.row - a.row0) * a.halves + a.half0 + (t.col >> 7)] = make_float2(m, s);
+    }
+};
+
+// g of a piece of the vocabulary; zeros behind the last row and the last column
+template <int PL> struct EpiGrad {
+    struct Args {
+        __nv_bfloat16 *g;
+        size_t plane;
+        int ld, cols, v0;
+        const int *tgt, *count;
+        const float *lse, *dl;
+    };
+    float r_hi, r_lo, dl;
+    int y;
+    bool live;
+    __device__ __forceinline__ void begin(const Args &a, const PgTile &t)
+    {
+        live = t.row < *a.count;
+        const float l = live ? a.lse[t.row] : 0.0f;
+        r_hi = l * kLog2e;
+        r_lo = fmaf(l, kLog2e, -r_hi);
+        dl = live ? a.dl[t.row] : 0.0f;
+        y = live ? a.tgt[t.row] - a.v0 - t.col : -1;
+    }
+    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32])
+    {
+        const int left = live ? a.cols - t.col - c : 0, at = y - c;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const float e = ex2(fmaf(v[i], kLog2e, -r_hi) - r_lo);
+            v[i] = i >= left ? 0.0f : dl * (at == i ? e - 1.0f : e);
+        }
+        __nv_bfloat16 *out = a.g + (size_t)t.row * a.ld + t.col + c;
+#pragma unroll
+        for (int q = 0; q < PL; ++q, out += a.plane) {
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+                if (q + 1 < PL) {
+                    v[2 * i] -= __uint_as_float(w[i] << 16);
+                    v[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
+                }
+            }
+            st_v8(out, w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]);
+            st_v8(out + 16, w[8], w[9], w[10], w[11], w[12], w[13], w[14], w[15]);
+        }
+    }
+    __device__ __forceinline__ void end(const Args &, const PgTile &) {}
+};
+
+// rows of float32, stored or added to
+struct EpiStoreF32 {
+    struct Args {
+        float *out;
+        int rows, cols, add;
+    };
+    __device__ __forceinline__ void begin(const Args &, const PgTile &) {}
+    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32])
+    {
+        if (t.row >= a.rows) return;
+        const int left = a.cols - t.col - c;
+        float *out = a.out + (size_t)t.row * a.cols + t.col + c;
+        if ((a.cols & 7) == 0) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+                if (i >= left) break;
+                if (a.add) {
+                    const float4 o0 = *reinterpret_cast<const float4 *>(out + i), o1 = *reinterpret_cast<const float4 *>(out + i + 4);
+                    v[i] += o0.x; v[i + 1] += o0.y; v[i + 2] += o0.z; v[i + 3] += o0.w;
+                    v[i + 4] += o1.x; v[i + 5] += o1.y; v[i + 6] += o1.z; v[i + 7] += o1.w;
+                }
+                const uint32_t *w = reinterpret_cast<const uint32_t *>(v) + i;
+                *reinterpret_cast<uint4 *>(out + i) = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<uint4 *>(out + i + 4) = make_uint4(w[4], w[5], w[6], w[7]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (i < left) out[i] = a.add ? out[i] + v[i] : v[i];
+        }
+    }
+    __device__ __forceinline__ void end(const Args &, const PgTile &) {}
+};
+
+// dx: the sums of the pieces so far in float32 (compact rows), the last one to the caller's rows
+template <typename T> struct EpiDx {
+    struct Args {
+        float *acc;
+        T *dx;
+        const int *map, *count;
+        int d, first, last;
+    };
+    int to;
+    __device__ __forceinline__ void begin(const Args &a, const PgTile &t)
+    {
+        to = t.row < *a.count ? (a.last ? a.map[t.row] : t.row) : -1;
+    }
+    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32])
+    {
+        if (to < 0) return;
+        const int left = a.d - t.col - c;
+        const size_t col = (size_t)t.col + c;
+        float *acc = a.acc + (size_t)t.row * a.d + col;
+        const bool vec = (a.d & 7) == 0;
+#pragma unroll
+        for (int i = 0; i < 32; i += 8) {
+            if (i >= left) break;
+            if (vec) {
+                if (!a.first) {
+                    const float4 o0 = *reinterpret_cast<const float4 *>(acc + i), o1 = *reinterpret_cast<const float4 *>(acc + i + 4);
+                    v[i] += o0.x; v[i + 1] += o0.y; v[i + 2] += o0.z; v[i + 3] += o0.w;
+                    v[i + 4] += o1.x; v[i + 5] += o1.y; v[i + 6] += o1.z; v[i + 7] += o1.w;
+                }
+                const uint32_t *w = reinterpret_cast<const uint32_t *>(v) + i;
+                if (a.last && sizeof(T) == 2) {
+                    *reinterpret_cast<uint4 *>(a.dx + (size_t)to * a.d + col + i) =
+                        make_uint4(pack_bf16(v[i], v[i + 1]), pack_bf16(v[i + 2], v[i + 3]), pack_bf16(v[i + 4], v[i + 5]), pack_bf16(v[i + 6], v[i + 7]));
+                } else {
+                    float *o = a.last ? reinterpret_cast<float *>(a.dx) + (size_t)to * a.d + col + i : acc + i;
+                    *reinterpret_cast<uint4 *>(o) = make_uint4(w[0], w[1], w[2], w[3]);
+                    *reinterpret_cast<uint4 *>(o + 4) = make_uint4(w[4], w[5], w[6], w[7]);
+                }
+            } else {
+#pragma unroll
+                for (int j = i; j < i + 8; ++j)
+                    if (j < left) {
+                        const float r = a.first ? v[j] : v[j] + acc[j];
+                        if (a.last) elem<T>::store(a.dx + (size_t)to * a.d + col + j, r);
+                        else acc[j] = r;
+                    }
+            }
+        }
+    }
+    __device__ __forceinline__ void end(const Args &, const PgTile &) {}
+};
+
+// ------------------------------------------------------------------------------------------------ joining the parts
+__global__ void __launch_bounds__(256) xent_join_kernel(const float2 *__restrict__ part, const float *__restrict__ tlogit,
+                                                        const int *__restrict__ tgt, const int *__restrict__ map,
+                                                        const int *__restrict__ count, int row0, int rows, int halves, float *loss, float *lse)
+{
+    depend_wait();
+    depend_launch();
+    const int lane = threadIdx.x & 31, n = min(row0 + rows, *count);
+    for (int row = row0 + blockIdx.x * 8 + (threadIdx.x >> 5); row < n; row += gridDim.x * 8) {
+        const float2 *q = part + (size_t)(row - row0) * halves;
+        float m = __int_as_float(0xff800000);
+        for (int i = lane; i < halves; i += 32) m = fmaxf(m, q[i].x);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+        const float base = m == __int_as_float(0xff800000) ? 0.0f : m;
+        float s = 0.0f;
+        for (int i = lane; i < halves; i += 32) s += q[i].y * ex2(q[i].x - base);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
+        if (lane == 0) {
+            const float l = (base + log2f(s)) * kLn2;
+            const int to = map[row];
+            lse[to] = l;
+            loss[to] = tgt[row] >= 0 ? l - tlogit[row] : __int_as_float(0x7fffffff);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ host side
+size_t up(size_t v) { return (v + 255) & ~(size_t)255; }
+int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+constexpr int kPairs = 74;                      // CTA pairs of a B200, for choosing sizes; the launches ask the device
+
+struct Layout {
+    bool direct;                                // W is read where it is (bf16 rows of 16-byte multiples)
+    int planes, gplanes, dp, piece;             // planes of x and W, of g; padded row; vocabulary entries per piece
+    int chunk, halves, trows;
+    size_t count, map, tgt, lse, dl, tlogit, x, w, part, g, dx, total;
+};
+
+// Vocabulary entries per piece of the backward pass: whole 256-entry tiles, a plane of g within a quarter of a gigabyte, and
+// as few rounds of the pairs over the tiles of the three products as can be had.
+int bwd_piece(int64_t tokens, int d, int vocab)
+{
+    const int mt = tokens > 0 ? ceil_div(tokens, 256) : 1, nt = ceil_div(d, 256), vt = ceil_div(vocab, 256);
+    int most = (int)(((size_t)256 << 20) / ((size_t)mt * 256 * 256 * 2));
+    most = most < 1 ? 1 : most > vt ? vt : most;
+    int best = most;
+    double best_cost = 1e300;
+    const int fewest = ceil_div(vt, most);
+    for (int pieces = fewest; pieces < fewest + 16 && pieces <= vt; ++pieces) {
+        const int k = ceil_div(vt, pieces);
+        double cost = 0.0;
+        for (int left = vt, n = 0; left > 0 && n < 2; ++n) {                  // the full pieces, then the last one
+            const int now = left < k ? left : k, times = left < k ? 1 : left / k;
+            const double z = (double)ceil_div((int64_t)mt * now, kPairs) * nt, w = (double)ceil_div((int64_t)now * nt, kPairs) * mt * 2,
+                         x = (double)ceil_div((int64_t)mt * nt, kPairs) * now;
+            cost += times * (z + w + x + 24.0);                               // in tiles of 256 of K; a piece costs some 10 us
+            left -= times * now;
+        }
+        if (cost < best_cost) { best_cost = cost; best = k; }
+    }
+    return best * 256;
+}
+
+Layout layout(int64_t tokens, int d, int vocab, int dtype, bool bwd)
+{
+    Layout l;
+    l.direct = dtype == MONARCH_BF16 && d % 8 == 0;
+    l.planes = dtype == MONARCH_F32 ? 3 : 1;
+    l.gplanes = dtype == MONARCH_F32 || tokens <= kFewTokens ? 3 : 2;
+    l.dp = (d + 7) / 8 * 8;
+    l.chunk = (int)(tokens < kTokenChunk ? tokens : kTokenChunk);
+    l.trows = ceil_div(tokens, 256) * 256;
+    if (bwd) {
+        l.piece = bwd_piece(tokens, d, vocab);
+    } else {
+        l.piece = vocab;
+        if (!l.direct) {                                                      // planes of W within 128 MB
+            const int64_t most = ((int64_t)128 << 20) / ((int64_t)l.dp * 2 * l.planes) / 256 * 256;
+            if (most < vocab) l.piece = (int)(most < 256 ? 256 : most);
+        }
+    }
+    // half tiles of all pieces: full pieces are whole tiles
+    l.halves = 2 * ceil_div(vocab, 256);
+    size_t at = MONARCH_STATUS_BYTES;
+    auto take = [&](size_t bytes) { const size_t o = at; at += up(bytes); return o; };
+    const size_t t = (size_t)tokens;
+    l.count = take(4);
+    l.map = take(t * 4);
+    l.tgt = take(t * 4);
+    l.lse = l.dl = l.tlogit = l.part = l.g = l.dx = 0;
+    if (bwd) { l.lse = take(t * 4); l.dl = take(t * 4); }
+    else l.tlogit = take(t * 4);
+    l.x = take(t * l.dp * 2 * l.planes);
+    l.w = l.direct ? 0 : take((size_t)l.piece * l.dp * 2 * l.planes);
+    if (bwd) {
+        l.g = take((size_t)l.trows * l.piece * 2 * l.gplanes);
+        l.dx = take(t * d * 4);
+    } else {
+        l.part = take((size_t)l.chunk * l.halves * sizeof(float2));
+    }
+    l.total = at;
+    return l;
+}
+
+template <typename T, int PL, bool BWD> int prep(PrepArgs a, cudaStream_t s)
+{
+    // few rows per CTA while there are SMs without one; every CTA reads all targets
+    int rows = ceil_div(a.tokens, 4 * 148);
+    rows = rows < 8 ? 8 : rows;
+    a.rows_per_cta = rows;
+    return launch_serialized(xent_prep_kernel<T, PL, BWD>, dim3((unsigned)ceil_div(a.tokens, rows)), 256, 0, s, a);
+}
+
+template <bool BWD> int prep_any(const PrepArgs &a, int dtype, cudaStream_t s)
+{
+    return dtype == MONARCH_F32 ? prep<float, 3, BWD>(a, s) : prep<__nv_bfloat16, 1, BWD>(a, s);
+}
+
+int split_w(const void *W, void *wp, int v0, int rows, int piece, int d, int dp, int dtype, cudaStream_t s)
+{
+    const dim3 grid((unsigned)(ceil_div(rows, 8) < 148 * 8 ? ceil_div(rows, 8) : 148 * 8));
+    const size_t plane = (size_t)piece * dp;
+    if (dtype == MONARCH_F32)
+        return launch_serialized(split_rows_kernel<float, 3>, grid, 256, 0, s, (const float *)W + (size_t)v0 * d, (__nv_bfloat16 *)wp, rows, plane, d, dp);
+    return launch_serialized(split_rows_kernel<__nv_bfloat16, 1>, grid, 256, 0, s, (const __nv_bfloat16 *)W + (size_t)v0 * d, (__nv_bfloat16 *)wp, rows, plane, d, dp);
+}
+
+PlaneGemm gemm(unsigned *status)
+{
+    PlaneGemm g = {};
+    g.status = status;
+    g.batches = g.splits = 1;
+    return g;
+}
+
+// Logits.  An error of z is a relative error of g, so their sums in tensor memory end after 64 (bf16) or 48 (fp32) steps
+// (pg_seg); the loss alone takes less harm (bf16, d = 1024: 3.4e-7 of lse).
+template <int SCHEME, class Epi> int logits(const CUtensorMap &ma, const CUtensorMap &mb, PlaneGemm p, const typename Epi::Args &e, bool exact, cudaStream_t s)
+{
+    p.seg = pg_seg(SCHEME);
+    if (exact && p.kdim > p.seg * kPgChunk) return launch_plane_gemm<0, 0, SCHEME, true, Epi>(ma, mb, p, e, s);
+    return launch_plane_gemm<0, 0, SCHEME, false, Epi>(ma, mb, p, e, s);
+}
+
+}  // namespace
+}  // namespace tc
+
+size_t xent_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab, int dtype, int bwd)
+{
+    return tc::layout(tokens, d, vocab, dtype, bwd != 0).total;
+}
+
+int xent_fwd(const void *x, const void *W, const int64_t *targets, float *loss, float *lse, int64_t tokens, int32_t d, int32_t vocab,
+             int64_t ignore_index, int dtype, void *ws, cudaStream_t s)
+{
+    using namespace tc;
+    if (tokens == 0) return MONARCH_OK;
+    const Layout l = layout(tokens, d, vocab, dtype, false);
+    char *base = (char *)ws;
+    unsigned *status = (unsigned *)ws;
+    int *count = (int *)(base + l.count), *map = (int *)(base + l.map), *tgt = (int *)(base + l.tgt);
+    float *tlogit = (float *)(base + l.tlogit);
+    float2 *part = (float2 *)(base + l.part);
+    __nv_bfloat16 *xp = (__nv_bfloat16 *)(base + l.x);
+
+    PrepArgs a = {};
+    a.x = x; a.targets = targets; a.loss = loss; a.lse = lse;
+    a.count = count; a.map = map; a.tgt = tgt; a.xp = xp;
+    a.ignore = ignore_index; a.tokens = (int)tokens; a.d = d; a.dp = l.dp; a.vocab = vocab;
+    MONARCH_TRY(prep_any<false>(a, dtype, s));
+
+    CUtensorMap ma, mb;
+    MONARCH_TRY(plane_map(&ma, xp, 0, tokens, l.dp, l.dp, tokens * l.dp, l.planes));
+    for (int64_t row0 = 0; row0 < tokens; row0 += l.chunk) {
+        const int rows = (int)(tokens - row0 < l.chunk ? tokens - row0 : l.chunk);
+        for (int v0 = 0; v0 < vocab; v0 += l.piece) {
+            const int cols = vocab - v0 < l.piece ? vocab - v0 : l.piece;
+            PlaneGemm p = gemm(status);
+            p.count = count; p.row0 = (int)row0; p.rows = rows; p.cols = cols; p.kdim = d;
+            p.a_zstep = p.b_zstep = l.planes;
+            if (l.direct) {
+                MONARCH_TRY(plane_map(&mb, W, 0, vocab, d, d, (int64_t)vocab * d, 1));
+                p.b_n0 = v0;
+            } else {
+                MONARCH_TRY(split_w(W, base + l.w, v0, cols, l.piece, d, l.dp, dtype, s));
+                MONARCH_TRY(plane_map(&mb, base + l.w, 0, cols, l.dp, l.dp, (int64_t)l.piece * l.dp, l.planes));
+            }
+            const EpiStats::Args e = {part, tlogit, tgt, count, (int)row0, cols, v0, l.halves, v0 / 128};
+            if (dtype == MONARCH_F32) MONARCH_TRY((logits<kP3x3, EpiStats>(ma, mb, p, e, true, s)));
+            else MONARCH_TRY((logits<kP1, EpiStats>(ma, mb, p, e, d > 8192, s)));
+        }
+        const int ctas = ceil_div(rows, 8) < 148 * 8 ? ceil_div(rows, 8) : 148 * 8;
+        MONARCH_TRY(launch_serialized(xent_join_kernel, dim3((unsigned)ctas), 256, 0, s, (const float2 *)part, (const float *)tlogit,
+                                      (const int *)tgt, (const int *)map, (const int *)count, (int)row0, rows, l.halves, loss, lse));
+    }
+    return MONARCH_OK;
+}
+
+namespace tc {
+namespace {
+
+template <typename T, int LOGITS, int GP, int DW, int DX>
+int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate, int64_t tokens, int32_t d, int32_t vocab, int dtype, char *base, cudaStream_t s)
+{
+    unsigned *status = (unsigned *)base;
+    const int *count = (const int *)(base + l.count), *map = (const int *)(base + l.map), *tgt = (const int *)(base + l.tgt);
+    const float *clse = (const float *)(base + l.lse), *cdl = (const float *)(base + l.dl);
+    __nv_bfloat16 *xp = (__nv_bfloat16 *)(base + l.x), *g = (__nv_bfloat16 *)(base + l.g);
+    float *acc = (float *)(base + l.dx);
+    const size_t gplane = (size_t)l.trows * l.piece;
+
+    CUtensorMap x_k, x_n, w_k, w_n, g_m, g_k;
+    MONARCH_TRY(plane_map(&x_k, xp, 0, tokens, l.dp, l.dp, tokens * l.dp, l.planes));
+    MONARCH_TRY(plane_map(&x_n, xp, 1, tokens, l.dp, l.dp, tokens * l.dp, l.planes));
+    MONARCH_TRY(plane_map(&g_k, g, 0, l.trows, l.piece, l.piece, (int64_t)gplane, l.gplanes));
+    MONARCH_TRY(plane_map(&g_m, g, 1, l.trows, l.piece, l.piece, (int64_t)gplane, l.gplanes));
+    if (l.direct) {
+        MONARCH_TRY(plane_map(&w_k, W, 0, vocab, d, d, (int64_t)vocab * d, 1));
+        MONARCH_TRY(plane_map(&w_n, W, 1, vocab, d, d, (int64_t)vocab * d, 1));
+    }
+    for (int v0 = 0; v0 < vocab; v0 += l.piece) {
+        const int cols = vocab - v0 < l.piece ? vocab - v0 : l.piece;
+        if (!l.direct) {
+            MONARCH_TRY(split_w(W, base + l.w, v0, cols, l.piece, d, l.dp, dtype, s));
+            MONARCH_TRY(plane_map(&w_k, base + l.w, 0, cols, l.dp, l.dp, (int64_t)l.piece * l.dp, l.planes));
+            MONARCH_TRY(plane_map(&w_n, base + l.w, 1, cols, l.dp, l.dp, (int64_t)l.piece * l.dp, l.planes));
+        }
+        // g
+        PlaneGemm p = gemm(status);
+        p.count = count; p.rows = (int)tokens; p.cols = cols; p.kdim = d;
+        p.a_zstep = p.b_zstep = l.planes;
+        p.b_n0 = l.direct ? v0 : 0;
+        const typename EpiGrad<GP>::Args eg = {g, gplane, l.piece, cols, v0, tgt, count, clse, cdl};
+        MONARCH_TRY((logits<LOGITS, EpiGrad<GP>>(x_k, w_k, p, eg, true, s)));
+        // dW = g^T x
+        p = gemm(status);
+        p.count = count; p.count_is_k = 1; p.rows = cols; p.cols = d; p.kdim = (int)tokens;
+        p.a_zstep = GP; p.b_zstep = l.planes;
+        p.n_fastest = 1;
+        p.seg = pg_seg(DW);
+        const EpiStoreF32::Args ew = {dW + (size_t)v0 * d, cols, d, accumulate};
+        MONARCH_TRY((launch_plane_gemm<1, 1, DW, true, EpiStoreF32>(g_m, x_n, p, ew, s)));
+        // dx += g W
+        p = gemm(status);
+        p.count = count; p.rows = (int)tokens; p.cols = d; p.kdim = cols;
+        p.a_zstep = GP; p.b_zstep = l.planes;
+        p.b_k0 = l.direct ? v0 : 0;
+        p.n_fastest = 1;
+        p.seg = pg_seg(DX);
+        const typename EpiDx<T>::Args ex = {acc, dx, map, count, d, v0 == 0, v0 + cols == vocab};
+        MONARCH_TRY((launch_plane_gemm<0, 1, DX, DX != kP1, EpiDx<T>>(g_k, w_n, p, ex, s)));
+    }
+    return MONARCH_OK;
+}
+
+}  // namespace
+}  // namespace tc
+
+int xent_bwd(const void *x, const void *W, const int64_t *targets, const float *lse, const float *dloss, void *dx, float *dW, int accumulate,
+             int64_t tokens, int32_t d, int32_t vocab, int64_t ignore_index, int dtype, void *ws, cudaStream_t s)
+{
+    using namespace tc;
+    if (tokens == 0) {
+        if (!accumulate) MONARCH_CUDA_TRY(cudaMemsetAsync(dW, 0, (size_t)vocab * d * sizeof(float), s));
+        return MONARCH_OK;
+    }
+    const Layout l = layout(tokens, d, vocab, dtype, true);
+    char *base = (char *)ws;
+    PrepArgs a = {};
+    a.x = x; a.targets = targets; a.lse_in = lse; a.dloss = dloss; a.dx = dx;
+    a.count = (int *)(base + l.count); a.map = (int *)(base + l.map); a.tgt = (int *)(base + l.tgt);
+    a.clse = (float *)(base + l.lse); a.cdl = (float *)(base + l.dl);
+    a.xp = (__nv_bfloat16 *)(base + l.x);
+    a.ignore = ignore_index; a.tokens = (int)tokens; a.d = d; a.dp = l.dp; a.vocab = vocab;
+    MONARCH_TRY(prep_any<true>(a, dtype, s));
+    if (dtype == MONARCH_F32)
+        return bwd_pieces<float, kP3x3, 3, kP3x3, kP3x3>(l, W, (float *)dx, dW, accumulate, tokens, d, vocab, dtype, base, s);
+    if (l.gplanes == 3)
+        return bwd_pieces<__nv_bfloat16, kP1, 3, kP3x1, kP2x1>(l, W, (__nv_bfloat16 *)dx, dW, accumulate, tokens, d, vocab, dtype, base, s);
+    return bwd_pieces<__nv_bfloat16, kP1, 2, kP2x1, kP1>(l, W, (__nv_bfloat16 *)dx, dW, accumulate, tokens, d, vocab, dtype, base, s);
+}
+
+}  // namespace monarch
