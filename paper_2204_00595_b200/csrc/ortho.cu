@@ -20,22 +20,104 @@ template <typename T> struct Io {
     T *out;
     float keep, step, beta;    // W <- keep W - step O
     int nesterov;
-    // U of element i; the momentum is updated where `update` says so (once per call), else read as updated
-    __device__ __forceinline__ float u(size_t i, bool update) const
+    // Reads and writes are separate steps, so that a thread can have all its reads under way before its first write.
+    struct In {
+        float g, v;
+    };
+    __device__ __forceinline__ In fetch(size_t i) const
     {
-        if (V == nullptr) return elem<T>::load((const T *)in + i);
-        const float g = ((const float *)in)[i];
-        float v = V[i];
-        if (update) {
-            v = fmaf(beta, v, g);
-            V[i] = v;
-        }
-        return nesterov ? fmaf(beta, v, g) : v;
+        if (V == nullptr) return {elem<T>::load((const T *)in + i), 0.0f};
+        return {((const float *)in)[i], V[i]};
     }
-    __device__ __forceinline__ void write(size_t i, float o) const
+    // U of element i; the momentum is updated where `update` says so (once per call), else `f.v` is the updated one
+    __device__ __forceinline__ float u(size_t i, In f, bool update) const
     {
-        if (V == nullptr) elem<T>::store(out + i, o);
-        else elem<T>::store(out + i, keep * elem<T>::load(out + i) - step * o);
+        if (V == nullptr) return f.g;
+        if (update) {
+            f.v = fmaf(beta, f.v, f.g);
+            V[i] = f.v;
+        }
+        return nesterov ? fmaf(beta, f.v, f.g) : f.v;
+    }
+    // the same for four consecutive elements, i a multiple of 4
+    struct In4 {
+        float g[4], v[4];
+    };
+    static __device__ __forceinline__ void load4(const float *p, float (&o)[4])
+    {
+        const float4 t = *reinterpret_cast<const float4 *>(p);
+        o[0] = t.x; o[1] = t.y; o[2] = t.z; o[3] = t.w;
+    }
+    static __device__ __forceinline__ void load4(const __nv_bfloat16 *p, float (&o)[4])
+    {
+        const uint2 t = *reinterpret_cast<const uint2 *>(p);
+        o[0] = __uint_as_float(t.x << 16); o[1] = __uint_as_float(t.x & 0xffff0000u);
+        o[2] = __uint_as_float(t.y << 16); o[3] = __uint_as_float(t.y & 0xffff0000u);
+    }
+    static __device__ __forceinline__ void store4(float *p, const float (&o)[4]) { *reinterpret_cast<float4 *>(p) = make_float4(o[0], o[1], o[2], o[3]); }
+    static __device__ __forceinline__ void store4(__nv_bfloat16 *p, const float (&o)[4])
+    {
+        *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
+    }
+    __device__ __forceinline__ In4 fetch4(size_t i) const
+    {
+        In4 f = {};
+        if (V == nullptr) {
+            load4((const T *)in + i, f.g);
+        } else {
+            load4((const float *)in + i, f.g);
+            load4(V + i, f.v);
+        }
+        return f;
+    }
+    __device__ __forceinline__ void u4(size_t i, In4 &f, float (&o)[4]) const
+    {
+        if (V == nullptr) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = f.g[e];
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            f.v[e] = fmaf(beta, f.v[e], f.g[e]);
+            o[e] = nesterov ? fmaf(beta, f.v[e], f.g[e]) : f.v[e];
+        }
+        store4(V + i, f.v);
+    }
+    __device__ __forceinline__ void old4(size_t i, float (&w)[4]) const
+    {
+        if (V != nullptr) load4(out + i, w);
+    }
+    __device__ __forceinline__ void write4(size_t i, float (&o)[4], const float (&w)[4]) const
+    {
+        if (V != nullptr) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(keep, w[e], -step * o[e]);
+        }
+        store4(out + i, o);
+    }
+    __device__ __forceinline__ float old(size_t i) const { return V == nullptr ? 0.0f : elem<T>::load(out + i); }
+    __device__ __forceinline__ void write(size_t i, float o, float w) const
+    {
+        elem<T>::store(out + i, V == nullptr ? o : fmaf(keep, w, -step * o));
+    }
+};
+
+// Element e = thread, thread + threads, .. of a row-major block as (row, column), without a division per element
+struct Walk {
+    int r, c, dr, dc, cols;
+    __device__ __forceinline__ Walk(int first, int stride, int cols_) : cols(cols_)
+    {
+        r = first / cols;
+        c = first - r * cols;
+        dr = stride / cols;
+        dc = stride - dr * cols;
+    }
+    __device__ __forceinline__ void next()
+    {
+        r += dr;
+        c += dc;
+        if (c >= cols) { c -= cols; ++r; }
     }
 };
 
@@ -71,7 +153,7 @@ __global__ void __launch_bounds__(kSmallThreads) ortho_small_kernel(const Io<T> 
     double q = 0.0;
     for (int i = tid; i < size; i += kSmallThreads) {
         const int r = i / cols, c = i - r * cols;
-        const float u = io.u(base + i, true);
+        const float u = io.u(base + i, io.fetch(base + i), true);
         q += (double)u * u;
         X[wide ? r * ldn + c : c * ldn + r] = u;
     }
@@ -158,7 +240,515 @@ __global__ void __launch_bounds__(kSmallThreads) ortho_small_kernel(const Io<T> 
     }
     for (int i = tid; i < size; i += kSmallThreads) {
         const int r = i / cols, c = i - r * cols;
-        io.write(base + i, X[wide ? r * ldn + c : c * ldn + r]);
+        io.write(base + i, X[wide ? r * ldn + c : c * ldn + r], io.old(base + i));
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ blocks up to 64 x 128
+// One CTA per block, everything on chip: X, S and P = b S + c S^2 are bf16 planes in shared memory (PL = 2 for bf16 results, 3 for
+// fp32), their fp32 values stay in the registers of the thread that holds them as an accumulator, warp-level MMAs (m16n8k16).
+// S is symmetric, so S and P serve as either operand as stored; only P X needs X transposed (ldmatrix.trans).  tcgen05 is little gain
+// here: 15 dependent products of 64 x 64 x 64.  128 blocks of 64 x 64, optimiser step: bf16 15.3 us (1.8 a step), fp32 22.2 (3.3 a step);
+// with fp32 FMA 75.
+// KP, NP: k and n rounded up; warps: KP / 16 rows of tiles times two column halves.
+template <int KP, int NP, int PL> struct BlockCfg {
+    static constexpr int kRows = KP / 16, kThreads = kRows * 2 * 32;
+    static constexpr int kLdX = NP + 8, kLdS = KP + 8;                       // rows 16 bytes apart in their banks
+    static constexpr int kXPlane = KP * kLdX, kSPlane = KP * kLdS;           // elements
+    static constexpr int kSmem = (2 * PL * kXPlane + 2 * PL * kSPlane) * 2;
+    static constexpr int kS = KP / 16, kX = NP / 16;                         // 8-column tiles of a warp in S and in X
+};
+
+// acc[t] += A B for T column tiles of 8.  A: planes at `a` (row-major, 16 rows of this warp), B: planes at `b`, TRANS: stored [k][n].
+template <int PL, int KSTEPS, int T, bool TRANS>
+__device__ __forceinline__ void plane_mma(float (&acc)[T][4], uint32_t a, uint32_t aplane, int lda, uint32_t b, uint32_t bplane, int ldb)
+{
+    const int lane = threadIdx.x & 31, mtx = lane >> 3, r = lane & 7;
+    // A: matrices (rows 0-7, k 0-7), (rows 8-15, k 0-7), (rows 0-7, k 8-15), (rows 8-15, k 8-15)
+    const uint32_t a_at = a + ((mtx & 1) * 8 + r) * lda * 2 + (mtx >> 1) * 16;
+    // B, two column tiles at a time: (n 0-7, k 0-7), (n 0-7, k 8-15), (n 8-15, k 0-7), (n 8-15, k 8-15)
+    const uint32_t b_at = TRANS ? b + ((mtx & 1) * 8 + r) * ldb * 2 + (mtx >> 1) * 16 : b + ((mtx >> 1) * 8 + r) * ldb * 2 + (mtx & 1) * 16;
+#pragma unroll
+    for (int k = 0; k < KSTEPS; ++k) {
+        uint32_t fa[PL][4];
+#pragma unroll
+        for (int q = 0; q < PL; ++q) ldm4(fa[q], a_at + q * aplane + k * 32);
+#pragma unroll
+        for (int t = 0; t < T; t += 2) {
+            uint32_t fb[PL][4];
+#pragma unroll
+            for (int q = 0; q < PL; ++q) {
+                if constexpr (TRANS) ldm4t(fb[q], b_at + q * bplane + k * 16 * ldb * 2 + t * 16);
+                else ldm4(fb[q], b_at + q * bplane + t * 8 * ldb * 2 + k * 32);
+            }
+            // the small products first
+#pragma unroll
+            for (int o = PL - 1; o >= 0; --o)
+#pragma unroll
+                for (int q = o; q >= 0; --q) {
+                    mma(acc[t], fa[q], fb[o - q][0], fb[o - q][1]);
+                    if (t + 1 < T) mma(acc[t + 1], fa[q], fb[o - q][2], fb[o - q][3]);
+                }
+        }
+    }
+}
+
+// this thread's values of T column tiles as planes: rows row, row + 8
+template <int PL, int T> __device__ __forceinline__ void put_tiles(const float (&v)[T][4], __nv_bfloat16 *to, int plane, int ld)
+{
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float x = v[t][2 * h], y = v[t][2 * h + 1];
+#pragma unroll
+            for (int q = 0; q < PL; ++q) {
+                const uint32_t w = pack_bf16(x, y);
+                *reinterpret_cast<uint32_t *>(to + q * plane + h * 8 * ld + t * 8) = w;
+                x -= __uint_as_float(w << 16);
+                y -= __uint_as_float(w & 0xffff0000u);
+            }
+        }
+}
+
+template <typename T, int KP, int NP, int PL>
+__global__ void __launch_bounds__(BlockCfg<KP, NP, PL>::kThreads) ortho_block_kernel(const Io<T> io, int rows, int cols, int steps)
+{
+    using C = BlockCfg<KP, NP, PL>;
+    extern __shared__ __align__(16) __nv_bfloat16 smb[];
+    __shared__ double s_norm[C::kThreads / 32];
+    __nv_bfloat16 *Xs = smb, *Ss = smb + 2 * PL * C::kXPlane, *Ps = Ss + PL * C::kSPlane;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int row0 = (warp >> 1) * 16, half = warp & 1;
+    const int r = lane >> 2, c2 = (lane & 3) * 2;
+    const bool wide = rows <= cols;
+    const int k = wide ? rows : cols, n = wide ? cols : rows;
+    const int sr = wide ? cols : 1, sc = wide ? 1 : cols;                    // X[i][j] = G[i sr + j sc]
+    const size_t base = (size_t)blockIdx.x * rows * cols;
+    depend_wait();
+    depend_launch();
+
+    float x[C::kX][4];
+    typename Io<T>::In f[C::kX][4];
+    double q = 0.0;
+#pragma unroll
+    for (int t = 0; t < C::kX; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = row0 + r + (e >> 1) * 8, j = half * (NP / 2) + t * 8 + c2 + (e & 1);
+            f[t][e] = {0.0f, 0.0f};
+            if (i < k && j < n) f[t][e] = io.fetch(base + (size_t)(i * sr + j * sc));
+        }
+#pragma unroll
+    for (int t = 0; t < C::kX; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = row0 + r + (e >> 1) * 8, j = half * (NP / 2) + t * 8 + c2 + (e & 1);
+            const float u = i < k && j < n ? io.u(base + (size_t)(i * sr + j * sc), f[t][e], true) : 0.0f;
+            x[t][e] = u;
+            q += (double)u * u;
+        }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) q += __shfl_xor_sync(~0u, q, o);
+    if (lane == 0) s_norm[warp] = q;
+    __syncthreads();
+    q = 0.0;
+#pragma unroll
+    for (int w = 0; w < C::kThreads / 32; ++w) q += s_norm[w];
+    const double inv = 1.0 / (sqrt(q) + (double)kEps);                       // fp64: norms beyond the fp32 range
+#pragma unroll
+    for (int t = 0; t < C::kX; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[t][e] = (float)((double)x[t][e] * inv);
+
+    const int x_at = (row0 + r) * C::kLdX + half * (NP / 2) + c2, s_at = (row0 + r) * C::kLdS + half * (KP / 2) + c2;
+    put_tiles<PL>(x, Xs + x_at, C::kXPlane, C::kLdX);
+    const uint32_t s_a = smem_u32(Ss) + row0 * C::kLdS * 2, s_b = smem_u32(Ss) + half * (KP / 2) * C::kLdS * 2;
+    const uint32_t p_a = smem_u32(Ps) + row0 * C::kLdS * 2;
+    for (int it = 0; it < steps; ++it) {
+        __syncthreads();
+        const uint32_t X = smem_u32(Xs) + (it & 1) * (PL * C::kXPlane * 2);
+        float s[C::kS][4] = {}, p[C::kS][4] = {};
+        plane_mma<PL, NP / 16, C::kS, false>(s, X + row0 * C::kLdX * 2, C::kXPlane * 2, C::kLdX, X + half * (KP / 2) * C::kLdX * 2, C::kXPlane * 2, C::kLdX);
+        put_tiles<PL>(s, Ss + s_at, C::kSPlane, C::kLdS);
+        __syncthreads();
+        plane_mma<PL, KP / 16, C::kS, false>(p, s_a, C::kSPlane * 2, C::kLdS, s_b, C::kSPlane * 2, C::kLdS);
+#pragma unroll
+        for (int t = 0; t < C::kS; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[t][e] = fmaf(kB, s[t][e], kC * p[t][e]);
+        put_tiles<PL>(p, Ps + s_at, C::kSPlane, C::kLdS);
+        __syncthreads();
+        float y[C::kX][4] = {};
+        plane_mma<PL, KP / 16, C::kX, true>(y, p_a, C::kSPlane * 2, C::kLdS, X + half * NP, C::kXPlane * 2, C::kLdX);
+#pragma unroll
+        for (int t = 0; t < C::kX; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[t][e] = fmaf(kA, x[t][e], y[t][e]);
+        if (it + 1 < steps) put_tiles<PL>(x, Xs + ((it + 1) & 1) * PL * C::kXPlane + x_at, C::kXPlane, C::kLdX);
+    }
+    float w[C::kX][4];
+#pragma unroll
+    for (int t = 0; t < C::kX; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = row0 + r + (e >> 1) * 8, j = half * (NP / 2) + t * 8 + c2 + (e & 1);
+            w[t][e] = i < k && j < n ? io.old(base + (size_t)(i * sr + j * sc)) : 0.0f;
+        }
+#pragma unroll
+    for (int t = 0; t < C::kX; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = row0 + r + (e >> 1) * 8, j = half * (NP / 2) + t * 8 + c2 + (e & 1);
+            if (i < k && j < n) io.write(base + (size_t)(i * sr + j * sc), x[t][e], w[t][e]);
+        }
+}
+
+template <typename T, int KP, int NP, int PL> int launch_block(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, cudaStream_t s)
+{
+    using C = BlockCfg<KP, NP, PL>;
+    return launch_serialized(ortho_block_kernel<T, KP, NP, PL>, dim3((unsigned)blocks), C::kThreads, C::kSmem, s, io, rows, cols, steps);
+}
+
+bool fits_block(int k, int n) { return k <= 64 && n <= 128; }
+
+template <typename T, int PL> int ortho_block(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, cudaStream_t s)
+{
+    const int k = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
+    if (k <= 16) {
+        if (n <= 16) return launch_block<T, 16, 16, PL>(io, blocks, rows, cols, steps, s);
+        if (n <= 32) return launch_block<T, 16, 32, PL>(io, blocks, rows, cols, steps, s);
+        if (n <= 64) return launch_block<T, 16, 64, PL>(io, blocks, rows, cols, steps, s);
+        return launch_block<T, 16, 128, PL>(io, blocks, rows, cols, steps, s);
+    }
+    if (k <= 32) {
+        if (n <= 32) return launch_block<T, 32, 32, PL>(io, blocks, rows, cols, steps, s);
+        if (n <= 64) return launch_block<T, 32, 64, PL>(io, blocks, rows, cols, steps, s);
+        return launch_block<T, 32, 128, PL>(io, blocks, rows, cols, steps, s);
+    }
+    if (n <= 64) return launch_block<T, 64, 64, PL>(io, blocks, rows, cols, steps, s);
+    return launch_block<T, 64, 128, PL>(io, blocks, rows, cols, steps, s);
+}
+
+// ------------------------------------------------------------------------------------------------ blocks up to 128 x 128
+// One CTA per block on the tcgen05 tensor cores, everything on chip: X and S in registers (thread = row and 16 columns of either
+// half), accumulators in tensor memory, operands as planes: the second one in shared memory as 128 x 64 slabs in the 128-byte
+// swizzle (K-major as stored; MN-major for the X of P X, whose rows are K), the first one in tensor memory, whose rows are the
+// threads' (both from shared memory take 8 KB for the 64 cycles of an MMA of 128 x 128 x 16, and 6 for the 32 of half of it: all
+// that an SM can read).  There is room there for two planes; of three, the third is read from shared
+// memory.  All 128 rows and columns are computed; those behind the block are zeros.
+//
+// A product is 8 K steps of 128 x 128 x 16 for each plane product, then: tensor memory -> fp32 -> planes of the next operand.  The
+// two overlap by column halves: the K steps that read the first 64 columns of an operand are issued as soon as those are written,
+// the others finish the first half of the result before the second, so that its values are converted meanwhile.
+// What a conversion overwrites (P over S, X over X) is the half that no MMA still under way reads.
+// Measured, 128 blocks of 128 x 128, optimiser step: bf16 27.5 us (3.7 a step: 2360 cycles a product, 1536 of them MMAs of three
+// plane products), fp32 43.6 (6.6 a step); with fp32 FMA 525.  The one thread that issues has to keep its operands in uniform
+// registers (elect_one): picked as thread 0 it took 60 cycles per MMA, 33.3 and 51.1 us.
+constexpr int kTcThreads = 512, kTcPlane = 128 * 128 * 2, kTcSlab = 128 * 128;
+template <int PL> constexpr int kTcSmem = 2 * PL * kTcPlane + 1024;
+
+struct KMajor { static constexpr bool value = false; };
+struct NMajor { static constexpr bool value = true; };
+
+// one lane of a converged warp; unlike lane == 0 it leaves the operands of what follows in uniform registers
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+// D[tmem] (+)= A[tmem] B[smem desc]
+__device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+                 "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// K half `kh` of A B for columns n0 .. n0 + N of B, all plane products, the small ones first.  A: planes 0 and 1 in tensor memory
+// (64 columns each), plane 2 in shared memory at `a2`.
+template <int PL, bool BMN, int N> __device__ __forceinline__ void tc_part(uint32_t d, uint32_t a, uint32_t a2, uint32_t b, int kh, int n0, uint32_t more)
+{
+    constexpr uint32_t idesc = make_idesc_bf16(128, N, 0, BMN);
+    a += kh * 32;
+    a2 += 2 * kTcPlane + kh * kTcSlab;
+    b += BMN ? (n0 >> 6) * kTcSlab + kh * 64 * 128 : kh * kTcSlab + n0 * 128;
+#pragma unroll
+    for (int o = PL - 1; o >= 0; --o)
+#pragma unroll
+        for (int q = o; q >= 0; --q) {
+            const uint64_t bd = BMN ? make_smem_desc(b + (o - q) * kTcPlane, kTcSlab, 1024, kSwizzle128) : make_smem_desc(b + (o - q) * kTcPlane, 16, 1024, kSwizzle128);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (q < 2) mma_f16_ts(d + n0, a + q * 64 + k * 8, bd + (BMN ? 128 : 2) * k, idesc, more);
+                else mma_f16_ss(d + n0, make_smem_desc(a2, 16, 1024, kSwizzle128) + 2 * k, bd + (BMN ? 128 : 2) * k, idesc, more);
+                more = 1;
+            }
+        }
+}
+
+// 16 values of a row (columns c .. c + 15 of a half) as planes: the first operand (tensor memory at `a`, the third plane in shared
+// memory), and if BOTH the second one (shared memory)
+template <int PL, bool BOTH> __device__ __forceinline__ void tc_put(uint32_t planes, uint32_t a, int row, int half, int c, float (&v)[16])
+{
+#pragma unroll
+    for (int q = 0; q < PL; ++q) {
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+            v[2 * e] -= __uint_as_float(w[e] << 16);
+            v[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
+        }
+        if (q < 2) tmem_st8(a + q * 64, w);
+        if (BOTH || q >= 2) {
+            const uint32_t at = planes + q * kTcPlane + half * kTcSlab + row * 128;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + ((((c >> 3) + j) ^ (row & 7)) << 4)), "r"(w[4 * j]), "r"(w[4 * j + 1]),
+                             "r"(w[4 * j + 2]), "r"(w[4 * j + 3])
+                             : "memory");
+        }
+    }
+}
+
+// 16 columns of this thread's lane, requested; tmem_ready names the registers so that nothing that reads them moves before it
+__device__ __forceinline__ void tmem_ask16(uint32_t taddr, float (&f)[16]) { tmem_ld16(taddr, reinterpret_cast<uint32_t (&)[16]>(f)); }
+__device__ __forceinline__ void tmem_ready(float (&f)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(f[0]), "+f"(f[1]), "+f"(f[2]), "+f"(f[3]), "+f"(f[4]), "+f"(f[5]), "+f"(f[6]), "+f"(f[7]), "+f"(f[8]), "+f"(f[9]),
+                   "+f"(f[10]), "+f"(f[11]), "+f"(f[12]), "+f"(f[13]), "+f"(f[14]), "+f"(f[15])
+                 :
+                 : "memory");
+}
+
+template <typename T, int PL>
+__global__ void __launch_bounds__(kTcThreads, 1) ortho_tc_kernel(const Io<T> io, int rows, int cols, int steps, unsigned *status)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bar_s[2];
+    __shared__ double s_norm[kTcThreads / 32];
+    __shared__ uint32_t tmem_base_s;
+    __shared__ int dead_s;
+    const uint32_t X = (smem_u32(smem_raw) + 1023u) & ~1023u, S = X + PL * kTcPlane, bar = smem_u32(bar_s);
+    float *stage = reinterpret_cast<float *>(smem_raw + (X - smem_u32(smem_raw)));       // 128 x 128 floats over the planes of X
+    const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;     // the same in all lanes, for the compiler too
+    const int row = (warp & 3) * 32 + lane, c0 = (warp >> 2) * 16;
+    const bool wide = rows <= cols;
+    const int size = rows * cols;
+    const size_t base = (size_t)blockIdx.x * size;
+    volatile int *dead = &dead_s;
+
+    if (tid == 0) {
+        mbar_init(bar, 1);
+        mbar_init(bar + 8, 1);
+        fence_mbar_init();
+        dead_s = 0;
+    }
+    if (warp == 0) {
+        tmem_alloc(smem_u32(&tmem_base_s), 512);
+        tmem_relinquish();
+    }
+    if (size < 128 * 128)
+        for (int i = tid * 4; i < 128 * 128; i += kTcThreads * 4) *reinterpret_cast<float4 *>(stage + i) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = __shfl_sync(~0u, tmem_base_s, 0);
+    depend_wait();
+    depend_launch();
+
+    // X[i][j] at stage[i * 128 + (j ^ (i & 31))]: consecutive values of G and one column of all rows are both in different banks
+    double q = 0.0;
+    const bool four = cols % 4 == 0;           // four values of a row at a time
+    Walk at(four ? 4 * tid : tid, four ? 4 * kTcThreads : kTcThreads, cols);
+    if (four) {
+        typename Io<T>::In4 f[8];
+#pragma unroll
+        for (int a = 0; a < 8; ++a)
+            if ((tid + a * kTcThreads) * 4 < size) f[a] = io.fetch4(base + (tid + a * kTcThreads) * 4);
+#pragma unroll
+        for (int a = 0; a < 8; ++a) {
+            if ((tid + a * kTcThreads) * 4 >= size) break;
+            float u[4];
+            io.u4(base + (tid + a * kTcThreads) * 4, f[a], u);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int i = wide ? at.r : at.c + b, j = wide ? at.c + b : at.r;
+                q += (double)u[b] * u[b];
+                stage[i * 128 + (j ^ (i & 31))] = u[b];
+            }
+            at.next();
+        }
+    } else
+    for (int e0 = tid; e0 < size; e0 += 8 * kTcThreads) {
+        typename Io<T>::In f[8];
+#pragma unroll
+        for (int a = 0; a < 8; ++a)
+            if (e0 + a * kTcThreads < size) f[a] = io.fetch(base + e0 + a * kTcThreads);
+#pragma unroll
+        for (int a = 0; a < 8; ++a) {
+            if (e0 + a * kTcThreads >= size) break;
+            const int i = wide ? at.r : at.c, j = wide ? at.c : at.r;
+            const float u = io.u(base + e0 + a * kTcThreads, f[a], true);
+            q += (double)u * u;
+            stage[i * 128 + (j ^ (i & 31))] = u;
+            at.next();
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) q += __shfl_xor_sync(~0u, q, o);
+    if (lane == 0) s_norm[warp] = q;
+    __syncthreads();
+    q = 0.0;
+#pragma unroll
+    for (int w = 0; w < kTcThreads / 32; ++w) q += s_norm[w];
+    const double inv = 1.0 / (sqrt(q) + (double)kEps);                       // fp64: norms beyond the fp32 range
+    float x[2][16];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[h][j] = (float)((double)stage[row * 128 + ((h * 64 + c0 + j) ^ lane)] * inv);
+    __syncthreads();
+
+    const uint32_t d_s = tmem, d_t = tmem + 128, d_x = tmem + 256, A = tmem + 384;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, mine = lanes + c0, a_mine = A + lanes + c0 / 2;
+    uint32_t phase = 0;
+    bool ok = true, stop = false;               // stop: some thread's wait ran out, the same in all threads
+    auto written = [&]() {                     // this half of the operands is written, and its accumulators are read
+        tmem_st_wait();
+        fence_proxy_async_smem();
+        tc_fence_before();
+        stop = __syncthreads_or(!ok);
+        tc_fence_after();
+    };
+    auto arrived = [&](int h) {
+        if (!mbar_wait(bar + h * 8, phase, status, dead, kErrMmaWait)) ok = false;
+        tc_fence_after();
+    };
+    // MMAs of a product with B at `b` (the third plane of A at `a2`): what the first half of the operands allows, or the rest
+    auto issue = [&](auto bmn, int h, uint32_t d, uint32_t a2, uint32_t b) {
+        if (warp != 0 || !elect_one()) return;
+        constexpr bool kBmn = decltype(bmn)::value;
+        if (h == 0) {
+            tc_part<PL, kBmn, 128>(d, A, a2, b, 0, 0, 0);
+        } else {
+            tc_part<PL, kBmn, 64>(d, A, a2, b, 1, 0, 1);
+            mma_commit(bar);
+            tc_part<PL, kBmn, 64>(d, A, a2, b, 1, 64, 1);
+            mma_commit(bar + 8);
+        }
+    };
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        float v[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = x[h][j];
+        tc_put<PL, true>(X, a_mine + h * 32, row, h, c0, v);
+    }
+    written();
+    issue(KMajor(), 0, d_s, X, X);
+    issue(KMajor(), 1, d_s, X, X);
+    for (int it = 0; it < steps; ++it) {
+        float s[2][16];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float v[16];
+            arrived(h);
+            tmem_ask16(d_s + mine + h * 64, v);
+            tmem_ready(v);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) s[h][j] = v[j];
+            tc_put<PL, true>(S, a_mine + h * 32, row, h, c0, v);
+            written();
+            issue(KMajor(), h, d_t, S, S);
+        }
+        phase ^= 1;
+        // P = b S + c S^2
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float v[16];
+            arrived(h);
+            tmem_ask16(d_t + mine + h * 64, v);
+            tmem_ready(v);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[j] = fmaf(kB, s[h][j], kC * v[j]);
+            tc_put<PL, false>(S, a_mine + h * 32, row, h, c0, v);
+            written();
+            issue(NMajor(), h, d_x, S, X);
+        }
+        phase ^= 1;
+        // X = a X + P X
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float v[16];
+            arrived(h);
+            tmem_ask16(d_x + mine + h * 64, v);
+            tmem_ready(v);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) x[h][j] = v[j] = fmaf(kA, x[h][j], v[j]);
+            if (it + 1 < steps) {
+                tc_put<PL, true>(X, a_mine + h * 32, row, h, c0, v);
+                written();
+                issue(KMajor(), h, d_s, X, X);
+            }
+        }
+        phase ^= 1;
+        if (stop) {
+            let_copies_land(dead);             // nor do MMAs outlive their shared memory
+            break;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0) tmem_dealloc(tmem, 512);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) stage[row * 128 + ((h * 64 + c0 + j) ^ lane)] = x[h][j];
+    __syncthreads();
+    at = Walk(four ? 4 * tid : tid, four ? 4 * kTcThreads : kTcThreads, cols);
+    if (four) {
+        float w[8][4];
+#pragma unroll
+        for (int a = 0; a < 8; ++a)
+            if ((tid + a * kTcThreads) * 4 < size) io.old4(base + (tid + a * kTcThreads) * 4, w[a]);
+#pragma unroll
+        for (int a = 0; a < 8; ++a) {
+            if ((tid + a * kTcThreads) * 4 >= size) break;
+            float o[4];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int i = wide ? at.r : at.c + b, j = wide ? at.c + b : at.r;
+                o[b] = stage[i * 128 + (j ^ (i & 31))];
+            }
+            io.write4(base + (tid + a * kTcThreads) * 4, o, w[a]);
+            at.next();
+        }
+    } else
+    for (int e0 = tid; e0 < size; e0 += 8 * kTcThreads) {
+        float w[8];
+#pragma unroll
+        for (int a = 0; a < 8; ++a)
+            if (e0 + a * kTcThreads < size) w[a] = io.old(base + e0 + a * kTcThreads);
+#pragma unroll
+        for (int a = 0; a < 8; ++a) {
+            if (e0 + a * kTcThreads >= size) break;
+            const int i = wide ? at.r : at.c, j = wide ? at.c : at.r;
+            io.write(base + e0 + a * kTcThreads, stage[i * 128 + (j ^ (i & 31))], w[a]);
+            at.next();
+        }
     }
 }
 
@@ -176,7 +766,7 @@ __global__ void __launch_bounds__(256) norm_kernel(const Io<T> io, double *part,
     const size_t base = (size_t)blockIdx.y * size;
     double q = 0.0;
     for (int64_t i = first + threadIdx.x; i < last; i += 256) {
-        const float u = io.u(base + i, true);
+        const float u = io.u(base + i, io.fetch(base + i), true);
         q += (double)u * u;
     }
 #pragma unroll
@@ -227,7 +817,7 @@ __global__ void __launch_bounds__(256) finish_kernel(const Finish f, const Io<T>
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
         float v;
         if (MODE == 0) {
-            v = (float)((double)io.u(base + i, false) * inv);
+            v = (float)((double)io.u(base + i, io.fetch(base + i), false) * inv);
         } else {
             const float *p = f.part + ((size_t)blockIdx.y * f.splits) * size + i;
             v = 0.0f;
@@ -236,7 +826,7 @@ __global__ void __launch_bounds__(256) finish_kernel(const Finish f, const Io<T>
             if (MODE == 3 || MODE == 4) v = fmaf(kA, f.f32[base + i], v);
         }
         if (MODE == 4) {
-            io.write(base + i, v);
+            io.write(base + i, v, io.old(base + i));
             continue;
         }
         if (MODE != 2) f.f32[base + i] = v;
@@ -369,6 +959,9 @@ int ortho_any(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, in
 {
     if (blocks == 0) return MONARCH_OK;
     const int k = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
+    if (fits_block(k, n)) return ortho_block<T, PL>(io, blocks, rows, cols, steps, s);
+    if (n <= 128)
+        return launch_serialized(ortho_tc_kernel<T, PL>, dim3((unsigned)blocks), kTcThreads, kTcSmem<PL>, s, io, rows, cols, steps, (unsigned *)ws);
     if (!fits_small(k, n)) return ortho_large<T, PL, SCHEME>(io, blocks, rows, cols, steps, dtype, ws, s);
     return launch_serialized(ortho_small_kernel<T>, dim3((unsigned)blocks), kSmallThreads, (int)(small_floats(k, n) * 4), s, io, rows, cols, steps);
 }
