@@ -451,13 +451,6 @@ template <int PL> constexpr int kTcSmem = 2 * PL * kTcPlane + 1024;
 struct KMajor { static constexpr bool value = false; };
 struct NMajor { static constexpr bool value = true; };
 
-// one lane of a converged warp; unlike lane == 0 it leaves the operands of what follows in uniform registers
-__device__ __forceinline__ bool elect_one()
-{
-    uint32_t p;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
-    return p != 0;
-}
 // D[tmem] (+)= A[tmem] B[smem desc]
 __device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
 {
@@ -884,7 +877,7 @@ Large large_layout(int64_t blocks, int rows, int cols, int dtype)
     l.split_p = split_for(blocks, l.k, l.k, l.k);
     l.split_x = split_for(blocks, rows, cols, l.k);
     const size_t kk = (size_t)l.k * l.k, rc = (size_t)rows * cols, b = (size_t)blocks;
-    size_t at = MONARCH_STATUS_BYTES;
+    size_t at = MONARCH_STATUS_BYTES + 65536;          // the status area and the counters of kernels that may share the workspace
     auto take = [&](size_t bytes) { const size_t o = at; at += up(bytes); return o; };
     l.norm = take(b * kNormParts * 8);
     l.x = take(b * rc * 4);
@@ -928,6 +921,7 @@ int ortho_large(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, 
     p.status = (unsigned *)ws;
     p.batches = (int)blocks;
     p.a_zstep = p.b_zstep = PL;
+    p.tn = 256;
     p.seg = SCHEME == kP3x3 ? pg_seg(SCHEME) : 16;         // bf16 results: 192 steps
     for (int i = 0; i < steps; ++i) {
         p.rows = p.cols = l.k;

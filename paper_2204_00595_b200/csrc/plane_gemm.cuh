@@ -10,8 +10,9 @@
 //
 //   C[m][n] = sum_k A(m, k) B(n, k)       A, B stored [rows][K] (K-major) or [K][rows] (MN-major), each with its own flag
 //
-// Persistent kernel on clusters of two CTAs, 256 x 256 output tiles: CTA r of a pair owns 128 rows of A and loads 128 of the
-// 256 rows of B; one MMA instruction of 256 x 256 x 16 runs on both SMs.  Shared memory is a ring of 16 KB operand tiles
+// Persistent kernel on clusters of two CTAs, output tiles of 256 rows and tn = 256 columns (192 or 128 where that fills the pairs
+// better: pg_tile): CTA r of a pair owns 128 rows of A and loads tn / 2 of the rows of B; one MMA instruction of 256 x tn x 16 runs
+// on both SMs.  Shared memory is a ring of 16 KB operand tiles
 // (128 x 64, 128-byte swizzle), loaded in the order in which the plane products use them, so that a tile of a plane is loaded
 // once per K chunk however many products it enters.  Two accumulators of 256 columns in tensor memory alternate.
 //   warps 0-7  epilogue: warp w reads rows 32 (w % 4) .. of column half w / 4
@@ -68,19 +69,42 @@ struct PlaneGemm {
     const int *count;          // device: rows that take part (token rows), or null
     int count_is_k;            // count bounds K (else M)
     int row0, rows;            // rows of M: row0 .. row0 + rows (rows clipped by *count - row0)
-    int cols;                  // columns of N
+    int cols, tn;              // columns of N; columns of a tile: 256, 128 or, K-major B only, 192
     int kdim;                  // contraction length (clipped by *count)
     int a_k0, b_k0;            // first K coordinate of the operands
     int b_n0;                  // first N coordinate of B
     int a_zstep, b_zstep;      // planes per matrix of a batch in the tensor maps
     int batches, splits;       // matrices; parts of K, each a product of its own (output index batch * splits + split)
+    int *splits_out;           // device: null, or `splits` is the most there may be, the kernel chooses (pg_cost) and says so here
+    const int *splits_in;      // device: null, or the number of parts
+    int lower;                 // symmetric result: only tiles whose block of 256 columns is not above the diagonal
     int n_fastest;             // neighbouring pairs take neighbouring column tiles (else row tiles)
     int seg;                   // K chunks per accumulation in tensor memory (kernels with PROMOTE)
 };
 
 struct PgTile {
-    int z, row, col, zero;     // output matrix; this thread's row; first of this warp's 128 columns; nothing was accumulated
+    int z, row, col;           // output matrix; this thread's row; first of this warp's columns (a half of the tile)
+    int half;                  // which half tile of the columns that is
+    int mirror;                // `lower`, off the diagonal: the transposed tile is this one's to write too
+    int zero;                  // nothing was accumulated
 };
+
+constexpr int kPgPairs = 74;       // CTA pairs of a B200: what sizes are chosen for (launches ask the device)
+
+// Time of `tiles` output tiles in `s` parts of K, in K chunks: rounds of the pairs over the parts; a part costs some 6 chunks more
+__host__ __device__ constexpr long long pg_cost(long long tiles, int kchunks, int s)
+{
+    return (tiles * s + kPgPairs - 1) / kPgPairs * ((kchunks + s - 1) / s + 6);
+}
+// Columns of a tile: the width that takes the pairs the fewest column rounds; narrower tiles reload A more often (a tenth, a fifth)
+inline int pg_tile(long long mtiles, int cols, bool any)
+{
+    auto cost = [&](int tn, int slow) { return (mtiles * ((cols + tn - 1) / tn) + kPgPairs - 1) / kPgPairs * tn * slow; };
+    int best = 256;
+    if (any && cost(192, 11) < cost(best, 10)) best = 192;
+    if (cost(128, 12) < cost(best, best == 192 ? 11 : 10)) best = 128;
+    return best;
+}
 
 __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap *m, int x, int y, int z, uint32_t bar)
 {
@@ -121,12 +145,20 @@ __device__ __forceinline__ void st_v8(void *p, uint32_t a, uint32_t b, uint32_t 
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e), "r"(f), "r"(g), "r"(h) : "memory");
 }
 
+// one lane of a converged warp; unlike lane == 0 it leaves the operands of what follows in uniform registers
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+
 struct PgBars {
     uint64_t full[kPgSlots], empty[kPgSlots];                           // full: used in the even CTA only
     uint64_t acc_full[2], acc_empty[2];
 };
 
-// Epi: struct with  begin(const Epi::Args &, const PgTile &),  chunk(args, tile, c, float (&v)[32])  for c = 0, 32, 64, 96,
+// Epi: struct with  begin(const Epi::Args &, const PgTile &),  chunk(args, tile, c, float (&v)[32])  for c = 0, 32, .. < tn / 2,
 // end(args, tile).  PROMOTE: at most p.seg chunks are accumulated in tensor memory, sums of those in fp32 registers.
 template <int AMN, int BMN, int SCHEME, bool PROMOTE, class Epi>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPgThreads, 1)
@@ -139,7 +171,7 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
     __shared__ int dead_s;
 
     const uint32_t ring0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;      // the same in all lanes, for the compiler too
     const uint32_t rank = cluster_ctarank();
     const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
     volatile int *dead = &dead_s;
@@ -167,7 +199,7 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
     cluster_arrive_release();                                           // both CTAs' barriers exist before any remote arrive
     cluster_wait_acquire();
     tc_fence_after();
-    const uint32_t tmem_base = tmem_base_s;
+    const uint32_t tmem_base = __shfl_sync(~0u, tmem_base_s, 0);
     depend_launch();
     depend_wait();
 
@@ -177,25 +209,49 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
         if (p.count_is_k) kdim = min(kdim, n);
         else rows = max(0, min(rows, n - p.row0));
     }
-    const int mtiles = (rows + kPgTile - 1) / kPgTile, ntiles = (p.cols + kPgTile - 1) / kPgTile;
+    const int tn = p.tn, sub = kPgTile / tn;                              // sub: with `lower`, tiles of a block of 256 columns
+    const int mtiles = (rows + kPgTile - 1) / kPgTile, ntiles = (p.cols + tn - 1) / tn;
     const int kchunks = (kdim + kPgChunk - 1) / kPgChunk;
-    const int per_split = (kchunks + p.splits - 1) / p.splits;
-    const long long plane_tiles = (long long)mtiles * ntiles, total = plane_tiles * p.batches * p.splits;
+    const long long plane_tiles = p.lower ? (long long)mtiles * (mtiles + 1) / 2 * sub : (long long)mtiles * ntiles;
+    int splits = p.splits_in != nullptr ? *p.splits_in : p.splits;
+    if (p.splits_out != nullptr) {
+        // the cheapest number of parts; every warp finds the same one
+        long long best = 0x7fffffffffffffffLL;
+        for (int s = lane + 1; s <= p.splits; s += 32) best = min(best, pg_cost(plane_tiles * p.batches, kchunks, s) << 10 | s);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) best = min(best, __shfl_xor_sync(~0u, best, o));
+        splits = (int)(best & 1023);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *p.splits_out = splits;
+    }
+    const int per_split = (kchunks + splits - 1) / splits;
+    const long long total = plane_tiles * p.batches * splits;
     const uint32_t full0 = smem_u32(bars.full), empty0 = smem_u32(bars.empty);
     const uint32_t accf0 = smem_u32(bars.acc_full), acce0 = smem_u32(bars.acc_empty);
     constexpr int kLoads = pg_loads(SCHEME);
     const int seg = PROMOTE ? p.seg : 0x7fffffff;
 
     struct At {
-        int z, split, mt, nt, c0, c1;
+        int z, split, mt, nt, c0, c1, mirror;
     };
     auto locate = [&](long long tile) {
         At a;
         const int zz = (int)(tile / plane_tiles), t = (int)(tile % plane_tiles);
-        a.z = zz / p.splits;
-        a.split = zz % p.splits;
-        a.mt = p.n_fastest ? t / ntiles : t % mtiles;
-        a.nt = p.n_fastest ? t % ntiles : t / mtiles;
+        a.z = zz / splits;
+        a.split = zz % splits;
+        a.mirror = 0;
+        if (p.lower) {
+            const int u = t / sub;
+            int m = (int)((sqrtf(8.0f * (float)u + 1.0f) - 1.0f) * 0.5f);
+            while (m * (m + 1) / 2 > u) --m;
+            while ((m + 1) * (m + 2) / 2 <= u) ++m;
+            const int n = u - m * (m + 1) / 2;
+            a.mt = m;
+            a.nt = n * sub + t % sub;
+            a.mirror = n < m;
+        } else {
+            a.mt = p.n_fastest ? t / ntiles : t % mtiles;
+            a.nt = p.n_fastest ? t % ntiles : t / mtiles;
+        }
         a.c0 = min(a.split * per_split, kchunks);
         a.c1 = min(a.c0 + per_split, kchunks);
         return a;
@@ -203,28 +259,28 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
 
     if (warp == 8) {
         // ------------------------------------------------------------ loader (both CTAs)
-        if (lane == 0) {
+        if (elect_one()) {
             uint32_t slot = 0, phase = 1;
             bool ok = true;
             for (long long tile = pair; ok && tile < total; tile += npairs) {
                 const At at = locate(tile);
-                const int m0 = p.row0 + at.mt * kPgTile + (int)rank * 128, n0 = p.b_n0 + at.nt * kPgTile + (int)rank * 128;
+                const int m0 = p.row0 + at.mt * kPgTile + (int)rank * 128, n0 = p.b_n0 + at.nt * tn + (int)rank * (tn / 2);
                 for (int c = at.c0; ok && c < at.c1; ++c) {
                     const int ka = p.a_k0 + c * kPgChunk, kb = p.b_k0 + c * kPgChunk;
 #pragma unroll
                     for (int l = 0; l < kLoads; ++l) {
                         if (!mbar_wait(empty0 + slot * 8, phase, p.status, dead, kErrSlotWait)) { ok = false; break; }
                         const uint32_t dst = ring0 + slot * kPgSlotBytes, full = full0 + slot * 8;
-                        // the even CTA announces the bytes of both halves; either CTA's may land first
-                        if (rank == 0) mbar_expect_tx(full, 2 * kPgSlotBytes);
                         constexpr int tag[6] = {pg_load(SCHEME, 0), pg_load(SCHEME, 1), pg_load(SCHEME, 2), pg_load(SCHEME, 3),
                                                 pg_load(SCHEME, 4), pg_load(SCHEME, 5)};
                         const int plane = tag[l] & 3;
+                        // the even CTA announces the bytes of both halves; either CTA's may land first
+                        if (rank == 0) mbar_expect_tx(full, (tag[l] & 4) ? tn * (kPgChunk * 2) : 2 * kPgSlotBytes);
                         if (tag[l] & 4) {
                             const int z = at.z * p.b_zstep + plane;
                             if constexpr (BMN) {
                                 tma_load_3d_pair(dst, &tm_b, n0, kb, z, full);
-                                tma_load_3d_pair(dst + 8192, &tm_b, n0 + 64, kb, z, full);
+                                if (tn == 256) tma_load_3d_pair(dst + 8192, &tm_b, n0 + 64, kb, z, full);
                             } else {
                                 tma_load_3d_pair(dst, &tm_b, kb, n0, z, full);
                             }
@@ -244,9 +300,9 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
             let_copies_land(dead);
         }
     } else if (warp == 9) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0 && elect_one()) {
             // ------------------------------------------------------------ even CTA: MMA issuer for the pair
-            constexpr uint32_t idesc = make_idesc_bf16(256, 256, AMN, BMN);
+            const uint32_t idesc = make_idesc_bf16(256, tn, AMN, BMN);
             constexpr uint32_t astep = AMN ? 128 : 2, bstep = BMN ? 128 : 2;
             const uint64_t adesc = AMN ? make_smem_desc(0, 8192, 1024, kSwizzle128) : make_smem_desc(0, 16, 1024, kSwizzle128);
             const uint64_t bdesc = BMN ? make_smem_desc(0, 8192, 1024, kSwizzle128) : make_smem_desc(0, 16, 1024, kSwizzle128);
@@ -290,15 +346,17 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
     } else {
         // ------------------------------------------------------------ epilogue (both CTAs; own 128 rows)
         const uint32_t acce_leader = map_to_cta(acce0, 0);
-        const uint32_t lane_base = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(warp >> 2) * 128;
+        const uint32_t lane_base = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)((warp >> 2) * (tn / 2));
         uint32_t it = 0;
         bool ok = true;
         for (long long tile = pair; ok && tile < total; tile += npairs) {
             const At at = locate(tile);
             PgTile t;
-            t.z = at.z * p.splits + at.split;
+            t.z = at.z * splits + at.split;
+            t.mirror = at.mirror;
+            t.half = at.nt * 2 + (warp >> 2);
             t.row = p.row0 + at.mt * kPgTile + (int)rank * 128 + (warp & 3) * 32 + lane;
-            t.col = at.nt * kPgTile + (warp >> 2) * 128;
+            t.col = at.nt * tn + (warp >> 2) * (tn / 2);
             t.zero = at.c0 >= at.c1;
             Epi e;
             e.begin(args, t);
@@ -311,10 +369,11 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
                 }
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
+                    if (h * 64 >= tn) break;
                     float v[32];
                     if (!t.zero) {
                         tmem_ld32(lane_base + buf * 256 + h * 32, v);
-                        if (h == 3) {
+                        if ((h + 1) * 64 >= tn) {
                             tc_fence_before();
                             __syncwarp();
                             if (lane == 0) mbar_arrive_remote(acce_leader + buf * 8);
@@ -337,6 +396,7 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
                     tc_fence_after();
 #pragma unroll
                     for (int h = 0; h < 4; ++h) {
+                        if (h * 64 >= tn) break;
                         float v[32];
                         tmem_ld32(lane_base + buf * 256 + h * 32, v);
 #pragma unroll
@@ -348,7 +408,8 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
                 }
                 if (!ok) break;
 #pragma unroll
-                for (int h = 0; h < 4; ++h) e.chunk(args, t, h * 32, acc[h]);
+                for (int h = 0; h < 4; ++h)
+                    if (h * 64 < tn) e.chunk(args, t, h * 32, acc[h]);
             }
             e.end(args, t);
         }
@@ -363,12 +424,13 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
 }
 
 // A stack of `z` matrices [rows][cols] (bf16, rows `ld` elements apart, matrices `zstride` elements apart) as an operand.
-// K-major: boxes of 64 columns x 128 rows; MN-major: 64 columns x 64 rows, two side by side.
-inline int plane_map(CUtensorMap *m, const void *base, int mn_major, int64_t rows, int64_t cols, int64_t ld, int64_t zstride, int64_t z)
+// K-major: boxes of 64 columns x 128 rows (`box_rows`: tn / 2 for the second operand); MN-major: 64 columns x 64 rows, two side by
+// side or, tn = 128, one.
+inline int plane_map(CUtensorMap *m, const void *base, int mn_major, int64_t rows, int64_t cols, int64_t ld, int64_t zstride, int64_t z, int box_rows = 128)
 {
     const uint64_t dims[3] = {(uint64_t)cols, (uint64_t)rows, (uint64_t)z};
     const uint64_t strides[2] = {(uint64_t)ld * 2, (uint64_t)zstride * 2};
-    const uint32_t box[3] = {64, mn_major ? 64u : 128u, 1};
+    const uint32_t box[3] = {64, mn_major ? 64u : (uint32_t)box_rows, 1};
     return encode_tmap_nd(m, base, 2, 3, dims, strides, box, 128);
 }
 
@@ -393,7 +455,8 @@ int launch_plane_gemm(const CUtensorMap &tm_a, const CUtensorMap &tm_b, const Pl
         cache.set(pairs);
     }
     if (pairs < 1) return MONARCH_ERR_CUDA;
-    const long long total = (long long)((p.rows + kPgTile - 1) / kPgTile) * ((p.cols + kPgTile - 1) / kPgTile) * p.batches * p.splits;
+    const long long mt = (p.rows + kPgTile - 1) / kPgTile;
+    const long long total = (p.lower ? mt * (mt + 1) / 2 * (kPgTile / p.tn) : mt * ((p.cols + p.tn - 1) / p.tn)) * p.batches * p.splits;
     if (total <= 0) return MONARCH_OK;
     const int grid = 2 * (int)(total < pairs ? total : pairs);
     return launch_serialized(kern, dim3((unsigned)grid), kPgThreads, kPgSmem, s, tm_a, tm_b, p, args);

@@ -62,10 +62,29 @@ __device__ __forceinline__ void copy_row(const T *__restrict__ src, __nv_bfloat1
 {
     if constexpr (sizeof(T) == 2) {
         if (d == dp) {
+#pragma unroll 4
             for (int c = lane * 8; c < dp; c += 256) *reinterpret_cast<uint4 *>(dst + c) = __ldg(reinterpret_cast<const uint4 *>(src + c));
             return;
         }
     }
+    if constexpr (sizeof(T) == 4) {
+        if (d % 4 == 0) {                                   // dp - d is 0 or 4
+#pragma unroll 4
+            for (int c = lane * 4; c < dp; c += 128) {
+                float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (c < d) v = __ldg(reinterpret_cast<const float4 *>(src + c));
+                __nv_bfloat16 o[4][PL];
+                split<PL>(v.x, o[0]); split<PL>(v.y, o[1]); split<PL>(v.z, o[2]); split<PL>(v.w, o[3]);
+#pragma unroll
+                for (int i = 0; i < PL; ++i) {
+                    __nv_bfloat162 w[2] = {__nv_bfloat162(o[0][i], o[1][i]), __nv_bfloat162(o[2][i], o[3][i])};
+                    *reinterpret_cast<uint2 *>(dst + i * plane + c) = *reinterpret_cast<const uint2 *>(w);
+                }
+            }
+            return;
+        }
+    }
+#pragma unroll 4
     for (int c = lane * 2; c < dp; c += 64) {
         __nv_bfloat16 a[PL], b[PL];
         split<PL>(c < d ? elem<T>::load(src + c) : 0.0f, a);
@@ -158,7 +177,7 @@ __global__ void __launch_bounds__(256) split_rows_kernel(const T *__restrict__ W
 }
 
 // ------------------------------------------------------------------------------------------------ epilogues
-// Per row and 128 columns: r = log2(e) times the maximum, rounded, and s = sum 2^(z log2 e - r).  Exponents are formed by one FMA
+// Per row and half tile: r = log2(e) times the maximum, rounded, and s = sum 2^(z log2 e - r).  Exponents are formed by one FMA
 // from z and r, so the rounding of r cancels in r + log2 s.
 struct EpiStats {
     struct Args {
@@ -208,7 +227,7 @@ struct EpiStats {
     }
     __device__ __forceinline__ void end(const Args &a, const PgTile &t)
     {
-        if (live) a.part[(size_t)(t.row - a.row0) * a.halves + a.half0 + (t.col >> 7)] = make_float2(m, s);
+        if (live) a.part[(size_t)(t.row - a.row0) * a.halves + a.half0 + t.half] = make_float2(m, s);
     }
 };
 
@@ -346,6 +365,64 @@ template <typename T> struct EpiDx {
     __device__ __forceinline__ void end(const Args &, const PgTile &) {}
 };
 
+// dx where a few tiles are split along the vocabulary: a sum per part, over the pieces, in float32
+struct EpiDxPart {
+    struct Args {
+        float *acc;                // [parts][tokens][d]
+        const int *count;
+        size_t part;
+        int d, first;
+    };
+    float *to;
+    __device__ __forceinline__ void begin(const Args &a, const PgTile &t)
+    {
+        to = t.row < *a.count ? a.acc + t.z * a.part + (size_t)t.row * a.d + t.col : nullptr;
+    }
+    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32])
+    {
+        if (to == nullptr) return;
+        const int left = a.d - t.col - c;
+        float *out = to + c;
+        if ((a.d & 3) == 0) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+                if (i >= left) break;
+                float4 o = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                if (!a.first) {
+                    const float4 q = *reinterpret_cast<const float4 *>(out + i);
+                    o.x += q.x; o.y += q.y; o.z += q.z; o.w += q.w;
+                }
+                *reinterpret_cast<float4 *>(out + i) = o;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (i < left) out[i] = a.first ? v[i] : v[i] + out[i];
+        }
+    }
+    __device__ __forceinline__ void end(const Args &, const PgTile &) {}
+};
+
+// the parts of dx, added up, to the caller's rows
+template <typename T>
+__global__ void __launch_bounds__(256) xent_dx_kernel(const float *__restrict__ acc, size_t part, const int *__restrict__ splits,
+                                                      const int *__restrict__ map, const int *__restrict__ count, T *dx, int d)
+{
+    depend_wait();
+    depend_launch();
+    const int n = *count, parts = *splits;
+    for (int row = blockIdx.x * 8 + (threadIdx.x >> 5); row < n; row += gridDim.x * 8) {
+        T *out = dx + (size_t)map[row] * d;
+        const float *in = acc + (size_t)row * d;
+        for (int c = threadIdx.x & 31; c < d; c += 32) {
+            float v = 0.0f;
+#pragma unroll 4
+            for (int q = 0; q < parts; ++q) v += in[q * part + c];
+            elem<T>::store(out + c, v);
+        }
+    }
+}
+
 // ------------------------------------------------------------------------------------------------ joining the parts
 __global__ void __launch_bounds__(256) xent_join_kernel(const float2 *__restrict__ part, const float *__restrict__ tlogit,
                                                         const int *__restrict__ tgt, const int *__restrict__ map,
@@ -374,17 +451,225 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const float2 *__restrict
     }
 }
 
+// ------------------------------------------------------------------------------------------------ forward of few tokens
+// One launch that reads W once at the speed of memory.  A warp takes 16 rows of W straight from memory into the first operand of
+// warp MMAs (a lane's 16 bytes are eight consecutive k of one row: the order of k within a chunk of 32 is the same for both
+// operands, so it does not matter), the tokens (8 per column tile) wait in shared memory.  Every lane keeps maximum and sum of its
+// rows; lanes, warps and, in the last CTA to finish, CTAs are joined.  fp32: three planes of both, six products.
+constexpr int kFewThreads = 512, kFewMost = 32;
+constexpr size_t kFewSmem = 200 * 1024;
+constexpr int kFewTicket = 16;                  // word of the status area, zero between calls
+
+int few_row(int d) { return ((d * 2 + 127) / 128 * 128 + 64) / 2; }             // rows 64 bytes apart in their banks
+int few_tiles(int tokens) { return tokens <= 8 ? 1 : tokens <= 16 ? 2 : 4; }      // column tiles of 8 tokens: what the kernels are built for
+size_t few_smem(int tokens, int d, int planes) { return (size_t)few_tiles(tokens) * 8 * few_row(d) * 2 * planes; }
+bool few_fits(int64_t tokens, int d, int dtype)
+{
+    return tokens <= kFewMost && d % 8 == 0 && few_smem((int)tokens, d, dtype == MONARCH_F32 ? 3 : 1) <= kFewSmem;
+}
+
+struct FewArgs {
+    const void *x, *W;
+    const int64_t *targets;
+    float *loss, *lse, *tlogit;
+    float2 *part;                               // [tokens][CTAs]
+    unsigned *ticket;
+    int64_t ignore;
+    int tokens, d, vocab, row;
+};
+
+__device__ __forceinline__ void join(float &m, float &s, float m2, float s2)
+{
+    const float n = fmaxf(m, m2), base = n == __int_as_float(0xff800000) ? 0.0f : n;
+    s = s * ex2(m - base) + s2 * ex2(m2 - base);
+    m = n;
+}
+
+// eight consecutive values of a row of W, and the planes of their pairs as MMA operands
+template <typename T> struct FewRaw;
+template <> struct FewRaw<__nv_bfloat16> {
+    uint4 v;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p, bool in) { v = in ? __ldcs(reinterpret_cast<const uint4 *>(p)) : make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void planes(uint32_t (&o)[1][4]) const { o[0][0] = v.x; o[0][1] = v.y; o[0][2] = v.z; o[0][3] = v.w; }
+};
+template <> struct FewRaw<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float *p, bool in)
+    {
+        a = b = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (in) {
+            a = __ldcs(reinterpret_cast<const float4 *>(p));
+            b = __ldcs(reinterpret_cast<const float4 *>(p + 4));
+        }
+    }
+    __device__ __forceinline__ void planes(uint32_t (&o)[3][4]) const
+    {
+        const float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            __nv_bfloat16 x[3], y[3];
+            split<3>(f[2 * i], x);
+            split<3>(f[2 * i + 1], y);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) {
+                const __nv_bfloat162 w(x[q], y[q]);
+                o[q][i] = *reinterpret_cast<const uint32_t *>(&w);
+            }
+        }
+    }
+};
+
+template <typename T, int PL, int NT>
+__global__ void __launch_bounds__(kFewThreads, 1) xent_few_kernel(const FewArgs p)
+{
+    extern __shared__ __align__(16) __nv_bfloat16 xs[];                        // [PL][8 NT][row]
+    __shared__ float2 s_part[kFewThreads / 32][8 * NT];
+    __shared__ int s_tgt[8 * NT], s_last;
+    constexpr int kStep = sizeof(T) == 2 ? 4 : 2;                               // chunks of 32 requested ahead
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    const size_t xplane = (size_t)8 * NT * p.row;
+    depend_wait();
+    depend_launch();
+    for (int t = warp; t < 8 * NT; t += kFewThreads / 32) {
+        int64_t y = t < p.tokens ? p.targets[t] : p.ignore;
+        const bool keep = y != p.ignore;
+        if (lane == 0) s_tgt[t] = !keep ? -2 : y >= 0 && y < p.vocab ? (int)y : -1;
+        for (int k = lane * 2; k < p.row; k += 64) {
+            __nv_bfloat16 a[PL], b[PL];
+            const T *src = (const T *)p.x + (size_t)t * p.d + k;
+            split<PL>(keep && k < p.d ? elem<T>::load(src) : 0.0f, a);
+            split<PL>(keep && k + 1 < p.d ? elem<T>::load(src + 1) : 0.0f, b);
+#pragma unroll
+            for (int q = 0; q < PL; ++q) *reinterpret_cast<__nv_bfloat162 *>(xs + q * xplane + (size_t)t * p.row + k) = __nv_bfloat162(a[q], b[q]);
+        }
+    }
+    __syncthreads();
+    int tgt[NT][2];
+    float m[NT][2], s[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            tgt[n][e] = s_tgt[n * 8 + 2 * c + e];
+            m[n][e] = __int_as_float(0xff800000);
+            s[n][e] = 0.0f;
+        }
+    const int groups = (p.vocab + 15) / 16, chunks = (p.d + 31) / 32;
+    const __nv_bfloat16 *xl = xs + (size_t)g * p.row + c * 8;
+    for (int grp = blockIdx.x * (kFewThreads / 32) + warp; grp < groups; grp += gridDim.x * (kFewThreads / 32)) {
+        const int r0 = grp * 16 + g, r1 = r0 + 8;
+        const T *w0 = (const T *)p.W + (size_t)min(r0, p.vocab - 1) * p.d + c * 8, *w1 = (const T *)p.W + (size_t)min(r1, p.vocab - 1) * p.d + c * 8;
+        float z[NT][4] = {}, sum[NT][4] = {};
+        FewRaw<T> raw[kStep][2];
+#pragma unroll
+        for (int u = 0; u < kStep; ++u) {
+            raw[u][0].load(w0 + u * 32, u * 32 + c * 8 < p.d);
+            raw[u][1].load(w1 + u * 32, u * 32 + c * 8 < p.d);
+        }
+        for (int k = 0; k < chunks; k += kStep) {
+            FewRaw<T> next[kStep][2];
+#pragma unroll
+            for (int u = 0; u < kStep; ++u) {
+                const int at = (k + kStep + u) * 32;
+                next[u][0].load(w0 + at, at + c * 8 < p.d);
+                next[u][1].load(w1 + at, at + c * 8 < p.d);
+            }
+#pragma unroll
+            for (int u = 0; u < kStep; ++u) {
+                if (k + u >= chunks) break;
+                uint32_t a0[PL][4], a1[PL][4];
+                raw[u][0].planes(a0);
+                raw[u][1].planes(a1);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    uint4 b[PL];
+#pragma unroll
+                    for (int q = 0; q < PL; ++q) b[q] = *reinterpret_cast<const uint4 *>(xl + q * xplane + (size_t)n * 8 * p.row + (k + u) * 32);
+#pragma unroll
+                    for (int o = PL - 1; o >= 0; --o)
+#pragma unroll
+                        for (int q = o; q >= 0; --q) {
+                            const uint32_t f0[4] = {a0[q][0], a1[q][0], a0[q][1], a1[q][1]}, f1[4] = {a0[q][2], a1[q][2], a0[q][3], a1[q][3]};
+                            mma(z[n], f0, b[o - q].x, b[o - q].y);
+                            mma(z[n], f1, b[o - q].z, b[o - q].w);
+                        }
+                }
+            }
+            if ((k / kStep) % 8 == 7)                                             // runs of at most 96 steps (plane_gemm.cuh)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { sum[n][e] += z[n][e]; z[n][e] = 0.0f; }
+#pragma unroll
+            for (int u = 0; u < kStep; ++u) { raw[u][0] = next[u][0]; raw[u][1] = next[u][1]; }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float z0 = sum[n][e] + z[n][e], z1 = sum[n][e + 2] + z[n][e + 2];
+                if (r0 == tgt[n][e]) p.tlogit[n * 8 + 2 * c + e] = z0;
+                if (r1 == tgt[n][e]) p.tlogit[n * 8 + 2 * c + e] = z1;
+                const float v0 = r0 < p.vocab ? z0 : __int_as_float(0xff800000), v1 = r1 < p.vocab ? z1 : __int_as_float(0xff800000);
+                const float top = fmaxf(m[n][e], fmaxf(v0, v1) * kLog2e), base = top == __int_as_float(0xff800000) ? 0.0f : top;
+                s[n][e] = s[n][e] * ex2(m[n][e] - base) + ex2(fmaf(v0, kLog2e, -base)) + ex2(fmaf(v1, kLog2e, -base));
+                m[n][e] = top;
+            }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) join(m[n][e], s[n][e], __shfl_xor_sync(~0u, m[n][e], o), __shfl_xor_sync(~0u, s[n][e], o));
+            if (g == 0) s_part[warp][n * 8 + 2 * c + e] = make_float2(m[n][e], s[n][e]);
+        }
+    __syncthreads();
+    if (threadIdx.x < (unsigned)p.tokens) {
+        float2 v = s_part[0][threadIdx.x];
+        for (int w = 1; w < kFewThreads / 32; ++w) join(v.x, v.y, s_part[w][threadIdx.x].x, s_part[w][threadIdx.x].y);
+        p.part[(size_t)threadIdx.x * gridDim.x + blockIdx.x] = v;
+    }
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s_last = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
+        if (s_last) *p.ticket = 0;
+    }
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
+    for (int t = warp; t < p.tokens; t += kFewThreads / 32) {
+        float mm = __int_as_float(0xff800000), ss = 0.0f;
+        for (int i = lane; i < (int)gridDim.x; i += 32) {
+            const float2 v = __ldcg(p.part + (size_t)t * gridDim.x + i);
+            join(mm, ss, v.x, v.y);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) join(mm, ss, __shfl_xor_sync(~0u, mm, o), __shfl_xor_sync(~0u, ss, o));
+        if (lane == 0) {
+            const int y = s_tgt[t];
+            const float l = (mm + log2f(ss)) * kLn2;
+            p.lse[t] = y == -2 ? 0.0f : l;
+            p.loss[t] = y == -2 ? 0.0f : y >= 0 ? l - __ldcg(p.tlogit + t) : __int_as_float(0x7fffffff);
+        }
+    }
+}
+
 // ------------------------------------------------------------------------------------------------ host side
 size_t up(size_t v) { return (v + 255) & ~(size_t)255; }
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-constexpr int kPairs = 74;                      // CTA pairs of a B200, for choosing sizes; the launches ask the device
+constexpr size_t kHead = MONARCH_STATUS_BYTES + 65536;      // the status area and the counters of kernels that may share the workspace
+constexpr int kPairs = kPgPairs;
 
 struct Layout {
     bool direct;                                // W is read where it is (bf16 rows of 16-byte multiples)
     int planes, gplanes, dp, piece;             // planes of x and W, of g; padded row; vocabulary entries per piece
     int chunk, halves, trows;
-    size_t count, map, tgt, lse, dl, tlogit, x, w, part, g, dx, total;
+    int tn, tn_dw, tn_dx;                       // columns of a tile: logits, dW, dx
+    int dx_parts;                               // most parts of the vocabulary in dx; 1: no parts
+    size_t count, splits, map, tgt, lse, dl, tlogit, x, w, part, g, dx, total;
 };
 
 // Vocabulary entries per piece of the backward pass: whole 256-entry tiles, a plane of g within a quarter of a gigabyte, and
@@ -430,12 +715,23 @@ Layout layout(int64_t tokens, int d, int vocab, int dtype, bool bwd)
             if (most < vocab) l.piece = (int)(most < 256 ? 256 : most);
         }
     }
-    // half tiles of all pieces: full pieces are whole tiles
-    l.halves = 2 * ceil_div(vocab, 256);
-    size_t at = MONARCH_STATUS_BYTES;
+    const int64_t mt = ceil_div(tokens, 256);
+    l.tn = pg_tile(mt, l.piece, !bwd);
+    // half tiles of all pieces
+    l.halves = 2 * (vocab / l.piece * ceil_div(l.piece, l.tn) + ceil_div(vocab % l.piece, l.tn));
+    l.tn_dw = pg_tile(ceil_div(l.piece, 256), d, false);
+    l.tn_dx = pg_tile(mt, d, false);
+    // dx of few tiles is split along the vocabulary: as far as the parts stay within L2
+    const int64_t tiles = mt * ceil_div(d, l.tn_dx), part = tokens * d * 4;
+    int64_t parts = part > 0 ? ((int64_t)64 << 20) / part : 1;
+    if (parts > l.piece / 256) parts = l.piece / 256;
+    if (parts > kPgPairs) parts = kPgPairs;
+    l.dx_parts = tiles >= 4 * kPgPairs || parts < 1 ? 1 : (int)parts;
+    size_t at = kHead;
     auto take = [&](size_t bytes) { const size_t o = at; at += up(bytes); return o; };
     const size_t t = (size_t)tokens;
     l.count = take(4);
+    l.splits = take(4);
     l.map = take(t * 4);
     l.tgt = take(t * 4);
     l.lse = l.dl = l.tlogit = l.part = l.g = l.dx = 0;
@@ -445,7 +741,7 @@ Layout layout(int64_t tokens, int d, int vocab, int dtype, bool bwd)
     l.w = l.direct ? 0 : take((size_t)l.piece * l.dp * 2 * l.planes);
     if (bwd) {
         l.g = take((size_t)l.trows * l.piece * 2 * l.gplanes);
-        l.dx = take(t * d * 4);
+        l.dx = take(t * d * 4 * l.dx_parts);
     } else {
         l.part = take((size_t)l.chunk * l.halves * sizeof(float2));
     }
@@ -496,9 +792,41 @@ template <int SCHEME, class Epi> int logits(const CUtensorMap &ma, const CUtenso
 }  // namespace
 }  // namespace tc
 
+namespace tc {
+namespace {
+
+constexpr int kFewCtas = 148;
+
+template <typename T, int PL, int NT> int few_launch(const FewArgs &a, cudaStream_t s)
+{
+    return launch_serialized(xent_few_kernel<T, PL, NT>, dim3(kFewCtas), kFewThreads, (int)few_smem(a.tokens, a.d, PL), s, a);
+}
+template <typename T, int PL> int few_any(const FewArgs &a, cudaStream_t s)
+{
+    const int tiles = few_tiles(a.tokens);
+    return tiles == 1 ? few_launch<T, PL, 1>(a, s) : tiles == 2 ? few_launch<T, PL, 2>(a, s) : few_launch<T, PL, 4>(a, s);
+}
+
+int few(const void *x, const void *W, const int64_t *targets, float *loss, float *lse, int tokens, int d, int vocab, int64_t ignore, int dtype,
+        void *ws, cudaStream_t s)
+{
+    FewArgs a = {};
+    a.x = x; a.W = W; a.targets = targets; a.loss = loss; a.lse = lse;
+    a.tlogit = (float *)((char *)ws + kHead);
+    a.part = (float2 *)(a.tlogit + kFewMost);
+    a.ticket = (unsigned *)ws + kFewTicket;
+    a.ignore = ignore; a.tokens = tokens; a.d = d; a.vocab = vocab; a.row = few_row(d);
+    return dtype == MONARCH_F32 ? few_any<float, 3>(a, s) : few_any<__nv_bfloat16, 1>(a, s);
+}
+
+}  // namespace
+}  // namespace tc
+
 size_t xent_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab, int dtype, int bwd)
 {
-    return tc::layout(tokens, d, vocab, dtype, bwd != 0).total;
+    // a workspace sized for a batch serves every smaller one, on whichever kernels: also the few tokens' parts
+    const size_t few = tc::kHead + tc::kFewMost * (4 + 8 * tc::kFewCtas), need = tc::layout(tokens, d, vocab, dtype, bwd != 0).total;
+    return need > few ? need : few;
 }
 
 int xent_fwd(const void *x, const void *W, const int64_t *targets, float *loss, float *lse, int64_t tokens, int32_t d, int32_t vocab,
@@ -506,6 +834,7 @@ int xent_fwd(const void *x, const void *W, const int64_t *targets, float *loss, 
 {
     using namespace tc;
     if (tokens == 0) return MONARCH_OK;
+    if (few_fits(tokens, d, dtype)) return few(x, W, targets, loss, lse, (int)tokens, d, vocab, ignore_index, dtype, ws, s);
     const Layout l = layout(tokens, d, vocab, dtype, false);
     char *base = (char *)ws;
     unsigned *status = (unsigned *)ws;
@@ -523,20 +852,22 @@ int xent_fwd(const void *x, const void *W, const int64_t *targets, float *loss, 
     CUtensorMap ma, mb;
     MONARCH_TRY(plane_map(&ma, xp, 0, tokens, l.dp, l.dp, tokens * l.dp, l.planes));
     for (int64_t row0 = 0; row0 < tokens; row0 += l.chunk) {
+        int half0 = 0;
         const int rows = (int)(tokens - row0 < l.chunk ? tokens - row0 : l.chunk);
         for (int v0 = 0; v0 < vocab; v0 += l.piece) {
             const int cols = vocab - v0 < l.piece ? vocab - v0 : l.piece;
             PlaneGemm p = gemm(status);
-            p.count = count; p.row0 = (int)row0; p.rows = rows; p.cols = cols; p.kdim = d;
+            p.count = count; p.row0 = (int)row0; p.rows = rows; p.cols = cols; p.kdim = d; p.tn = l.tn;
             p.a_zstep = p.b_zstep = l.planes;
             if (l.direct) {
-                MONARCH_TRY(plane_map(&mb, W, 0, vocab, d, d, (int64_t)vocab * d, 1));
+                MONARCH_TRY(plane_map(&mb, W, 0, vocab, d, d, (int64_t)vocab * d, 1, l.tn / 2));
                 p.b_n0 = v0;
             } else {
                 MONARCH_TRY(split_w(W, base + l.w, v0, cols, l.piece, d, l.dp, dtype, s));
-                MONARCH_TRY(plane_map(&mb, base + l.w, 0, cols, l.dp, l.dp, (int64_t)l.piece * l.dp, l.planes));
+                MONARCH_TRY(plane_map(&mb, base + l.w, 0, cols, l.dp, l.dp, (int64_t)l.piece * l.dp, l.planes, l.tn / 2));
             }
-            const EpiStats::Args e = {part, tlogit, tgt, count, (int)row0, cols, v0, l.halves, v0 / 128};
+            const EpiStats::Args e = {part, tlogit, tgt, count, (int)row0, cols, v0, l.halves, half0};
+            half0 += 2 * ceil_div(cols, l.tn);
             if (dtype == MONARCH_F32) MONARCH_TRY((logits<kP3x3, EpiStats>(ma, mb, p, e, true, s)));
             else MONARCH_TRY((logits<kP1, EpiStats>(ma, mb, p, e, d > 8192, s)));
         }
@@ -558,6 +889,7 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
     const float *clse = (const float *)(base + l.lse), *cdl = (const float *)(base + l.dl);
     __nv_bfloat16 *xp = (__nv_bfloat16 *)(base + l.x), *g = (__nv_bfloat16 *)(base + l.g);
     float *acc = (float *)(base + l.dx);
+    int *splits = (int *)(base + l.splits);
     const size_t gplane = (size_t)l.trows * l.piece;
 
     CUtensorMap x_k, x_n, w_k, w_n, g_m, g_k;
@@ -566,26 +898,26 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
     MONARCH_TRY(plane_map(&g_k, g, 0, l.trows, l.piece, l.piece, (int64_t)gplane, l.gplanes));
     MONARCH_TRY(plane_map(&g_m, g, 1, l.trows, l.piece, l.piece, (int64_t)gplane, l.gplanes));
     if (l.direct) {
-        MONARCH_TRY(plane_map(&w_k, W, 0, vocab, d, d, (int64_t)vocab * d, 1));
+        MONARCH_TRY(plane_map(&w_k, W, 0, vocab, d, d, (int64_t)vocab * d, 1, l.tn / 2));
         MONARCH_TRY(plane_map(&w_n, W, 1, vocab, d, d, (int64_t)vocab * d, 1));
     }
     for (int v0 = 0; v0 < vocab; v0 += l.piece) {
         const int cols = vocab - v0 < l.piece ? vocab - v0 : l.piece;
         if (!l.direct) {
             MONARCH_TRY(split_w(W, base + l.w, v0, cols, l.piece, d, l.dp, dtype, s));
-            MONARCH_TRY(plane_map(&w_k, base + l.w, 0, cols, l.dp, l.dp, (int64_t)l.piece * l.dp, l.planes));
+            MONARCH_TRY(plane_map(&w_k, base + l.w, 0, cols, l.dp, l.dp, (int64_t)l.piece * l.dp, l.planes, l.tn / 2));
             MONARCH_TRY(plane_map(&w_n, base + l.w, 1, cols, l.dp, l.dp, (int64_t)l.piece * l.dp, l.planes));
         }
         // g
         PlaneGemm p = gemm(status);
-        p.count = count; p.rows = (int)tokens; p.cols = cols; p.kdim = d;
+        p.count = count; p.rows = (int)tokens; p.cols = cols; p.kdim = d; p.tn = l.tn;
         p.a_zstep = p.b_zstep = l.planes;
         p.b_n0 = l.direct ? v0 : 0;
         const typename EpiGrad<GP>::Args eg = {g, gplane, l.piece, cols, v0, tgt, count, clse, cdl};
         MONARCH_TRY((logits<LOGITS, EpiGrad<GP>>(x_k, w_k, p, eg, true, s)));
         // dW = g^T x
         p = gemm(status);
-        p.count = count; p.count_is_k = 1; p.rows = cols; p.cols = d; p.kdim = (int)tokens;
+        p.count = count; p.count_is_k = 1; p.rows = cols; p.cols = d; p.kdim = (int)tokens; p.tn = l.tn_dw;
         p.a_zstep = GP; p.b_zstep = l.planes;
         p.n_fastest = 1;
         p.seg = pg_seg(DW);
@@ -593,13 +925,26 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
         MONARCH_TRY((launch_plane_gemm<1, 1, DW, true, EpiStoreF32>(g_m, x_n, p, ew, s)));
         // dx += g W
         p = gemm(status);
-        p.count = count; p.rows = (int)tokens; p.cols = d; p.kdim = cols;
+        p.count = count; p.rows = (int)tokens; p.cols = d; p.kdim = cols; p.tn = l.tn_dx;
         p.a_zstep = GP; p.b_zstep = l.planes;
         p.b_k0 = l.direct ? v0 : 0;
         p.n_fastest = 1;
         p.seg = pg_seg(DX);
-        const typename EpiDx<T>::Args ex = {acc, dx, map, count, d, v0 == 0, v0 + cols == vocab};
-        MONARCH_TRY((launch_plane_gemm<0, 1, DX, DX != kP1, EpiDx<T>>(g_k, w_n, p, ex, s)));
+        if (l.dx_parts == 1) {
+            const typename EpiDx<T>::Args ex = {acc, dx, map, count, d, v0 == 0, v0 + cols == vocab};
+            MONARCH_TRY((launch_plane_gemm<0, 1, DX, DX != kP1, EpiDx<T>>(g_k, w_n, p, ex, s)));
+        } else {
+            // the last piece may be smaller: every piece has as many parts as the first found best
+            p.splits = l.dx_parts;
+            p.splits_out = v0 == 0 ? splits : nullptr;
+            p.splits_in = v0 == 0 ? nullptr : splits;
+            const EpiDxPart::Args ex = {acc, count, (size_t)tokens * d, d, v0 == 0};
+            MONARCH_TRY((launch_plane_gemm<0, 1, DX, DX != kP1, EpiDxPart>(g_k, w_n, p, ex, s)));
+        }
+    }
+    if (l.dx_parts > 1) {
+        const int ctas = ceil_div(tokens, 8) < 148 * 8 ? ceil_div(tokens, 8) : 148 * 8;
+        return launch_serialized(xent_dx_kernel<T>, dim3((unsigned)ctas), 256, 0, s, (const float *)acc, (size_t)tokens * d, (const int *)splits, map, count, dx, d);
     }
     return MONARCH_OK;
 }

@@ -139,6 +139,7 @@ SIZES = [
     # tokens, d, vocab, ignored
     (1, 8, 1, 0.0), (1, 16, 7, 0.0), (1, 1024, 1000, 0.0), (2, 64, 256, 0.5), (7, 72, 255, 0.0), (63, 128, 257, 0.3),
     (64, 8, 512, 0.0), (127, 256, 1000, 0.1), (128, 200, 128, 0.9), (129, 1, 300, 0.0), (255, 67, 1001, 0.2), (256, 64, 2048, 0.0),
+    (3, 512, 5000, 0.0), (8, 40, 16, 0.5), (9, 2048, 1500, 0.2), (16, 136, 999, 0.0), (17, 64, 2000, 0.3), (32, 1024, 3000, 0.1), (33, 1024, 3000, 0.0),
     (257, 136, 4099, 0.5), (300, 1032, 777, 0.0), (600, 250, 511, 0.1), (1000, 96, 20000, 0.2),
 ]
 
@@ -309,6 +310,43 @@ def test_same_bits_every_run_and_in_a_graph(dtype):
     torch.cuda.synchronize()
     for a, b in ((loss, gl), (lse, gs), (dx, gx), (dW, gw)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("T", [5, 20, 100])
+def test_one_workspace_for_calls_that_follow_one_another(T):
+    """A workspace large enough for all may serve every call of the library in turn: none leaves anything there that another minds."""
+    d, V, m, rows = 128, 700, 128, 300
+    big = max(P.monarch_xent_workspace_bytes(T, d, V, P.BF16), P.monarch_xent_bwd_workspace_bytes(T, d, V, P.BF16),
+              P.monarch_workspace_bytes(P.OP_FWD, rows, m * m, m, P.BF16), P.monarch_workspace_bytes(P.OP_BWD, rows, m * m, m, P.BF16),
+              P.monarch_ortho_workspace_bytes(1, 200, 200, P.BF16), P.monarch_workspace_bytes(P.OP_FWD, 500, 256, 16, P.F32))
+    ws = P.Workspace(big)
+    g = gen(3)
+    r = lambda *s, dt=torch.bfloat16: torch.randn(*s, generator=g, device="cuda").to(dt)  # noqa: E731
+    a, L, R = r(rows, m * m), r(m, m, m) / 12, r(m, m, m) / 12
+    f, Lf, Rf = r(500, 256, dt=torch.float32), r(16, 16, 16, dt=torch.float32), r(16, 16, 16, dt=torch.float32)
+    x, W, y, dloss = make(T, d, V, "bf16", 0.1, seed=1)
+    G = gradient(1, 200, 200, 9).bfloat16()
+
+    def everything():
+        out = [torch.empty_like(a), torch.empty_like(f), torch.empty(T, device="cuda"), torch.empty(T, device="cuda"), torch.empty_like(x),
+               torch.empty(V, d, device="cuda"), torch.empty_like(G), torch.empty_like(G[:, :128, :128].contiguous())]
+        P.monarch_fwd(a, L, R, out[0], rows, m * m, m, ws)
+        P.monarch_xent_fwd(x, W, y, out[2], out[3], T, d, V, IGNORE, ws)
+        P.monarch_fwd(f, Lf, Rf, out[1], 500, 256, 16, ws)
+        P.monarch_xent_bwd(x, W, y, out[3], dloss, out[4], out[5], 0, T, d, V, IGNORE, ws)
+        P.monarch_orthogonalize(G, out[6], 1, 200, 200, 5, ws)
+        P.monarch_orthogonalize(G[:, :128, :128].contiguous(), out[7], 1, 128, 128, 5, ws)
+        torch.cuda.synchronize()
+        assert P.monarch_last_device_status(ws) == 0
+        return out
+
+    first = everything()
+    for _ in range(2):
+        for p, q in zip(first, everything()):
+            assert torch.equal(p, q)
+    fresh = torch.empty_like(a)
+    P.monarch_fwd(a, L, R, fresh, rows, m * m, m, P.Workspace.for_op(P.OP_FWD, rows, m, P.BF16))
+    assert torch.equal(fresh, first[0])
 
 
 def test_pieces_of_the_vocabulary_and_token_chunks():
