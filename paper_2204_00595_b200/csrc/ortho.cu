@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(kSmallThreads) ortho_small_kernel(const Io<T> 
     }
 }
 
-// ------------------------------------------------------------------------------------------------ blocks up to 64 x 128
+// ------------------------------------------------------------------------------------------------ blocks up to 64 x 256
 // One CTA per block, everything on chip: X, S and P = b S + c S^2 are bf16 planes in shared memory (PL = 2 for bf16 results, 3 for
 // fp32), their fp32 values stay in the registers of the thread that holds them as an accumulator, warp-level MMAs (m16n8k16).
 // S is symmetric, so S and P serve as either operand as stored; only P X needs X transposed (ldmatrix.trans).  tcgen05 is little gain
@@ -255,7 +255,8 @@ template <int KP, int NP, int PL> struct BlockCfg {
     static constexpr int kRows = KP / 16, kThreads = kRows * 2 * 32;
     static constexpr int kLdX = NP + 8, kLdS = KP + 8;                       // rows 16 bytes apart in their banks
     static constexpr int kXPlane = KP * kLdX, kSPlane = KP * kLdS;           // elements
-    static constexpr int kSmem = (2 * PL * kXPlane + 2 * PL * kSPlane) * 2;
+    static constexpr int kXBufs = NP > 128 ? 1 : 2;                          // the next X beside the one it is made of, or over it
+    static constexpr int kSmem = (kXBufs * PL * kXPlane + 2 * PL * kSPlane) * 2;
     static constexpr int kS = KP / 16, kX = NP / 16;                         // 8-column tiles of a warp in S and in X
 };
 
@@ -317,7 +318,7 @@ __global__ void __launch_bounds__(BlockCfg<KP, NP, PL>::kThreads) ortho_block_ke
     using C = BlockCfg<KP, NP, PL>;
     extern __shared__ __align__(16) __nv_bfloat16 smb[];
     __shared__ double s_norm[C::kThreads / 32];
-    __nv_bfloat16 *Xs = smb, *Ss = smb + 2 * PL * C::kXPlane, *Ps = Ss + PL * C::kSPlane;
+    __nv_bfloat16 *Xs = smb, *Ss = smb + C::kXBufs * PL * C::kXPlane, *Ps = Ss + PL * C::kSPlane;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int row0 = (warp >> 1) * 16, half = warp & 1;
     const int r = lane >> 2, c2 = (lane & 3) * 2;
@@ -367,7 +368,7 @@ __global__ void __launch_bounds__(BlockCfg<KP, NP, PL>::kThreads) ortho_block_ke
     const uint32_t p_a = smem_u32(Ps) + row0 * C::kLdS * 2;
     for (int it = 0; it < steps; ++it) {
         __syncthreads();
-        const uint32_t X = smem_u32(Xs) + (it & 1) * (PL * C::kXPlane * 2);
+        const uint32_t X = smem_u32(Xs) + (C::kXBufs > 1 ? it & 1 : 0) * (PL * C::kXPlane * 2);
         float s[C::kS][4] = {}, p[C::kS][4] = {};
         plane_mma<PL, NP / 16, C::kS, false>(s, X + row0 * C::kLdX * 2, C::kXPlane * 2, C::kLdX, X + half * (KP / 2) * C::kLdX * 2, C::kXPlane * 2, C::kLdX);
         put_tiles<PL>(s, Ss + s_at, C::kSPlane, C::kLdS);
@@ -385,7 +386,10 @@ __global__ void __launch_bounds__(BlockCfg<KP, NP, PL>::kThreads) ortho_block_ke
         for (int t = 0; t < C::kX; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[t][e] = fmaf(kA, x[t][e], y[t][e]);
-        if (it + 1 < steps) put_tiles<PL>(x, Xs + ((it + 1) & 1) * PL * C::kXPlane + x_at, C::kXPlane, C::kLdX);
+        if (it + 1 < steps) {
+            if (C::kXBufs == 1) __syncthreads();
+            put_tiles<PL>(x, Xs + (C::kXBufs > 1 ? (it + 1) & 1 : 0) * PL * C::kXPlane + x_at, C::kXPlane, C::kLdX);
+        }
     }
     float w[C::kX][4];
 #pragma unroll
@@ -410,7 +414,7 @@ template <typename T, int KP, int NP, int PL> int launch_block(const Io<T> &io, 
     return launch_serialized(ortho_block_kernel<T, KP, NP, PL>, dim3((unsigned)blocks), C::kThreads, C::kSmem, s, io, rows, cols, steps);
 }
 
-bool fits_block(int k, int n) { return k <= 64 && n <= 128; }
+bool fits_block(int k, int n) { return k <= 64 && n <= 256; }
 
 template <typename T, int PL> int ortho_block(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, cudaStream_t s)
 {
@@ -419,15 +423,18 @@ template <typename T, int PL> int ortho_block(const Io<T> &io, int64_t blocks, i
         if (n <= 16) return launch_block<T, 16, 16, PL>(io, blocks, rows, cols, steps, s);
         if (n <= 32) return launch_block<T, 16, 32, PL>(io, blocks, rows, cols, steps, s);
         if (n <= 64) return launch_block<T, 16, 64, PL>(io, blocks, rows, cols, steps, s);
-        return launch_block<T, 16, 128, PL>(io, blocks, rows, cols, steps, s);
+        if (n <= 128) return launch_block<T, 16, 128, PL>(io, blocks, rows, cols, steps, s);
+        return launch_block<T, 16, 256, PL>(io, blocks, rows, cols, steps, s);
     }
     if (k <= 32) {
         if (n <= 32) return launch_block<T, 32, 32, PL>(io, blocks, rows, cols, steps, s);
         if (n <= 64) return launch_block<T, 32, 64, PL>(io, blocks, rows, cols, steps, s);
-        return launch_block<T, 32, 128, PL>(io, blocks, rows, cols, steps, s);
+        if (n <= 128) return launch_block<T, 32, 128, PL>(io, blocks, rows, cols, steps, s);
+        return launch_block<T, 32, 256, PL>(io, blocks, rows, cols, steps, s);
     }
     if (n <= 64) return launch_block<T, 64, 64, PL>(io, blocks, rows, cols, steps, s);
-    return launch_block<T, 64, 128, PL>(io, blocks, rows, cols, steps, s);
+    if (n <= 128) return launch_block<T, 64, 128, PL>(io, blocks, rows, cols, steps, s);
+    return launch_block<T, 64, 256, PL>(io, blocks, rows, cols, steps, s);
 }
 
 // ------------------------------------------------------------------------------------------------ blocks up to 128 x 128
@@ -746,95 +753,126 @@ __global__ void __launch_bounds__(kTcThreads, 1) ortho_tc_kernel(const Io<T> io,
 }
 
 // ------------------------------------------------------------------------------------------------ larger blocks
-constexpr int kNormParts = 64;
+// Three products a step on plane_gemm.cuh (CTA pairs, tcgen05), with the square completed so that each needs its operands alone:
+//   S~ = X X^T + beta I,   P = c S~ S~^T + (a - c beta^2) I = a I + b S + c S^2,   X <- P X,      beta = b / 2c
+// (X^T X and X P where rows > cols).  An error of P counts against its eigenvalues, 0.64 to 3.44; that b S comes out of a difference
+// costs nothing there.  S~, P and X exist only as planes; an epilogue turns its accumulator into the next operand's planes, the last
+// one into the caller's result.  S~ and P are symmetric: only the blocks of 256 columns up to the diagonal are computed, each tile
+// below it is written transposed as well.  Products of fewer tiles than there are CTA pairs are split along K, in which case a launch
+// adds the parts and does the same.
+constexpr float kBeta = kB / (2.0f * kC), kGamma = kA - kC * kBeta * kBeta;
+constexpr int kNormParts = 256;
 
-// sums of squares of kNormParts parts of each block (and the new momentum)
-template <typename T>
-__global__ void __launch_bounds__(256) norm_kernel(const Io<T> io, double *part, int64_t size)
-{
-    __shared__ double s_part[8];
-    depend_wait();
-    depend_launch();
-    const int64_t per = (size + kNormParts - 1) / kNormParts, first = blockIdx.x * per, last = min(size, first + per);
-    const size_t base = (size_t)blockIdx.y * size;
-    double q = 0.0;
-    for (int64_t i = first + threadIdx.x; i < last; i += 256) {
-        const float u = io.u(base + i, io.fetch(base + i), true);
-        q += (double)u * u;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) q += __shfl_xor_sync(~0u, q, o);
-    if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = q;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        q = 0.0;
-        for (int w = 0; w < 8; ++w) q += s_part[w];
-        part[(size_t)blockIdx.y * kNormParts + blockIdx.x] = q;
-    }
-}
-
-// one value into PL planes
 template <int PL> __device__ __forceinline__ void put_planes(__nv_bfloat16 *to, size_t plane, float v)
 {
 #pragma unroll
-    for (int i = 0; i < PL; ++i) {
+    for (int q = 0; q < PL; ++q) {
         const __nv_bfloat16 h = __float2bfloat16_rn(v);
-        to[i * plane] = h;
+        to[q * plane] = h;
         v -= __bfloat162float(h);
     }
 }
-
-struct Finish {
-    const float *part;            // [blocks][splits][rows][cols]
-    int splits;
-    int rows, cols, ld;           // ld: row of a plane
-    float *f32;                   // S or X, [blocks][rows][cols]
-    __nv_bfloat16 *planes;        // [blocks][PL][rows][ld]
-};
-
-// MODE 0: X = U / |U|;  1: S = sum of the parts;  2: P = b S + c sum;  3: X = a X + sum;  4: the last X, to the caller
-template <typename T, int PL, int MODE>
-__global__ void __launch_bounds__(256) finish_kernel(const Finish f, const Io<T> io, const double *norm)
+// four consecutive values, the first at a multiple of four
+template <int PL> __device__ __forceinline__ void put_planes4(__nv_bfloat16 *to, size_t plane, const float (&from)[4])
 {
-    depend_wait();
-    depend_launch();
-    const int64_t size = (int64_t)f.rows * f.cols;
-    const size_t base = (size_t)blockIdx.y * size;
-    const size_t plane = (size_t)f.rows * f.ld;
-    double inv = 0.0;
-    if (MODE == 0) {
-        double q = 0.0;
-        for (int i = 0; i < kNormParts; ++i) q += norm[(size_t)blockIdx.y * kNormParts + i];
-        inv = 1.0 / (sqrt(q) + (double)kEps);
-    }
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
-        float v;
-        if (MODE == 0) {
-            v = (float)((double)io.u(base + i, io.fetch(base + i), false) * inv);
-        } else {
-            const float *p = f.part + ((size_t)blockIdx.y * f.splits) * size + i;
-            v = 0.0f;
-            for (int s = 0; s < f.splits; ++s) v += p[(size_t)s * size];
-            if (MODE == 2) v = fmaf(kB, f.f32[base + i], kC * v);
-            if (MODE == 3 || MODE == 4) v = fmaf(kA, f.f32[base + i], v);
-        }
-        if (MODE == 4) {
-            io.write(base + i, v, io.old(base + i));
-            continue;
-        }
-        if (MODE != 2) f.f32[base + i] = v;
-        const int64_t r = i / f.cols, c = i - r * f.cols;
-        put_planes<PL>(f.planes + (size_t)blockIdx.y * PL * plane + (size_t)r * f.ld + c, plane, v);
+    float u[4] = {from[0], from[1], from[2], from[3]};
+#pragma unroll
+    for (int q = 0; q < PL; ++q) {
+        const uint32_t w0 = pack_bf16(u[0], u[1]), w1 = pack_bf16(u[2], u[3]);
+        *reinterpret_cast<uint2 *>(to + q * plane) = make_uint2(w0, w1);
+        u[0] -= __uint_as_float(w0 << 16); u[1] -= __uint_as_float(w0 & 0xffff0000u);
+        u[2] -= __uint_as_float(w1 << 16); u[3] -= __uint_as_float(w1 & 0xffff0000u);
     }
 }
 
-struct EpiPart {
+// A stack of matrices as planes: [blocks][PL][rows][ld], ld a multiple of 16 (what stands behind the columns is never read)
+struct Planes {
+    __nv_bfloat16 *at;
+    int rows, cols, ld;
+    __device__ __forceinline__ size_t plane() const { return (size_t)rows * ld; }
+    template <int PL> __device__ __forceinline__ __nv_bfloat16 *element(int64_t block, int r, int c) const
+    {
+        return at + (block * PL * rows + r) * ld + c;
+    }
+};
+
+enum Role { kRoleS = 0, kRoleP = 1, kRoleX = 2, kRoleOut = 3 };
+
+// what becomes of a sum at (row, col)
+template <int ROLE> __device__ __forceinline__ float finished(float v, int row, int col)
+{
+    if (ROLE == kRoleS) return row == col ? v + kBeta : v;
+    if (ROLE == kRoleP) return row == col ? fmaf(kC, v, kGamma) : kC * v;
+    return v;
+}
+
+template <typename T, int PL, int ROLE> struct EpiPlanes {
+    static constexpr int kStage = ROLE == kRoleOut ? 0 : 2;
     struct Args {
-        float *out;
+        Planes to;                 // also the sizes of the result
+        Io<T> io;                  // kRoleOut
+    };
+    __device__ __forceinline__ void begin(const Args &, const PgTile &) {}
+    template <class Stage> __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], Stage &st)
+    {
+        const Planes &m = a.to;
+        const int col = t.col + c, row0 = t.row & ~31;
+        if constexpr (ROLE == kRoleOut) {
+            if (t.row >= m.rows) return;
+            const size_t at = ((size_t)t.z * m.rows + t.row) * m.cols + col;
+            if (m.cols % 4 == 0) {
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) {
+                    float w[2][4];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        if (col + i + 4 * j < m.cols) a.io.old4(at + i + 4 * j, w[j]);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        if (col + i + 4 * j < m.cols) {
+                            float o[4] = {v[i + 4 * j], v[i + 4 * j + 1], v[i + 4 * j + 2], v[i + 4 * j + 3]};
+                            a.io.write4(at + i + 4 * j, o, w[j]);
+                        }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (col + i < m.cols) a.io.write(at + i, v[i], a.io.old(at + i));
+            }
+        } else {
+            if (row0 >= m.rows || col >= m.cols) return;                       // the same in all lanes; TMA clips the rest
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = finished<ROLE>(v[i], t.row, col + i);
+#pragma unroll
+            for (int q = 0; q < PL; ++q) {
+                uint32_t w[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+                    v[2 * i] -= __uint_as_float(w[i] << 16);
+                    v[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
+                }
+                st.row(st.begin(), w);
+                st.send(col, row0, t.z * PL + q);
+                if ((ROLE == kRoleS || ROLE == kRoleP) && t.mirror) {
+                    st.column(st.begin(), w);
+                    st.send(row0, col, t.z * PL + q);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void end(const Args &, const PgTile &) {}
+};
+
+// a part of K, float32
+struct EpiPart {
+    static constexpr int kStage = 0;
+    struct Args {
+        float *out;                // [blocks][splits][rows][cols]
         int rows, cols;
     };
     __device__ __forceinline__ void begin(const Args &, const PgTile &) {}
-    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32])
+    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<1> &)
     {
         if (t.row >= a.rows) return;
         const int left = a.cols - t.col - c;
@@ -852,44 +890,233 @@ struct EpiPart {
     __device__ __forceinline__ void end(const Args &, const PgTile &) {}
 };
 
-struct Large {
-    int k, n, ldx, ldk, planes, split_s, split_p, split_x;
-    size_t norm, x, xp, s, sp, pp, part, total;
+// The parts added up, and what the epilogues do.  Tiles of 32 x 32, for S~ and P those up to the diagonal, the ones off it written
+// transposed as well.
+template <typename T, int PL, int ROLE>
+__global__ void __launch_bounds__(256) finish_kernel(const float *__restrict__ part, int splits, const typename EpiPlanes<T, PL, ROLE>::Args a)
+{
+    __shared__ float tile[32][33];
+    constexpr bool kSym = ROLE == kRoleS || ROLE == kRoleP;
+    depend_wait();
+    depend_launch();
+    const Planes &m = a.to;
+    const int tr = (m.rows + 31) / 32, tc = (m.cols + 31) / 32, per = kSym ? tr * (tr + 1) / 2 : tr * tc;
+    const int block = blockIdx.x / per, t = blockIdx.x % per;
+    int I, J;
+    if (kSym) {
+        I = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
+        while (I * (I + 1) / 2 > t) --I;
+        while ((I + 1) * (I + 2) / 2 <= t) ++I;
+        J = t - I * (I + 1) / 2;
+    } else {
+        I = t / tc;
+        J = t % tc;
+    }
+    const size_t size = (size_t)m.rows * m.cols;
+    const float *from = part + (size_t)block * splits * size;
+    const int lr = threadIdx.x >> 3, lc = (threadIdx.x & 7) * 4, r = I * 32 + lr, c = J * 32 + lc;
+    float v[4] = {};
+    if (r < m.rows && c < m.cols) {
+        const size_t at = (size_t)r * m.cols + c;
+        if (m.cols % 4 == 0) {
+#pragma unroll 8
+            for (int s = 0; s < splits; ++s) {
+                const float4 q = *reinterpret_cast<const float4 *>(from + s * size + at);
+                v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w;
+            }
+        } else {
+            for (int s = 0; s < splits; ++s)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (c + e < m.cols) v[e] += from[s * size + at + e];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = finished<ROLE>(v[e], r, c + e);
+            if (c + e >= m.cols) break;
+            if (ROLE == kRoleOut) {
+                const size_t i = (size_t)block * size + at + e;
+                a.io.write(i, v[e], a.io.old(i));
+            }
+        }
+        // four columns or what is left of the row's multiple of sixteen: the columns behind the last are never read
+        if (ROLE != kRoleOut) put_planes4<PL>(m.template element<PL>(block, r, c), m.plane(), v);
+    }
+    if (!kSym || I == J) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) tile[lr][lc + e] = v[e];
+    __syncthreads();
+    const int rr = J * 32 + lr, cc = I * 32 + lc;                            // of the transposed tile
+    if (rr < m.rows && cc < m.cols) {
+        const float w[4] = {tile[lc][lr], tile[lc + 1][lr], tile[lc + 2][lr], tile[lc + 3][lr]};
+        put_planes4<PL>(m.template element<PL>(block, rr, cc), m.plane(), w);
+    }
+}
+
+// sums of squares of `parts` parts of each block, and the new momentum
+template <typename T>
+__global__ void __launch_bounds__(256) norm_kernel(const Io<T> io, double *part, int parts, int64_t size)
+{
+    __shared__ double s_part[8];
+    depend_wait();
+    depend_launch();
+    const int block = blockIdx.x / parts, p = blockIdx.x % parts;
+    const int64_t per = ((size + parts - 1) / parts + 3) / 4 * 4, first = p * per, last = min(size, first + per);
+    const size_t base = (size_t)block * size;
+    double q = 0.0;
+    if (size % 4 == 0) {
+        for (int64_t i = first + threadIdx.x * 4; i < last; i += 4096) {
+            typename Io<T>::In4 f[4];
+#pragma unroll
+            for (int a = 0; a < 4; ++a)
+                if (i + a * 1024 < last) f[a] = io.fetch4(base + i + a * 1024);
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                if (i + a * 1024 >= last) break;
+                float u[4];
+                io.u4(base + i + a * 1024, f[a], u);
+                // four squares in fp64 as well: their fp32 range ends at 1.8e19
+#pragma unroll
+                for (int e = 0; e < 4; ++e) q += (double)u[e] * u[e];
+            }
+        }
+    } else {
+        for (int64_t i = first + threadIdx.x; i < last; i += 256) {
+            const float u = io.u(base + i, io.fetch(base + i), true);
+            q += (double)u * u;
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) q += __shfl_xor_sync(~0u, q, o);
+    if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = q;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        q = 0.0;
+        for (int w = 0; w < 8; ++w) q += s_part[w];
+        part[(size_t)block * parts + p] = q;
+    }
+}
+
+// X0 = U / (|U| + 1e-7) as planes: `ctas` CTAs per block
+template <typename T, int PL>
+__global__ void __launch_bounds__(256) start_kernel(const Planes x, const Io<T> io, const double *norm, int parts, int ctas)
+{
+    __shared__ double s_part[8];
+    depend_wait();
+    depend_launch();
+    const int block = blockIdx.x / ctas, p = blockIdx.x % ctas;
+    double q = threadIdx.x < parts ? norm[(size_t)block * parts + threadIdx.x] : 0.0;                // kNormParts <= 256
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) q += __shfl_xor_sync(~0u, q, o);
+    if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = q;
+    __syncthreads();
+    q = 0.0;
+    for (int w = 0; w < 8; ++w) q += s_part[w];
+    const double inv = 1.0 / (sqrt(q) + (double)kEps);
+    const int64_t size = (int64_t)x.rows * x.cols;
+    const size_t base = (size_t)block * size;
+    if (x.cols % 4 == 0) {
+        const int per_row = x.cols / 4;
+        for (int64_t i = (int64_t)p * 256 + threadIdx.x; i < size / 4; i += (int64_t)ctas * 256) {
+            const int r = (int)(i / per_row), c = (int)(i - (int64_t)r * per_row) * 4;
+            typename Io<T>::In4 f = io.fetch4(base + i * 4);
+            __nv_bfloat16 *to = x.template element<PL>(block, r, c);
+            float u[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[e] = (float)((double)io.u(0, {f.g[e], f.v[e]}, false) * inv);
+            put_planes4<PL>(to, x.plane(), u);
+        }
+    } else {
+        for (int64_t i = (int64_t)p * 256 + threadIdx.x; i < size; i += (int64_t)ctas * 256) {
+            const int r = (int)(i / x.cols), c = (int)(i - (int64_t)r * x.cols);
+            put_planes<PL>(x.template element<PL>(block, r, c), x.plane(), (float)((double)io.u(base + i, io.fetch(base + i), false) * inv));
+        }
+    }
+}
+
+// How a product is cut: columns of a tile, parts of K
+struct Cut {
+    int tn, splits;
 };
 
-int split_for(int64_t blocks, int m, int n, int kdim)
+// by the time it takes, in cycles: rounds of the CTA pairs over tiles of `products` MMAs of 512 cycles per K chunk (narrow tiles load
+// more per MMA), 3000 for a tile's start and end, 8000 for the launch that adds parts up
+Cut cut(int64_t blocks, int m, int n, int kdim, int products, bool lower)
 {
-    const int64_t tiles = blocks * ceil_div(m, kPgTile) * ceil_div(n, kPgTile), chunks = ceil_div(kdim, kPgChunk);
-    int64_t s = tiles > 0 ? 74 / tiles : 1;
-    if (s > chunks / 4) s = chunks / 4;
-    return s < 1 ? 1 : (int)s;
+    Cut best = {256, 1};
+    double best_cost = 1e300;
+    const int64_t mt = ceil_div(m, 256), chunks = ceil_div(kdim, kPgChunk);
+    for (int tn = 256; tn >= 128; tn /= 2) {
+        const int64_t tiles = blocks * (lower ? mt * (mt + 1) / 2 * (256 / tn) : mt * ceil_div(n, tn));
+        for (int s = 1; s <= 16 && s * 2 <= chunks + 1; ++s) {
+            if (s > 1 && tiles * (s - 1) >= 2 * kPgPairs) break;
+            const int64_t rounds = (tiles * s + kPgPairs - 1) / kPgPairs;
+            const double chunk = 512.0 * products * tn / 256 * (tn == 128 ? 1.2 : 1.0);
+            const double cost = rounds * ((double)((chunks + s - 1) / s) * chunk + 3000.0) + (s > 1 ? 8000.0 : 0.0);
+            if (cost < best_cost) {
+                best_cost = cost;
+                best = {tn, s};
+            }
+        }
+    }
+    return best;
 }
+
+struct Large {
+    int k, n, ldx, ldk, planes, parts;
+    Cut s, p, x;
+    size_t norm, xp[2], sp, pp, part, total;
+};
 
 Large large_layout(int64_t blocks, int rows, int cols, int dtype)
 {
     Large l;
     l.k = rows < cols ? rows : cols;
     l.n = rows < cols ? cols : rows;
-    l.ldx = (cols + 7) / 8 * 8;
-    l.ldk = (l.k + 7) / 8 * 8;
+    l.ldx = (cols + 15) / 16 * 16;
+    l.ldk = (l.k + 15) / 16 * 16;
     l.planes = dtype == MONARCH_F32 ? 3 : 2;
-    l.split_s = split_for(blocks, l.k, l.k, l.n);
-    l.split_p = split_for(blocks, l.k, l.k, l.k);
-    l.split_x = split_for(blocks, rows, cols, l.k);
+    const int products = dtype == MONARCH_F32 ? 6 : 3;
+    l.s = cut(blocks, l.k, l.k, l.n, products, true);
+    l.p = cut(blocks, l.k, l.k, l.k, products, true);
+    l.x = cut(blocks, rows, cols, l.k, products, false);
     const size_t kk = (size_t)l.k * l.k, rc = (size_t)rows * cols, b = (size_t)blocks;
+    const int64_t want = (int64_t)((rc + 8191) / 8192);
+    l.parts = (int)(want < kNormParts ? want : kNormParts);
     size_t at = MONARCH_STATUS_BYTES + 65536;          // the status area and the counters of kernels that may share the workspace
     auto take = [&](size_t bytes) { const size_t o = at; at += up(bytes); return o; };
-    l.norm = take(b * kNormParts * 8);
-    l.x = take(b * rc * 4);
-    l.xp = take(b * l.planes * rows * l.ldx * 2);
-    l.s = take(b * kk * 4);
+    l.norm = take(b * l.parts * 8);
+    // two X: the last product of a step reads the one and writes the other
+    l.xp[0] = take(b * l.planes * rows * l.ldx * 2);
+    l.xp[1] = take(b * l.planes * rows * l.ldx * 2);
     l.sp = take(b * l.planes * l.k * l.ldk * 2);
     l.pp = take(b * l.planes * l.k * l.ldk * 2);
-    size_t part = kk * (l.split_s > l.split_p ? l.split_s : l.split_p);
-    if (rc * l.split_x > part) part = rc * l.split_x;
+    size_t part = 0;
+    if (l.s.splits > 1) part = kk * l.s.splits;
+    if (l.p.splits > 1 && kk * l.p.splits > part) part = kk * l.p.splits;
+    if (l.x.splits > 1 && rc * l.x.splits > part) part = rc * l.x.splits;
     l.part = take(b * part * 4);
     l.total = at;
     return l;
+}
+
+template <typename T, int PL, int SCHEME, int AMN, int BMN, int ROLE>
+int ortho_product(const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mc, PlaneGemm p, const Cut &c, int kdim, const typename EpiPlanes<T, PL, ROLE>::Args &a,
+                  float *part, cudaStream_t s)
+{
+    const Planes &m = a.to;
+    constexpr bool kSym = ROLE == kRoleS || ROLE == kRoleP;
+    p.rows = m.rows;
+    p.cols = m.cols;
+    p.kdim = kdim;
+    p.tn = c.tn;
+    p.splits = c.splits;
+    p.lower = kSym;
+    if (c.splits == 1) return launch_plane_gemm<AMN, BMN, SCHEME, true, EpiPlanes<T, PL, ROLE>>(ma, mb, mc, p, a, s);
+    const EpiPart::Args e = {part, m.rows, m.cols};
+    MONARCH_TRY((launch_plane_gemm<AMN, BMN, SCHEME, true, EpiPart>(ma, mb, mb, p, e, s)));
+    const int64_t tr = ceil_div(m.rows, 32), tc = ceil_div(m.cols, 32), tiles = kSym ? tr * (tr + 1) / 2 : tr * tc;
+    return launch_serialized(finish_kernel<T, PL, ROLE>, dim3((unsigned)(tiles * p.batches)), 256, 0, s, (const float *)part, c.splits, a);
 }
 
 template <typename T, int PL, int SCHEME>
@@ -899,51 +1126,49 @@ int ortho_large(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, 
     char *base = (char *)ws;
     const bool wide = rows <= cols;
     double *norm = (double *)(base + l.norm);
-    float *X = (float *)(base + l.x), *S = (float *)(base + l.s), *part = (float *)(base + l.part);
-    __nv_bfloat16 *xp = (__nv_bfloat16 *)(base + l.xp), *sp = (__nv_bfloat16 *)(base + l.sp), *pp = (__nv_bfloat16 *)(base + l.pp);
-    const int64_t size = (int64_t)rows * cols;
-    if (blocks > 65535) return MONARCH_ERR_UNSUPPORTED;
+    float *part = (float *)(base + l.part);
+    const Planes sp = {(__nv_bfloat16 *)(base + l.sp), l.k, l.k, l.ldk}, pp = {(__nv_bfloat16 *)(base + l.pp), l.k, l.k, l.ldk};
+    Planes x[2];
+    CUtensorMap x_k[2], x_n[2], x_b[2], x_to[2], s_a, s_b, s_to, p_a, p_b, p_to;
+    for (int i = 0; i < 2; ++i) {
+        x[i] = {(__nv_bfloat16 *)(base + l.xp[i]), rows, cols, l.ldx};
+        MONARCH_TRY(plane_map(&x_k[i], x[i].at, 0, rows, cols, l.ldx, (int64_t)rows * l.ldx, blocks * PL));
+        MONARCH_TRY(plane_map(&x_b[i], x[i].at, 0, rows, cols, l.ldx, (int64_t)rows * l.ldx, blocks * PL, l.s.tn / 2));
+        MONARCH_TRY(plane_map(&x_n[i], x[i].at, 1, rows, cols, l.ldx, (int64_t)rows * l.ldx, blocks * PL));
+    }
+    for (int i = 0; i < 2; ++i) MONARCH_TRY(plane_target(&x_to[i], x[i].at, rows, cols, l.ldx, (int64_t)rows * l.ldx, blocks * PL));
+    MONARCH_TRY(plane_target(&s_to, sp.at, l.k, l.k, l.ldk, (int64_t)l.k * l.ldk, blocks * PL));
+    MONARCH_TRY(plane_target(&p_to, pp.at, l.k, l.k, l.ldk, (int64_t)l.k * l.ldk, blocks * PL));
+    MONARCH_TRY(plane_map(&s_a, sp.at, 0, l.k, l.k, l.ldk, (int64_t)l.k * l.ldk, blocks * PL));
+    MONARCH_TRY(plane_map(&s_b, sp.at, 0, l.k, l.k, l.ldk, (int64_t)l.k * l.ldk, blocks * PL, l.p.tn / 2));
+    MONARCH_TRY(plane_map(&p_a, pp.at, 0, l.k, l.k, l.ldk, (int64_t)l.k * l.ldk, blocks * PL));
+    MONARCH_TRY(plane_map(&p_b, pp.at, 0, l.k, l.k, l.ldk, (int64_t)l.k * l.ldk, blocks * PL, l.x.tn / 2));
 
-    CUtensorMap x_k, x_n, s_k, p_k;
-    MONARCH_TRY(plane_map(&x_k, xp, 0, rows, cols, l.ldx, (int64_t)rows * l.ldx, blocks * PL));
-    MONARCH_TRY(plane_map(&x_n, xp, 1, rows, cols, l.ldx, (int64_t)rows * l.ldx, blocks * PL));
-    MONARCH_TRY(plane_map(&s_k, sp, 0, l.k, l.k, l.ldk, (int64_t)l.k * l.ldk, blocks * PL));
-    MONARCH_TRY(plane_map(&p_k, pp, 0, l.k, l.k, l.ldk, (int64_t)l.k * l.ldk, blocks * PL));
-    const Finish fx = {part, l.split_x, rows, cols, l.ldx, X, xp}, fs = {part, l.split_s, l.k, l.k, l.ldk, S, sp},
-                 fp = {part, l.split_p, l.k, l.k, l.ldk, S, pp};
-    auto grid = [&](int64_t n) {
-        int64_t g = (n + 1023) / 1024, most = 148 * 8 / blocks + 1;
-        return dim3((unsigned)(g < most ? g : most), (unsigned)blocks);
-    };
-    MONARCH_TRY(launch_serialized(norm_kernel<T>, dim3(kNormParts, (unsigned)blocks), 256, 0, s, io, norm, size));
-    MONARCH_TRY(launch_serialized(finish_kernel<T, PL, 0>, grid(size), 256, 0, s, fx, io, (const double *)norm));
+    MONARCH_TRY(launch_serialized(norm_kernel<T>, dim3((unsigned)(blocks * l.parts)), 256, 0, s, io, norm, l.parts, (int64_t)rows * cols));
+    int64_t ctas = ceil_div((int64_t)rows * cols, 4096), most = 148 * 8 / blocks + 1;
+    if (ctas > most) ctas = most;
+    MONARCH_TRY(launch_serialized(start_kernel<T, PL>, dim3((unsigned)(blocks * ctas)), 256, 0, s, x[0], io, (const double *)norm, l.parts, (int)ctas));
     PlaneGemm p = {};
     p.status = (unsigned *)ws;
     p.batches = (int)blocks;
     p.a_zstep = p.b_zstep = PL;
-    p.tn = 256;
     p.seg = SCHEME == kP3x3 ? pg_seg(SCHEME) : 16;         // bf16 results: 192 steps
     for (int i = 0; i < steps; ++i) {
-        p.rows = p.cols = l.k;
-        p.kdim = l.n;
-        p.splits = l.split_s;
-        const EpiPart::Args ek = {part, l.k, l.k}, ex = {part, rows, cols};
-        if (wide) MONARCH_TRY((launch_plane_gemm<0, 0, SCHEME, true, EpiPart>(x_k, x_k, p, ek, s)));
-        else MONARCH_TRY((launch_plane_gemm<1, 1, SCHEME, true, EpiPart>(x_n, x_n, p, ek, s)));
-        MONARCH_TRY(launch_serialized(finish_kernel<T, PL, 1>, grid((int64_t)l.k * l.k), 256, 0, s, fs, io, (const double *)norm));
-        p.kdim = l.k;
-        p.splits = l.split_p;
-        MONARCH_TRY((launch_plane_gemm<0, 0, SCHEME, true, EpiPart>(s_k, s_k, p, ek, s)));
-        MONARCH_TRY(launch_serialized(finish_kernel<T, PL, 2>, grid((int64_t)l.k * l.k), 256, 0, s, fp, io, (const double *)norm));
-        p.rows = rows;
-        p.cols = cols;
-        p.splits = l.split_x;
-        if (wide) MONARCH_TRY((launch_plane_gemm<0, 1, SCHEME, true, EpiPart>(p_k, x_n, p, ex, s)));
-        else MONARCH_TRY((launch_plane_gemm<0, 0, SCHEME, true, EpiPart>(x_k, p_k, p, ex, s)));
-        if (i + 1 < steps)
-            MONARCH_TRY(launch_serialized(finish_kernel<T, PL, 3>, grid(size), 256, 0, s, fx, io, (const double *)norm));
-        else
-            MONARCH_TRY(launch_serialized(finish_kernel<T, PL, 4>, grid(size), 256, 0, s, fx, io, (const double *)norm));
+        const int at = i & 1;
+        const typename EpiPlanes<T, PL, kRoleS>::Args es = {sp, io};
+        if (wide) MONARCH_TRY((ortho_product<T, PL, SCHEME, 0, 0, kRoleS>(x_k[at], x_b[at], s_to, p, l.s, l.n, es, part, s)));
+        else MONARCH_TRY((ortho_product<T, PL, SCHEME, 1, 1, kRoleS>(x_n[at], x_n[at], s_to, p, l.s, l.n, es, part, s)));
+        const typename EpiPlanes<T, PL, kRoleP>::Args ep = {pp, io};
+        MONARCH_TRY((ortho_product<T, PL, SCHEME, 0, 0, kRoleP>(s_a, s_b, p_to, p, l.p, l.k, ep, part, s)));
+        if (i + 1 < steps) {
+            const typename EpiPlanes<T, PL, kRoleX>::Args ex = {x[at ^ 1], io};
+            if (wide) MONARCH_TRY((ortho_product<T, PL, SCHEME, 0, 1, kRoleX>(p_a, x_n[at], x_to[at ^ 1], p, l.x, l.k, ex, part, s)));
+            else MONARCH_TRY((ortho_product<T, PL, SCHEME, 0, 0, kRoleX>(x_k[at], p_b, x_to[at ^ 1], p, l.x, l.k, ex, part, s)));
+        } else {
+            const typename EpiPlanes<T, PL, kRoleOut>::Args eo = {x[at], io};
+            if (wide) MONARCH_TRY((ortho_product<T, PL, SCHEME, 0, 1, kRoleOut>(p_a, x_n[at], x_to[at ^ 1], p, l.x, l.k, eo, part, s)));
+            else MONARCH_TRY((ortho_product<T, PL, SCHEME, 0, 0, kRoleOut>(x_k[at], p_b, x_to[at ^ 1], p, l.x, l.k, eo, part, s)));
+        }
     }
     return MONARCH_OK;
 }

@@ -5,7 +5,7 @@
 //   kP2x1  hi hi + lo hi                                first operand in two planes, second one bf16
 //   kP3x1  the same with three planes of the first
 //   kP2x2  hi hi + hi lo + lo hi                        both in two planes (left out: lo lo, at most 2^-16 of the product)
-//   kP3x3  the six with at most two orders of lo        fp32 operands (left out: 2^-23 of the product)
+//   kP3x3  the six with at most two orders of lo        fp32 operands (left out: 2^-23 of the product), hi hi last
 // A tf32 product would keep 11 bits and fp32 FMA runs at a 25th of this rate.
 //
 //   C[m][n] = sum_k A(m, k) B(n, k)       A, B stored [rows][K] (K-major) or [K][rows] (MN-major), each with its own flag
@@ -28,16 +28,19 @@ namespace tc {
 enum PlaneScheme { kP1 = 0, kP2x1 = 1, kP2x2 = 2, kP3x3 = 3, kP3x1 = 4 };
 
 constexpr int kPgTile = 256, kPgChunk = 64;
-constexpr int kPgSlotBytes = 128 * kPgChunk * 2, kPgSlots = 13;
+constexpr int kPgSlotBytes = 128 * kPgChunk * 2, kPgMaxSlots = 13;
 constexpr int kPgThreads = 320, kPgEpiWarps = 8;
-constexpr int kPgSmem = kPgSlots * kPgSlotBytes + 1024;
+constexpr int kPgStageBytes = 32 * 32 * 2;      // an epilogue warp's piece of a bf16 result
+// slots beside `stage` such pieces per epilogue warp
+__host__ __device__ constexpr int pg_slots(int stage) { return kPgMaxSlots - stage * kPgEpiWarps * kPgStageBytes / kPgSlotBytes; }
+__host__ __device__ constexpr int pg_smem(int stage) { return pg_slots(stage) * kPgSlotBytes + stage * kPgEpiWarps * kPgStageBytes + 1024; }
 
 // loads per K chunk: bit 2 = operand B, bits 0-1 = plane
 __host__ __device__ constexpr int pg_loads(int s) { return s == kP1 ? 2 : s == kP2x1 ? 3 : s == kP2x2 || s == kP3x1 ? 4 : 6; }
 __host__ __device__ constexpr int pg_load(int s, int l)
 {
     constexpr int kB = 4;
-    constexpr int t[5][6] = {{0, kB, 0, 0, 0, 0}, {kB, 0, 1, 0, 0, 0}, {0, kB, kB + 1, 1, 0, 0}, {0, kB, kB + 1, kB + 2, 1, 2}, {kB, 0, 1, 2, 0, 0}};
+    constexpr int t[5][6] = {{0, kB, 0, 0, 0, 0}, {kB, 0, 1, 0, 0, 0}, {0, kB, kB + 1, 1, 0, 0}, {0, kB + 2, kB + 1, 1, kB, 2}, {kB, 0, 1, 2, 0, 0}};
     return t[s][l];
 }
 // products that become possible with load l: (load of A) | (load of B) << 4, up to two; 0xff: none
@@ -47,22 +50,23 @@ __host__ __device__ constexpr int pg_mma(int s, int l, int i)
     constexpr int t[5][6][2] = {{{none, none}, {0x10, none}, {none, none}, {none, none}, {none, none}, {none, none}},
                                 {{none, none}, {0x01, none}, {0x02, none}, {none, none}, {none, none}, {none, none}},
                                 {{none, none}, {0x10, none}, {0x20, none}, {0x13, none}, {none, none}, {none, none}},
-                                {{none, none}, {0x10, none}, {0x20, none}, {0x30, none}, {0x14, 0x24}, {0x15, none}},
+                                {{none, none}, {0x10, none}, {0x20, none}, {0x23, none}, {0x43, none}, {0x45, 0x40}},
                                 {{none, none}, {0x01, none}, {0x02, none}, {0x03, none}, {none, none}, {none, none}}};
     return t[s][l][i];
 }
 // loads whose last use is among the products of load l (bit mask)
 __host__ __device__ constexpr int pg_done(int s, int l)
 {
-    constexpr int t[5][6] = {{0, 3, 0, 0, 0, 0}, {0, 2, 5, 0, 0, 0}, {0, 0, 5, 10, 0, 0}, {0, 0, 0, 9, 20, 34}, {0, 2, 4, 9, 0, 0}};
+    constexpr int t[5][6] = {{0, 3, 0, 0, 0, 0}, {0, 2, 5, 0, 0, 0}, {0, 0, 5, 10, 0, 0}, {0, 2, 0, 4, 8, 49}, {0, 2, 4, 9, 0, 0}};
     return t[s][l];
 }
 
 // The tensor cores add to an fp32 accumulator without rounding to nearest: sums of mixed signs shrink by some 2^-25 per step of 16
 // products (measured: a sum over 8192 tokens of two planes, 1024 steps, was 1.9e-5 off; 3e-5 over 1500 steps).  Where the result is
 // float32, a run in tensor memory ends after this many K chunks and the epilogue warps add the runs up in registers, while the
-// MMAs go on in the other accumulator.
-__host__ __device__ constexpr int pg_seg(int s) { return s == kP1 ? 16 : s == kP2x1 ? 8 : s == kP2x2 || s == kP3x1 ? 5 : 2; }
+// MMAs go on in the other accumulator.  With all six plane products a run is one chunk, hi hi last: the 20 steps before it lose of
+// sums that are 2^-8 as large, four of the whole (orthogonalised update in fp32, hi hi first and runs of two chunks: 1.9e-5 off).
+__host__ __device__ constexpr int pg_seg(int s) { return s == kP1 ? 16 : s == kP2x1 ? 8 : s == kP2x2 || s == kP3x1 ? 5 : 1; }
 
 struct PlaneGemm {
     unsigned *status;
@@ -139,12 +143,6 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&f)[32])
     asm volatile("" : "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])::"memory");
 }
 
-// 32 bytes in one store: a full sector
-__device__ __forceinline__ void st_v8(void *p, uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t e, uint32_t f, uint32_t g, uint32_t h)
-{
-    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e), "r"(f), "r"(g), "r"(h) : "memory");
-}
-
 // one lane of a converged warp; unlike lane == 0 it leaves the operands of what follows in uniform registers
 __device__ __forceinline__ bool elect_one()
 {
@@ -153,18 +151,61 @@ __device__ __forceinline__ bool elect_one()
     return p != 0;
 }
 
+// Results in bf16 leave through shared memory: 32 x 32 pieces (64-byte swizzle) that TMA writes.  A thread has a row: stored from
+// registers, each instruction would touch 32 rows of 32 bytes.  One such ring per warp; lane 0 sends and waits.
+template <int N> struct PgStage {
+    const CUtensorMap *map;
+    uint32_t base;
+    int at, lane;
+    __device__ __forceinline__ uint32_t begin()
+    {
+        if (lane == 0) tma_store_wait_read<N - 1>();
+        __syncwarp();
+        return base + at * kPgStageBytes;
+    }
+    __device__ __forceinline__ void send(int x, int y, int z)
+    {
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+            tma_store_3d(map, base + at * kPgStageBytes, x, y, z);
+            tma_store_commit();
+        }
+        at = at + 1 == N ? 0 : at + 1;
+    }
+    // 16 packed words: this lane's row of 32 values
+    __device__ __forceinline__ void row(uint32_t buf, const uint32_t (&w)[16]) const
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)), "r"(w[4 * j]), "r"(w[4 * j + 1]),
+                         "r"(w[4 * j + 2]), "r"(w[4 * j + 3])
+                         : "memory");
+    }
+    // the same as a column
+    __device__ __forceinline__ void column(uint32_t buf, const uint32_t (&w)[16]) const
+    {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            asm volatile("st.shared.b16 [%0], %1;" ::"r"(buf + j * 64 + (((lane >> 3) ^ ((j >> 1) & 3)) << 4) + (lane & 7) * 2),
+                         "h"((uint16_t)(w[j / 2] >> (j % 2 * 16)))
+                         : "memory");
+    }
+};
+
 struct PgBars {
-    uint64_t full[kPgSlots], empty[kPgSlots];                           // full: used in the even CTA only
+    uint64_t full[kPgMaxSlots], empty[kPgMaxSlots];                           // full: used in the even CTA only
     uint64_t acc_full[2], acc_empty[2];
 };
 
-// Epi: struct with  begin(const Epi::Args &, const PgTile &),  chunk(args, tile, c, float (&v)[32])  for c = 0, 32, .. < tn / 2,
-// end(args, tile).  PROMOTE: at most p.seg chunks are accumulated in tensor memory, sums of those in fp32 registers.
+// Epi: struct with  begin(const Epi::Args &, const PgTile &),  chunk(args, tile, c, float (&v)[32], stage)  for c = 0, 32, .. < tn / 2,
+// end(args, tile); kStage: pieces in `stage`, its warp's PgStage (0: none).  PROMOTE: at most p.seg chunks are accumulated in tensor memory, sums of those in fp32 registers.
 template <int AMN, int BMN, int SCHEME, bool PROMOTE, class Epi>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPgThreads, 1)
-plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const PlaneGemm p,
-                  const typename Epi::Args args)
+plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CUtensorMap tm_c,
+                  const PlaneGemm p, const typename Epi::Args args)
 {
+    constexpr int kPgSlots = pg_slots(Epi::kStage);
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) PgBars bars;
     __shared__ uint32_t tmem_base_s;
@@ -349,6 +390,7 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
         const uint32_t lane_base = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)((warp >> 2) * (tn / 2));
         uint32_t it = 0;
         bool ok = true;
+        PgStage<(Epi::kStage > 0 ? Epi::kStage : 1)> stage = {&tm_c, ring0 + kPgSlots * kPgSlotBytes + warp * Epi::kStage * kPgStageBytes, 0, lane};
         for (long long tile = pair; ok && tile < total; tile += npairs) {
             const At at = locate(tile);
             PgTile t;
@@ -382,7 +424,7 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] = 0.0f;
                     }
-                    e.chunk(args, t, h * 32, v);
+                    e.chunk(args, t, h * 32, v, stage);
                 }
             } else {
                 float acc[4][32];
@@ -409,10 +451,11 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
                 if (!ok) break;
 #pragma unroll
                 for (int h = 0; h < 4; ++h)
-                    if (h * 64 < tn) e.chunk(args, t, h * 32, acc[h]);
+                    if (h * 64 < tn) e.chunk(args, t, h * 32, acc[h], stage);
             }
             e.end(args, t);
         }
+        if (Epi::kStage > 0 && lane == 0) tma_store_wait_all<0>();
     }
 
     // the even CTA's barriers receive arrivals from the odd CTA until it is done: leave together
@@ -434,9 +477,20 @@ inline int plane_map(CUtensorMap *m, const void *base, int mn_major, int64_t row
     return encode_tmap_nd(m, base, 2, 3, dims, strides, box, 128);
 }
 
-template <int AMN, int BMN, int SCHEME, bool PROMOTE, class Epi>
-int launch_plane_gemm(const CUtensorMap &tm_a, const CUtensorMap &tm_b, const PlaneGemm &p, const typename Epi::Args &args, cudaStream_t s)
+// as the target of PgStage pieces
+inline int plane_target(CUtensorMap *m, const void *base, int64_t rows, int64_t cols, int64_t ld, int64_t zstride, int64_t z)
 {
+    const uint64_t dims[3] = {(uint64_t)cols, (uint64_t)rows, (uint64_t)z};
+    const uint64_t strides[2] = {(uint64_t)ld * 2, (uint64_t)zstride * 2};
+    const uint32_t box[3] = {32, 32, 1};
+    return encode_tmap_nd(m, base, 2, 3, dims, strides, box, 64);
+}
+
+// tm_c: the target of an epilogue that has a stage (any map for the others)
+template <int AMN, int BMN, int SCHEME, bool PROMOTE, class Epi>
+int launch_plane_gemm(const CUtensorMap &tm_a, const CUtensorMap &tm_b, const CUtensorMap &tm_c, const PlaneGemm &p, const typename Epi::Args &args, cudaStream_t s)
+{
+    constexpr int kPgSmem = pg_smem(Epi::kStage);
     const auto kern = plane_gemm_kernel<AMN, BMN, SCHEME, PROMOTE, Epi>;
     static PerDeviceCache cache;
     int pairs = cache.get();
@@ -459,7 +513,7 @@ int launch_plane_gemm(const CUtensorMap &tm_a, const CUtensorMap &tm_b, const Pl
     const long long total = (p.lower ? mt * (mt + 1) / 2 * (kPgTile / p.tn) : mt * ((p.cols + p.tn - 1) / p.tn)) * p.batches * p.splits;
     if (total <= 0) return MONARCH_OK;
     const int grid = 2 * (int)(total < pairs ? total : pairs);
-    return launch_serialized(kern, dim3((unsigned)grid), kPgThreads, kPgSmem, s, tm_a, tm_b, p, args);
+    return launch_serialized(kern, dim3((unsigned)grid), kPgThreads, kPgSmem, s, tm_a, tm_b, tm_c, p, args);
 }
 
 }  // namespace tc

@@ -180,6 +180,7 @@ __global__ void __launch_bounds__(256) split_rows_kernel(const T *__restrict__ W
 // Per row and half tile: r = log2(e) times the maximum, rounded, and s = sum 2^(z log2 e - r).  Exponents are formed by one FMA
 // from z and r, so the rounding of r cancels in r + log2 s.
 struct EpiStats {
+    static constexpr int kStage = 0;
     struct Args {
         float2 *part;              // [rows of the chunk][2 * column tiles]
         float *tlogit;             // logit of the target
@@ -196,7 +197,7 @@ struct EpiStats {
         live = t.row < *a.count;
         y = live ? a.tgt[t.row] - a.v0 - t.col : -1;
     }
-    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32])
+    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<1> &)
     {
         const int left = a.cols - t.col - c;
         if (left <= 0) return;
@@ -233,10 +234,9 @@ struct EpiStats {
 
 // g of a piece of the vocabulary; zeros behind the last row and the last column
 template <int PL> struct EpiGrad {
+    static constexpr int kStage = 2;
     struct Args {
-        __nv_bfloat16 *g;
-        size_t plane;
-        int ld, cols, v0;
+        int cols, v0;
         const int *tgt, *count;
         const float *lse, *dl;
     };
@@ -252,7 +252,7 @@ template <int PL> struct EpiGrad {
         dl = live ? a.dl[t.row] : 0.0f;
         y = live ? a.tgt[t.row] - a.v0 - t.col : -1;
     }
-    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32])
+    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<kStage> &st)
     {
         const int left = live ? a.cols - t.col - c : 0, at = y - c;
 #pragma unroll
@@ -260,9 +260,8 @@ template <int PL> struct EpiGrad {
             const float e = ex2(fmaf(v[i], kLog2e, -r_hi) - r_lo);
             v[i] = i >= left ? 0.0f : dl * (at == i ? e - 1.0f : e);
         }
-        __nv_bfloat16 *out = a.g + (size_t)t.row * a.ld + t.col + c;
 #pragma unroll
-        for (int q = 0; q < PL; ++q, out += a.plane) {
+        for (int q = 0; q < PL; ++q) {
             uint32_t w[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -272,8 +271,8 @@ template <int PL> struct EpiGrad {
                     v[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
                 }
             }
-            st_v8(out, w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]);
-            st_v8(out + 16, w[8], w[9], w[10], w[11], w[12], w[13], w[14], w[15]);
+            st.row(st.begin(), w);
+            st.send(t.col + c, t.row & ~31, q);
         }
     }
     __device__ __forceinline__ void end(const Args &, const PgTile &) {}
@@ -281,12 +280,13 @@ template <int PL> struct EpiGrad {
 
 // rows of float32, stored or added to
 struct EpiStoreF32 {
+    static constexpr int kStage = 0;
     struct Args {
         float *out;
         int rows, cols, add;
     };
     __device__ __forceinline__ void begin(const Args &, const PgTile &) {}
-    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32])
+    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<1> &)
     {
         if (t.row >= a.rows) return;
         const int left = a.cols - t.col - c;
@@ -315,6 +315,7 @@ struct EpiStoreF32 {
 
 // dx: the sums of the pieces so far in float32 (compact rows), the last one to the caller's rows
 template <typename T> struct EpiDx {
+    static constexpr int kStage = 0;
     struct Args {
         float *acc;
         T *dx;
@@ -326,7 +327,7 @@ template <typename T> struct EpiDx {
     {
         to = t.row < *a.count ? (a.last ? a.map[t.row] : t.row) : -1;
     }
-    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32])
+    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<1> &)
     {
         if (to < 0) return;
         const int left = a.d - t.col - c;
@@ -367,6 +368,7 @@ template <typename T> struct EpiDx {
 
 // dx where a few tiles are split along the vocabulary: a sum per part, over the pieces, in float32
 struct EpiDxPart {
+    static constexpr int kStage = 0;
     struct Args {
         float *acc;                // [parts][tokens][d]
         const int *count;
@@ -378,7 +380,7 @@ struct EpiDxPart {
     {
         to = t.row < *a.count ? a.acc + t.z * a.part + (size_t)t.row * a.d + t.col : nullptr;
     }
-    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32])
+    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<1> &)
     {
         if (to == nullptr) return;
         const int left = a.d - t.col - c;
@@ -780,13 +782,13 @@ PlaneGemm gemm(unsigned *status)
     return g;
 }
 
-// Logits.  An error of z is a relative error of g, so their sums in tensor memory end after 64 (bf16) or 48 (fp32) steps
+// Logits.  An error of z is a relative error of g, so their sums in tensor memory end after 64 (bf16) or 24 (fp32) steps
 // (pg_seg); the loss alone takes less harm (bf16, d = 1024: 3.4e-7 of lse).
-template <int SCHEME, class Epi> int logits(const CUtensorMap &ma, const CUtensorMap &mb, PlaneGemm p, const typename Epi::Args &e, bool exact, cudaStream_t s)
+template <int SCHEME, class Epi> int logits(const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mc, PlaneGemm p, const typename Epi::Args &e, bool exact, cudaStream_t s)
 {
     p.seg = pg_seg(SCHEME);
-    if (exact && p.kdim > p.seg * kPgChunk) return launch_plane_gemm<0, 0, SCHEME, true, Epi>(ma, mb, p, e, s);
-    return launch_plane_gemm<0, 0, SCHEME, false, Epi>(ma, mb, p, e, s);
+    if (exact && p.kdim > p.seg * kPgChunk) return launch_plane_gemm<0, 0, SCHEME, true, Epi>(ma, mb, mc, p, e, s);
+    return launch_plane_gemm<0, 0, SCHEME, false, Epi>(ma, mb, mc, p, e, s);
 }
 
 }  // namespace
@@ -868,8 +870,8 @@ int xent_fwd(const void *x, const void *W, const int64_t *targets, float *loss, 
             }
             const EpiStats::Args e = {part, tlogit, tgt, count, (int)row0, cols, v0, l.halves, half0};
             half0 += 2 * ceil_div(cols, l.tn);
-            if (dtype == MONARCH_F32) MONARCH_TRY((logits<kP3x3, EpiStats>(ma, mb, p, e, true, s)));
-            else MONARCH_TRY((logits<kP1, EpiStats>(ma, mb, p, e, d > 8192, s)));
+            if (dtype == MONARCH_F32) MONARCH_TRY((logits<kP3x3, EpiStats>(ma, mb, mb, p, e, true, s)));
+            else MONARCH_TRY((logits<kP1, EpiStats>(ma, mb, mb, p, e, d > 8192, s)));
         }
         const int ctas = ceil_div(rows, 8) < 148 * 8 ? ceil_div(rows, 8) : 148 * 8;
         MONARCH_TRY(launch_serialized(xent_join_kernel, dim3((unsigned)ctas), 256, 0, s, (const float2 *)part, (const float *)tlogit,
@@ -892,7 +894,8 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
     int *splits = (int *)(base + l.splits);
     const size_t gplane = (size_t)l.trows * l.piece;
 
-    CUtensorMap x_k, x_n, w_k, w_n, g_m, g_k;
+    CUtensorMap x_k, x_n, w_k, w_n, g_m, g_k, g_to;
+    MONARCH_TRY(plane_target(&g_to, g, l.trows, l.piece, l.piece, (int64_t)gplane, l.gplanes));
     MONARCH_TRY(plane_map(&x_k, xp, 0, tokens, l.dp, l.dp, tokens * l.dp, l.planes));
     MONARCH_TRY(plane_map(&x_n, xp, 1, tokens, l.dp, l.dp, tokens * l.dp, l.planes));
     MONARCH_TRY(plane_map(&g_k, g, 0, l.trows, l.piece, l.piece, (int64_t)gplane, l.gplanes));
@@ -913,8 +916,8 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
         p.count = count; p.rows = (int)tokens; p.cols = cols; p.kdim = d; p.tn = l.tn;
         p.a_zstep = p.b_zstep = l.planes;
         p.b_n0 = l.direct ? v0 : 0;
-        const typename EpiGrad<GP>::Args eg = {g, gplane, l.piece, cols, v0, tgt, count, clse, cdl};
-        MONARCH_TRY((logits<LOGITS, EpiGrad<GP>>(x_k, w_k, p, eg, true, s)));
+        const typename EpiGrad<GP>::Args eg = {cols, v0, tgt, count, clse, cdl};
+        MONARCH_TRY((logits<LOGITS, EpiGrad<GP>>(x_k, w_k, g_to, p, eg, true, s)));
         // dW = g^T x
         p = gemm(status);
         p.count = count; p.count_is_k = 1; p.rows = cols; p.cols = d; p.kdim = (int)tokens; p.tn = l.tn_dw;
@@ -922,7 +925,7 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
         p.n_fastest = 1;
         p.seg = pg_seg(DW);
         const EpiStoreF32::Args ew = {dW + (size_t)v0 * d, cols, d, accumulate};
-        MONARCH_TRY((launch_plane_gemm<1, 1, DW, true, EpiStoreF32>(g_m, x_n, p, ew, s)));
+        MONARCH_TRY((launch_plane_gemm<1, 1, DW, true, EpiStoreF32>(g_m, x_n, x_n, p, ew, s)));
         // dx += g W
         p = gemm(status);
         p.count = count; p.rows = (int)tokens; p.cols = d; p.kdim = cols; p.tn = l.tn_dx;
@@ -932,14 +935,14 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
         p.seg = pg_seg(DX);
         if (l.dx_parts == 1) {
             const typename EpiDx<T>::Args ex = {acc, dx, map, count, d, v0 == 0, v0 + cols == vocab};
-            MONARCH_TRY((launch_plane_gemm<0, 1, DX, DX != kP1, EpiDx<T>>(g_k, w_n, p, ex, s)));
+            MONARCH_TRY((launch_plane_gemm<0, 1, DX, DX != kP1, EpiDx<T>>(g_k, w_n, w_n, p, ex, s)));
         } else {
             // the last piece may be smaller: every piece has as many parts as the first found best
             p.splits = l.dx_parts;
             p.splits_out = v0 == 0 ? splits : nullptr;
             p.splits_in = v0 == 0 ? nullptr : splits;
             const EpiDxPart::Args ex = {acc, count, (size_t)tokens * d, d, v0 == 0};
-            MONARCH_TRY((launch_plane_gemm<0, 1, DX, DX != kP1, EpiDxPart>(g_k, w_n, p, ex, s)));
+            MONARCH_TRY((launch_plane_gemm<0, 1, DX, DX != kP1, EpiDxPart>(g_k, w_n, w_n, p, ex, s)));
         }
     }
     if (l.dx_parts > 1) {
