@@ -219,6 +219,17 @@ _SPECS = {
 }
 
 
+# Sizes of the tensors as products of integer arguments, by name: these calls check them, and that the tensors are on the current
+# device, whose stream is used.
+_SIZES = {
+    "monarch_xent_fwd": {"x": "tokens d", "W": "vocab d", "targets": "tokens", "loss": "tokens", "lse": "tokens"},
+    "monarch_xent_bwd": {"x": "tokens d", "W": "vocab d", "targets": "tokens", "lse": "tokens", "dloss": "tokens", "dx": "tokens d",
+                         "dW": "vocab d"},
+    "monarch_orthogonalize": {"G": "blocks rows cols", "O": "blocks rows cols"},
+    "monarch_muon_step": {"W": "blocks rows cols", "dW": "blocks rows cols", "V": "blocks rows cols"},
+}
+
+
 def _current_stream() -> int:
     import torch
     return torch.cuda.current_stream().cuda_stream
@@ -232,7 +243,12 @@ def _native(name: str):
     current = (lambda: raw(device())) if raw is not None and device is not None else _current_stream
     spec, names = _SPECS[name]
     address = ctypes.cast(getattr(lib(), name), _vp).value
-    call = _pycalls.Call(name, address, spec, tuple(names.split()), (torch.float32, torch.bfloat16, torch.int64), _check, current)
+    names = tuple(names.split())
+    sizes = _SIZES.get(name)
+    if sizes is not None:
+        sizes = tuple(tuple(names.index(f) for f in sizes.get(n, "").split()) for n in names)
+    device_of = device if device is not None and torch.cuda.is_available() else (lambda: 0)
+    call = _pycalls.Call(name, address, spec, names, (torch.float32, torch.bfloat16, torch.int64), _check, current, sizes, device_of)
     _calls[name] = call
     return call
 
@@ -296,19 +312,6 @@ def monarch_project(A, L, R, n, m, rotation_count=None, stream=None) -> None:
     (_calls.get("monarch_project") or _native("monarch_project"))(A, L, R, n, m, rotation_count, stream)
 
 
-def _sizes(call: str, **tensors) -> None:
-    """The tensors of a call, each with the number of values that the call touches: enough of them, on the current device, whose stream is used."""
-    import torch
-    device = torch.cuda.current_device() if torch.cuda.is_available() else 0
-    for name, (t, n) in tensors.items():
-        if t is None:
-            continue
-        if t.numel() < n:
-            raise ValueError(f"{call}: {name} must have at least {n} values, got {t.numel()}")
-        if t.is_cuda and t.get_device() != device:
-            raise ValueError(f"{call}: {name} is on device {t.get_device()}, the current one is {device}")
-
-
 def monarch_xent_workspace_bytes(tokens: int, d: int, vocab: int, dtype: int) -> int:
     return int(lib().monarch_xent_workspace_bytes(tokens, d, vocab, dtype))
 
@@ -319,15 +322,12 @@ def monarch_xent_bwd_workspace_bytes(tokens: int, d: int, vocab: int, dtype: int
 
 def monarch_xent_fwd(x, W, targets, loss, lse, tokens, d, vocab, ignore_index, workspace, stream=None) -> None:
     """loss[t] = lse[t] - x[t] . W[targets[t]], lse[t] = log sum_v exp(x[t] . W[v]); targets int64, loss and lse float32."""
-    _sizes("monarch_xent_fwd", x=(x, tokens * d), W=(W, vocab * d), targets=(targets, tokens), loss=(loss, tokens), lse=(lse, tokens))
     (_calls.get("monarch_xent_fwd") or _native("monarch_xent_fwd"))(x, W, targets, loss, lse, tokens, d, vocab, ignore_index,
                                                                     workspace, stream)
 
 
 def monarch_xent_bwd(x, W, targets, lse, dloss, dx, dW, accumulate, tokens, d, vocab, ignore_index, workspace, stream=None) -> None:
     """Gradients of sum_t dloss[t] loss[t]: dx like x, dW [vocab, d] in float32 (accumulate=1 adds to it)."""
-    _sizes("monarch_xent_bwd", x=(x, tokens * d), W=(W, vocab * d), targets=(targets, tokens), lse=(lse, tokens),
-           dloss=(dloss, tokens), dx=(dx, tokens * d), dW=(dW, vocab * d))
     (_calls.get("monarch_xent_bwd") or _native("monarch_xent_bwd"))(x, W, targets, lse, dloss, dx, dW, int(accumulate), tokens, d,
                                                                     vocab, ignore_index, workspace, stream)
 
@@ -338,15 +338,11 @@ def monarch_ortho_workspace_bytes(blocks: int, rows: int, cols: int, dtype: int)
 
 def monarch_orthogonalize(G, O, blocks, rows, cols, steps, workspace, stream=None) -> None:
     """O = G with the singular values of every [rows, cols] block taken near 1 by ``steps`` Newton-Schulz products."""
-    n = blocks * rows * cols
-    _sizes("monarch_orthogonalize", G=(G, n), O=(O, n))
     (_calls.get("monarch_orthogonalize") or _native("monarch_orthogonalize"))(G, O, blocks, rows, cols, steps, workspace, stream)
 
 
 def monarch_muon_step(W, dW, V, blocks, rows, cols, lr, weight_decay, beta, nesterov, scale, steps, workspace, stream=None) -> None:
     """V <- beta V + dW; W <- (1 - lr weight_decay) W - lr scale orthogonalised(dW + beta V, or V without nesterov), in place."""
-    n = blocks * rows * cols
-    _sizes("monarch_muon_step", W=(W, n), dW=(dW, n), V=(V, n))
     (_calls.get("monarch_muon_step") or _native("monarch_muon_step"))(W, dW, V, blocks, rows, cols, lr, weight_decay, beta,
                                                                       int(nesterov), scale, steps, workspace, stream)
 

@@ -522,17 +522,6 @@ template <int PL, bool BOTH> __device__ __forceinline__ void tc_put(uint32_t pla
     }
 }
 
-// 16 columns of this thread's lane, requested; tmem_ready names the registers so that nothing that reads them moves before it
-__device__ __forceinline__ void tmem_ask16(uint32_t taddr, float (&f)[16]) { tmem_ld16(taddr, reinterpret_cast<uint32_t (&)[16]>(f)); }
-__device__ __forceinline__ void tmem_ready(float (&f)[16])
-{
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+f"(f[0]), "+f"(f[1]), "+f"(f[2]), "+f"(f[3]), "+f"(f[4]), "+f"(f[5]), "+f"(f[6]), "+f"(f[7]), "+f"(f[8]), "+f"(f[9]),
-                   "+f"(f[10]), "+f"(f[11]), "+f"(f[12]), "+f"(f[13]), "+f"(f[14]), "+f"(f[15])
-                 :
-                 : "memory");
-}
-
 template <typename T, int PL>
 __global__ void __launch_bounds__(kTcThreads, 1) ortho_tc_kernel(const Io<T> io, int rows, int cols, int steps, unsigned *status)
 {
@@ -807,7 +796,7 @@ template <int ROLE> __device__ __forceinline__ float finished(float v, int row, 
 }
 
 template <typename T, int PL, int ROLE> struct EpiPlanes {
-    static constexpr int kStage = ROLE == kRoleOut ? 0 : 2;
+    static constexpr int kStage = ROLE == kRoleOut ? 3 : ROLE == kRoleX ? PL : 4;            // S, P: a plane and its transpose, twice
     struct Args {
         Planes to;                 // also the sizes of the result
         Io<T> io;                  // kRoleOut
@@ -817,46 +806,61 @@ template <typename T, int PL, int ROLE> struct EpiPlanes {
     {
         const Planes &m = a.to;
         const int col = t.col + c, row0 = t.row & ~31;
+        if (row0 >= m.rows || col >= m.cols) return;                           // the same in all lanes; TMA clips the rest
         if constexpr (ROLE == kRoleOut) {
-            if (t.row >= m.rows) return;
-            const size_t at = ((size_t)t.z * m.rows + t.row) * m.cols + col;
-            if (m.cols % 4 == 0) {
-#pragma unroll
-                for (int i = 0; i < 32; i += 8) {
-                    float w[2][4];
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        if (col + i + 4 * j < m.cols) a.io.old4(at + i + 4 * j, w[j]);
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        if (col + i + 4 * j < m.cols) {
-                            float o[4] = {v[i + 4 * j], v[i + 4 * j + 1], v[i + 4 * j + 2], v[i + 4 * j + 3]};
-                            a.io.write4(at + i + 4 * j, o, w[j]);
-                        }
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (col + i < m.cols) a.io.write(at + i, v[i], a.io.old(at + i));
-            }
+            const size_t at = ((size_t)t.z * m.rows + row0) * m.cols + col + st.lane;
+            const int rows = col + st.lane < m.cols ? m.rows - row0 : 0;
+            st.rows(
+                v, [&](int r) { return r < rows ? a.io.old(at + (size_t)r * m.cols) : 0.0f; },
+                [&](int r, float x, float w) {
+                    if (r < rows) a.io.write(at + (size_t)r * m.cols, x, w);
+                });
         } else {
-            if (row0 >= m.rows || col >= m.cols) return;                       // the same in all lanes; TMA clips the rest
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = finished<ROLE>(v[i], t.row, col + i);
-#pragma unroll
-            for (int q = 0; q < PL; ++q) {
-                uint32_t w[16];
+            auto next_plane = [&](uint32_t (&w)[16]) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
                     v[2 * i] -= __uint_as_float(w[i] << 16);
                     v[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
                 }
-                st.row(st.begin(), w);
-                st.send(col, row0, t.z * PL + q);
-                if ((ROLE == kRoleS || ROLE == kRoleP) && t.mirror) {
-                    st.column(st.begin(), w);
-                    st.send(row0, col, t.z * PL + q);
+            };
+            if constexpr (ROLE == kRoleX) {
+                st.begin();
+#pragma unroll
+                for (int q = 0; q < PL; ++q) {
+                    uint32_t w[16];
+                    next_plane(w);
+                    st.row(q, w);
+                }
+                st.ready();
+#pragma unroll
+                for (int q = 0; q < PL; ++q) st.send(q, col, row0, t.z * PL + q);
+                st.close();
+            } else {
+                // two planes behind one fence, then the third (fp32): more pieces would be taken from the operands' ring
+#pragma unroll
+                for (int q0 = 0; q0 < PL; q0 += 2) {
+                    st.begin();
+#pragma unroll
+                    for (int q = q0; q < q0 + 2 && q < PL; ++q) {
+                        uint32_t w[16];
+                        next_plane(w);
+                        st.row(q - q0, w);
+                    }
+                    if (t.mirror) {
+                        __syncwarp();
+#pragma unroll
+                        for (int q = q0; q < q0 + 2 && q < PL; ++q) st.transpose(q - q0, 2 + q - q0);
+                    }
+                    st.ready();
+#pragma unroll
+                    for (int q = q0; q < q0 + 2 && q < PL; ++q) {
+                        st.send(q - q0, col, row0, t.z * PL + q);
+                        if (t.mirror) st.send(2 + q - q0, row0, col, t.z * PL + q);
+                    }
+                    st.close();
                 }
             }
         }
@@ -866,26 +870,23 @@ template <typename T, int PL, int ROLE> struct EpiPlanes {
 
 // a part of K, float32
 struct EpiPart {
-    static constexpr int kStage = 0;
+    static constexpr int kStage = 3;
     struct Args {
         float *out;                // [blocks][splits][rows][cols]
         int rows, cols;
     };
     __device__ __forceinline__ void begin(const Args &, const PgTile &) {}
-    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<1> &)
+    template <class Stage> __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], Stage &st)
     {
-        if (t.row >= a.rows) return;
-        const int left = a.cols - t.col - c;
-        float *out = a.out + ((size_t)t.z * a.rows + t.row) * a.cols + t.col + c;
-        if ((a.cols & 3) == 0) {
-#pragma unroll
-            for (int i = 0; i < 32; i += 4)
-                if (i < left) *reinterpret_cast<float4 *>(out + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (i < left) out[i] = v[i];
-        }
+        const int col = t.col + c, row0 = t.row & ~31;
+        if (row0 >= a.rows || col >= a.cols) return;
+        float *out = a.out + ((size_t)t.z * a.rows + row0) * a.cols + col + st.lane;
+        const int rows = col + st.lane < a.cols ? a.rows - row0 : 0;
+        st.rows(
+            v, [](int) { return 0.0f; },
+            [&](int r, float x, float) {
+                if (r < rows) out[(size_t)r * a.cols] = x;
+            });
     }
     __device__ __forceinline__ void end(const Args &, const PgTile &) {}
 };
@@ -1040,7 +1041,7 @@ struct Cut {
 };
 
 // by the time it takes, in cycles: rounds of the CTA pairs over tiles of `products` MMAs of 512 cycles per K chunk (narrow tiles load
-// more per MMA), 3000 for a tile's start and end, 8000 for the launch that adds parts up
+// more per MMA), 6000 for a tile's start and end, 20000 for the launch that adds parts up
 Cut cut(int64_t blocks, int m, int n, int kdim, int products, bool lower)
 {
     Cut best = {256, 1};
@@ -1052,7 +1053,7 @@ Cut cut(int64_t blocks, int m, int n, int kdim, int products, bool lower)
             if (s > 1 && tiles * (s - 1) >= 2 * kPgPairs) break;
             const int64_t rounds = (tiles * s + kPgPairs - 1) / kPgPairs;
             const double chunk = 512.0 * products * tn / 256 * (tn == 128 ? 1.2 : 1.0);
-            const double cost = rounds * ((double)((chunks + s - 1) / s) * chunk + 3000.0) + (s > 1 ? 8000.0 : 0.0);
+            const double cost = rounds * ((double)((chunks + s - 1) / s) * chunk + 6000.0) + (s > 1 ? 20000.0 : 0.0);
             if (cost < best_cost) {
                 best_cost = cost;
                 best = {tn, s};

@@ -143,6 +143,17 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&f)[32])
     asm volatile("" : "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])::"memory");
 }
 
+// 16 columns of this thread's lane, requested; tmem_ready names the registers so that nothing that reads them moves before it
+__device__ __forceinline__ void tmem_ask16(uint32_t taddr, float (&f)[16]) { tmem_ld16(taddr, reinterpret_cast<uint32_t (&)[16]>(f)); }
+__device__ __forceinline__ void tmem_ready(float (&f)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(f[0]), "+f"(f[1]), "+f"(f[2]), "+f"(f[3]), "+f"(f[4]), "+f"(f[5]), "+f"(f[6]), "+f"(f[7]), "+f"(f[8]), "+f"(f[9]),
+                   "+f"(f[10]), "+f"(f[11]), "+f"(f[12]), "+f"(f[13]), "+f"(f[14]), "+f"(f[15])
+                 :
+                 : "memory");
+}
+
 // one lane of a converged warp; unlike lane == 0 it leaves the operands of what follows in uniform registers
 __device__ __forceinline__ bool elect_one()
 {
@@ -151,45 +162,75 @@ __device__ __forceinline__ bool elect_one()
     return p != 0;
 }
 
-// Results in bf16 leave through shared memory: 32 x 32 pieces (64-byte swizzle) that TMA writes.  A thread has a row: stored from
-// registers, each instruction would touch 32 rows of 32 bytes.  One such ring per warp; lane 0 sends and waits.
+// Results leave through shared memory, N pieces of 2 KB per epilogue warp.  A thread has a row of 32 columns: stored from registers,
+// each instruction would touch 32 rows of 16 or 32 bytes.
+//   bf16 planes  32 x 32 pieces (64-byte swizzle) that TMA writes, all planes of a chunk behind one proxy fence (a fence per piece
+//                took 0.5 us each); lane 0 sends and waits
+//   float32      a 32 x 33 tile in the same memory, read back a row at a time, lane = column
 template <int N> struct PgStage {
     const CUtensorMap *map;
     uint32_t base;
-    int at, lane;
-    __device__ __forceinline__ uint32_t begin()
+    int lane;
+    __device__ __forceinline__ uint32_t piece(int i) const { return base + i * kPgStageBytes; }
+    // the pieces sent last have been read
+    __device__ __forceinline__ void begin() const
     {
-        if (lane == 0) tma_store_wait_read<N - 1>();
+        if (lane == 0) tma_store_wait_read<0>();
         __syncwarp();
-        return base + at * kPgStageBytes;
-    }
-    __device__ __forceinline__ void send(int x, int y, int z)
-    {
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) {
-            tma_store_3d(map, base + at * kPgStageBytes, x, y, z);
-            tma_store_commit();
-        }
-        at = at + 1 == N ? 0 : at + 1;
     }
     // 16 packed words: this lane's row of 32 values
-    __device__ __forceinline__ void row(uint32_t buf, const uint32_t (&w)[16]) const
+    __device__ __forceinline__ void row(int i, const uint32_t (&w)[16]) const
     {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)), "r"(w[4 * j]), "r"(w[4 * j + 1]),
-                         "r"(w[4 * j + 2]), "r"(w[4 * j + 3])
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(piece(i) + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)), "r"(w[4 * j]),
+                         "r"(w[4 * j + 1]), "r"(w[4 * j + 2]), "r"(w[4 * j + 3])
                          : "memory");
     }
-    // the same as a column
-    __device__ __forceinline__ void column(uint32_t buf, const uint32_t (&w)[16]) const
+    // piece `to` = piece `from` transposed, 8 x 8 blocks at a time (after a __syncwarp)
+    __device__ __forceinline__ void transpose(int from, int to) const
     {
+        const int i = lane, r = lane & 7, blk = lane >> 3;
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-            asm volatile("st.shared.b16 [%0], %1;" ::"r"(buf + j * 64 + (((lane >> 3) ^ ((j >> 1) & 3)) << 4) + (lane & 7) * 2),
-                         "h"((uint16_t)(w[j / 2] >> (j % 2 * 16)))
-                         : "memory");
+        for (int j = 0; j < 4; ++j) {
+            uint32_t m[4];
+            ldm4t(m, piece(from) + i * 64 + ((j ^ ((i >> 1) & 3)) << 4));                         // blocks (0 .. 3, j)
+            const int o = 8 * j + r;
+            stm4(piece(to) + o * 64 + ((blk ^ ((o >> 1) & 3)) << 4), m);                          // blocks (j, 0 .. 3)
+        }
+    }
+    // everything written is visible to TMA; then lane 0 sends pieces and closes the group
+    __device__ __forceinline__ void ready() const
+    {
+        fence_proxy_async_smem();
+        __syncwarp();
+    }
+    __device__ __forceinline__ void send(int i, int x, int y, int z) const
+    {
+        if (lane == 0) tma_store_3d(map, piece(i), x, y, z);
+    }
+    __device__ __forceinline__ void close() const
+    {
+        if (lane == 0) tma_store_commit();
+    }
+    // f(row, value of column `lane` in that row, old(row)) for 32 rows, eight `old` at a time before the first of their `f`; N >= 3
+    template <class G, class F> __device__ __forceinline__ void rows(const float (&v)[32], G old, F f) const
+    {
+        static_assert(N * kPgStageBytes >= 32 * 33 * 4, "a 32 x 33 tile of floats");
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 32; ++j) asm volatile("st.shared.f32 [%0], %1;" ::"r"(base + (lane * 33 + j) * 4), "f"(v[j]) : "memory");
+        __syncwarp();
+#pragma unroll 1
+        for (int r0 = 0; r0 < 32; r0 += 8) {
+            float w[8], x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) w[k] = old(r0 + k);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[k]) : "r"(base + ((r0 + k) * 33 + lane) * 4) : "memory");
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f(r0 + k, x[k], w[k]);
+        }
     }
 };
 
@@ -197,6 +238,17 @@ struct PgBars {
     uint64_t full[kPgMaxSlots], empty[kPgMaxSlots];                           // full: used in the even CTA only
     uint64_t acc_full[2], acc_empty[2];
 };
+
+// A wait whose common case is one instruction, the rest out of line: these kernels are often launched for one tile per pair, and
+// what they have not executed before has to be fetched first.
+static __device__ __noinline__ bool pg_wait_on(uint32_t bar, uint32_t parity, unsigned *status, volatile int *dead, unsigned code)
+{
+    return mbar_wait<true>(bar, parity, status, dead, code);
+}
+__device__ __forceinline__ bool pg_wait(uint32_t bar, uint32_t parity, unsigned *status, volatile int *dead, unsigned code)
+{
+    return mbar_try_wait_cluster_acquire(bar, parity) || pg_wait_on(bar, parity, status, dead, code);
+}
 
 // Epi: struct with  begin(const Epi::Args &, const PgTile &),  chunk(args, tile, c, float (&v)[32], stage)  for c = 0, 32, .. < tn / 2,
 // end(args, tile); kStage: pieces in `stage`, its warp's PgStage (0: none).  PROMOTE: at most p.seg chunks are accumulated in tensor memory, sums of those in fp32 registers.
@@ -310,7 +362,7 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
                     const int ka = p.a_k0 + c * kPgChunk, kb = p.b_k0 + c * kPgChunk;
 #pragma unroll
                     for (int l = 0; l < kLoads; ++l) {
-                        if (!mbar_wait(empty0 + slot * 8, phase, p.status, dead, kErrSlotWait)) { ok = false; break; }
+                        if (!pg_wait(empty0 + slot * 8, phase, p.status, dead, kErrSlotWait)) { ok = false; break; }
                         const uint32_t dst = ring0 + slot * kPgSlotBytes, full = full0 + slot * 8;
                         constexpr int tag[6] = {pg_load(SCHEME, 0), pg_load(SCHEME, 1), pg_load(SCHEME, 2), pg_load(SCHEME, 3),
                                                 pg_load(SCHEME, 4), pg_load(SCHEME, 5)};
@@ -354,7 +406,7 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
                 for (int c0 = at.c0; ok && c0 < at.c1; c0 = (at.c1 - c0 > seg) ? c0 + seg : at.c1, ++it) {
                     const int c1 = (at.c1 - c0 > seg) ? c0 + seg : at.c1;
                     const uint32_t buf = it & 1;
-                    if (!mbar_wait<true>(acce0 + buf * 8, ((it >> 1) & 1) ^ 1, p.status, dead, kErrTmemWait)) { ok = false; break; }
+                    if (!pg_wait(acce0 + buf * 8, ((it >> 1) & 1) ^ 1, p.status, dead, kErrTmemWait)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t d = tmem_base + buf * 256;
                     for (int c = c0; ok && c < c1; ++c) {
@@ -362,7 +414,7 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
 #pragma unroll
                         for (int l = 0; l < kLoads; ++l) {
                             at_slot[l] = slot;
-                            if (!mbar_wait<true>(full0 + slot * 8, phase, p.status, dead, kErrTmaWait)) { ok = false; break; }
+                            if (!pg_wait(full0 + slot * 8, phase, p.status, dead, kErrTmaWait)) { ok = false; break; }
                             if (++slot == kPgSlots) { slot = 0; phase ^= 1; }
                             tc_fence_after();
 #pragma unroll
@@ -390,7 +442,7 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
         const uint32_t lane_base = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)((warp >> 2) * (tn / 2));
         uint32_t it = 0;
         bool ok = true;
-        PgStage<(Epi::kStage > 0 ? Epi::kStage : 1)> stage = {&tm_c, ring0 + kPgSlots * kPgSlotBytes + warp * Epi::kStage * kPgStageBytes, 0, lane};
+        PgStage<(Epi::kStage > 0 ? Epi::kStage : 1)> stage = {&tm_c, ring0 + kPgSlots * kPgSlotBytes + warp * Epi::kStage * kPgStageBytes, lane};
         for (long long tile = pair; ok && tile < total; tile += npairs) {
             const At at = locate(tile);
             PgTile t;
@@ -405,13 +457,12 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
             if constexpr (!PROMOTE) {
                 uint32_t buf = it & 1;
                 if (!t.zero) {
-                    if (!mbar_wait(accf0 + buf * 8, (it >> 1) & 1, p.status, dead, kErrMmaWait)) { ok = false; break; }
+                    if (!pg_wait(accf0 + buf * 8, (it >> 1) & 1, p.status, dead, kErrMmaWait)) { ok = false; break; }
                     tc_fence_after();
                     ++it;
                 }
-#pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    if (h * 64 >= tn) break;
+#pragma unroll 1
+                for (int h = 0; h * 64 < tn; ++h) {
                     float v[32];
                     if (!t.zero) {
                         tmem_ld32(lane_base + buf * 256 + h * 32, v);
@@ -434,24 +485,33 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
                     for (int i = 0; i < 32; ++i) acc[h][i] = 0.0f;
                 for (int c0 = at.c0; c0 < at.c1; c0 = (at.c1 - c0 > seg) ? c0 + seg : at.c1, ++it) {
                     const uint32_t buf = it & 1;
-                    if (!mbar_wait(accf0 + buf * 8, (it >> 1) & 1, p.status, dead, kErrMmaWait)) { ok = false; break; }
+                    if (!pg_wait(accf0 + buf * 8, (it >> 1) & 1, p.status, dead, kErrMmaWait)) { ok = false; break; }
                     tc_fence_after();
 #pragma unroll
                     for (int h = 0; h < 4; ++h) {
                         if (h * 64 >= tn) break;
-                        float v[32];
-                        tmem_ld32(lane_base + buf * 256 + h * 32, v);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) acc[h][i] += v[i];
+                        for (int g = 0; g < 32; g += 16) {                    // 16 at a time: registers
+                            float v[16];
+                            tmem_ask16(lane_base + buf * 256 + h * 32 + g, v);
+                            tmem_ready(v);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) acc[h][g + i] += v[i];
+                        }
                     }
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive_remote(acce_leader + buf * 8);
                 }
                 if (!ok) break;
+                // one copy of the conversion, the columns moved up to it: a launch of one tile per pair runs this code once, and most
+                // of the time of four copies went into fetching them (2 us for 32 columns)
+#pragma unroll 1
+                for (int h = 0; h * 64 < tn; ++h) {
+                    e.chunk(args, t, h * 32, acc[0], stage);
 #pragma unroll
-                for (int h = 0; h < 4; ++h)
-                    if (h * 64 < tn) e.chunk(args, t, h * 32, acc[h], stage);
+                    for (int i = 0; i < 32; ++i) { acc[0][i] = acc[1][i]; acc[1][i] = acc[2][i]; acc[2][i] = acc[3][i]; }
+                }
             }
             e.end(args, t);
         }

@@ -2,12 +2,14 @@
  * ctypes.  A call on a few tokens takes the GPU 5 to 10 us, and ctypes with the checks written in Python took the host
  * 6 to 7 us of every call (4 attribute reads per tensor, 11 to 22 argument conversions); this takes about 1 us.
  *
- * Call(name, address, spec, names, float_types, on_error, stream_of) is a callable object.  spec has one letter per
+ * Call(name, address, spec, names, float_types, on_error, stream_of, sizes, device_of) is a callable object.  spec has one letter per
  * positional argument, in the order of the C function's parameters:
  *   t  tensor of the storage dtype (the first one decides which)      f  float32 tensor       q  int64 tensor
  *   i  integer     d  float (double)     w  workspace: object with ptr and nbytes, or (ptr, nbytes); two C parameters
  *   v  workspace pointer, or None     s  stream: None (the current one), an integer, or an object with cuda_stream
  *   D  (no argument) the dtype code
+ * sizes is None, or for each argument a tuple of the positions of up to three integer arguments (none: an empty tuple): a tensor
+ * has to have at least their product of values, and to be on the device that device_of() says is the current one.
  * None as a tensor is a null pointer.  A non-zero status is given to on_error(status, name). */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -71,9 +73,11 @@ typedef struct {
     char spec[MAX_ARGS];
     int n_spec, n_args;
     PyObject *name, *names, *types, *on_error, *stream_of;   /* types: (float32, bfloat16, int64) */
+    PyObject *device_of;                                     /* null: sizes are not checked */
+    signed char need[MAX_ARGS][3];                           /* positions of the factors, -1: no more; first -2: not checked */
 } Call;
 
-static PyObject *s_is_cuda, *s_is_contiguous, *s_dtype, *s_data_ptr, *s_ptr, *s_nbytes, *s_cuda_stream;
+static PyObject *s_is_cuda, *s_is_contiguous, *s_dtype, *s_data_ptr, *s_ptr, *s_nbytes, *s_cuda_stream, *s_numel, *s_get_device;
 
 static int to_u64(PyObject *o, uint64_t *out)
 {
@@ -145,12 +149,56 @@ static int workspace_of(PyObject *w, uint64_t *ptr, uint64_t *bytes)
     return attr_u64(w, s_ptr, ptr) || attr_u64(w, s_nbytes, bytes) ? -1 : 0;
 }
 
+static int method_i64(PyObject *o, PyObject *method, long long *out)
+{
+    PyObject *v = PyObject_CallMethodNoArgs(o, method);
+    if (v == NULL) return -1;
+    *out = PyLong_AsLongLong(v);
+    Py_DECREF(v);
+    return *out == -1 && PyErr_Occurred() ? -1 : 0;
+}
+
+/* every tensor is large enough for what the integer arguments say, and on the current device */
+static int check_sizes(Call *c, PyObject *const *args)
+{
+    long long device = 0;
+    PyObject *v = PyObject_CallNoArgs(c->device_of);
+    if (v == NULL) return -1;
+    device = PyLong_AsLongLong(v);
+    Py_DECREF(v);
+    if (device == -1 && PyErr_Occurred()) return -1;
+    for (int i = 0; i < c->n_args; ++i) {
+        if (c->need[i][0] == -2 || args[i] == Py_None) continue;
+        unsigned long long n = 1;
+        for (int k = 0; k < 3 && c->need[i][k] >= 0; ++k) {
+            uint64_t f;
+            if (to_u64(args[(int)c->need[i][k]], &f)) return -1;
+            if ((int64_t)f < 0) { n = 0; break; }                    /* the call itself refuses it */
+            if (__builtin_mul_overflow(n, (unsigned long long)f, &n)) n = ~0ull;
+        }
+        long long have, at;
+        if (method_i64(args[i], s_numel, &have)) return -1;
+        PyObject *name = PyTuple_GET_ITEM(c->names, i);
+        if ((unsigned long long)have < n) {
+            PyErr_Format(PyExc_ValueError, "%U: %U must have at least %llu values, got %lld", c->name, name, n, have);
+            return -1;
+        }
+        if (method_i64(args[i], s_get_device, &at)) return -1;
+        if (at >= 0 && at != device) {
+            PyErr_Format(PyExc_ValueError, "%U: %U is on device %lld, the current one is %lld", c->name, name, at, device);
+            return -1;
+        }
+    }
+    return 0;
+}
+
 static PyObject *call_it(PyObject *self, PyObject *const *args, size_t nargsf, PyObject *kw)
 {
     Call *c = (Call *)self;
     const Py_ssize_t n = PyVectorcall_NARGS(nargsf);
     if (n != c->n_args || (kw != NULL && PyTuple_GET_SIZE(kw) != 0))
         return PyErr_Format(PyExc_TypeError, "%U takes %d positional arguments (%zd given)", c->name, c->n_args, n);
+    if (c->device_of != NULL && check_sizes(c, args)) return NULL;
     uint64_t a[MAX_ARGS], ignored;
     PyObject *storage = NULL;
     int code = 0, out = 0, in = 0, dtype_at = -1;
@@ -199,12 +247,13 @@ static PyObject *call_it(PyObject *self, PyObject *const *args, size_t nargsf, P
 
 static PyObject *call_new(PyTypeObject *type, PyObject *args, PyObject *kw)
 {
-    PyObject *name, *names, *types, *on_error, *stream_of;
+    PyObject *name, *names, *types, *on_error, *stream_of, *sizes, *device_of;
     unsigned long long fn;
     const char *spec;
     Py_ssize_t len;
     if (kw != NULL && PyDict_GET_SIZE(kw) != 0) { PyErr_SetString(PyExc_TypeError, "Call takes no keywords"); return NULL; }
-    if (!PyArg_ParseTuple(args, "UKs#O!O!OO", &name, &fn, &spec, &len, &PyTuple_Type, &names, &PyTuple_Type, &types, &on_error, &stream_of))
+    if (!PyArg_ParseTuple(args, "UKs#O!O!OOOO", &name, &fn, &spec, &len, &PyTuple_Type, &names, &PyTuple_Type, &types, &on_error, &stream_of, &sizes,
+                          &device_of))
         return NULL;
     if (len > MAX_ARGS || PyTuple_GET_SIZE(types) != 3) { PyErr_SetString(PyExc_ValueError, "bad spec"); return NULL; }
     int n_args = 0, params = 0;
@@ -217,8 +266,20 @@ static PyObject *call_new(PyTypeObject *type, PyObject *args, PyObject *kw)
     for (size_t k = 0; k < sizeof(kCalls) / sizeof(kCalls[0]); ++k)
         if (PyUnicode_CompareWithASCIIString(name, kCalls[k].name) == 0 && kCalls[k].params == params) apply = kCalls[k].apply;
     if (apply == NULL || fn == 0 || PyTuple_GET_SIZE(names) != n_args) { PyErr_SetString(PyExc_ValueError, "spec does not fit the function"); return NULL; }
+    if (sizes != Py_None && (!PyTuple_Check(sizes) || PyTuple_GET_SIZE(sizes) != n_args)) { PyErr_SetString(PyExc_ValueError, "bad sizes"); return NULL; }
     Call *c = (Call *)type->tp_alloc(type, 0);
     if (c == NULL) return NULL;
+    for (int i = 0; sizes != Py_None && i < n_args; ++i) {
+        PyObject *t = PyTuple_GET_ITEM(sizes, i);
+        const Py_ssize_t n = PyTuple_Check(t) ? PyTuple_GET_SIZE(t) : 4;
+        c->need[i][0] = n == 0 ? -2 : -1;
+        for (Py_ssize_t k = 0; k < 3 && n <= 3; ++k) {
+            const long at = k < n ? PyLong_AsLong(PyTuple_GET_ITEM(t, k)) : -1;
+            if (k < n) c->need[i][k] = at >= 0 && at < n_args ? (signed char)at : -1;
+            else if (k > 0) c->need[i][k] = -1;
+        }
+    }
+    c->device_of = sizes != Py_None ? Py_NewRef(device_of) : NULL;
     c->vectorcall = call_it;
     c->fn = (void *)(uintptr_t)fn;
     c->apply = apply;
@@ -241,6 +302,7 @@ static void call_dealloc(PyObject *self)
     Py_XDECREF(c->types);
     Py_XDECREF(c->on_error);
     Py_XDECREF(c->stream_of);
+    Py_XDECREF(c->device_of);
     Py_TYPE(self)->tp_free(self);
 }
 
@@ -267,6 +329,8 @@ PyMODINIT_FUNC PyInit__pycalls(void)
     s_ptr = PyUnicode_InternFromString("ptr");
     s_nbytes = PyUnicode_InternFromString("nbytes");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
+    s_numel = PyUnicode_InternFromString("numel");
+    s_get_device = PyUnicode_InternFromString("get_device");
     PyObject *m = PyModule_Create(&module);
     if (m == NULL || PyModule_AddObjectRef(m, "Call", (PyObject *)&CallType) < 0) return NULL;
     return m;

@@ -234,7 +234,7 @@ struct EpiStats {
 
 // g of a piece of the vocabulary; zeros behind the last row and the last column
 template <int PL> struct EpiGrad {
-    static constexpr int kStage = 2;
+    static constexpr int kStage = PL;
     struct Args {
         int cols, v0;
         const int *tgt, *count;
@@ -260,6 +260,7 @@ template <int PL> struct EpiGrad {
             const float e = ex2(fmaf(v[i], kLog2e, -r_hi) - r_lo);
             v[i] = i >= left ? 0.0f : dl * (at == i ? e - 1.0f : e);
         }
+        st.begin();
 #pragma unroll
         for (int q = 0; q < PL; ++q) {
             uint32_t w[16];
@@ -271,9 +272,12 @@ template <int PL> struct EpiGrad {
                     v[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
                 }
             }
-            st.row(st.begin(), w);
-            st.send(t.col + c, t.row & ~31, q);
+            st.row(q, w);
         }
+        st.ready();
+#pragma unroll
+        for (int q = 0; q < PL; ++q) st.send(q, t.col + c, t.row & ~31, q);
+        st.close();
     }
     __device__ __forceinline__ void end(const Args &, const PgTile &) {}
 };
@@ -413,12 +417,27 @@ __global__ void __launch_bounds__(256) xent_dx_kernel(const float *__restrict__ 
     depend_wait();
     depend_launch();
     const int n = *count, parts = *splits;
-    for (int row = blockIdx.x * 8 + (threadIdx.x >> 5); row < n; row += gridDim.x * 8) {
-        T *out = dx + (size_t)map[row] * d;
+    // four columns at a time where rows allow it, a thread each
+    const bool four = d % 4 == 0;
+    const int per = four ? d / 4 : d;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)n * per; i += (long long)gridDim.x * 256) {
+        const int row = (int)(i / per), c = (int)(i - (long long)row * per);
         const float *in = acc + (size_t)row * d;
-        for (int c = threadIdx.x & 31; c < d; c += 32) {
+        T *out = dx + (size_t)map[row] * d;
+        if (four) {
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+            for (int q = 0; q < parts; ++q) {
+                const float4 w = *reinterpret_cast<const float4 *>(in + q * part + 4 * c);
+                v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+            }
+            if constexpr (sizeof(T) == 2)
+                *reinterpret_cast<uint2 *>(out + 4 * c) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+            else
+                *reinterpret_cast<float4 *>(out + 4 * c) = v;
+        } else {
             float v = 0.0f;
-#pragma unroll 4
+#pragma unroll 8
             for (int q = 0; q < parts; ++q) v += in[q * part + c];
             elem<T>::store(out + c, v);
         }
@@ -946,7 +965,8 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
         }
     }
     if (l.dx_parts > 1) {
-        const int ctas = ceil_div(tokens, 8) < 148 * 8 ? ceil_div(tokens, 8) : 148 * 8;
+        const int64_t want = (tokens * d / (d % 4 == 0 ? 4 : 1) + 255) / 256;
+        const int ctas = (int)(want < 148 * 8 ? want : 148 * 8);
         return launch_serialized(xent_dx_kernel<T>, dim3((unsigned)ctas), 256, 0, s, (const float *)acc, (size_t)tokens * d, (const int *)splits, map, count, dx, d);
     }
     return MONARCH_OK;
