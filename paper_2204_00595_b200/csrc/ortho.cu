@@ -742,13 +742,22 @@ __global__ void __launch_bounds__(kTcThreads, 1) ortho_tc_kernel(const Io<T> io,
 }
 
 // ------------------------------------------------------------------------------------------------ larger blocks
-// Three products a step on plane_gemm.cuh (CTA pairs, tcgen05), with the square completed so that each needs its operands alone:
+// Three products a step, with the square completed so that each needs its operands alone:
 //   S~ = X X^T + beta I,   P = c S~ S~^T + (a - c beta^2) I = a I + b S + c S^2,   X <- P X,      beta = b / 2c
 // (X^T X and X P where rows > cols).  An error of P counts against its eigenvalues, 0.64 to 3.44; that b S comes out of a difference
-// costs nothing there.  S~, P and X exist only as planes; an epilogue turns its accumulator into the next operand's planes, the last
-// one into the caller's result.  S~ and P are symmetric: only the blocks of 256 columns up to the diagonal are computed, each tile
-// below it is written transposed as well.  Products of fewer tiles than there are CTA pairs are split along K, in which case a launch
-// adds the parts and does the same.
+// costs nothing there.  S~, P and X exist only as bf16 planes in memory.  S~ and P are symmetric: only the blocks of 256 columns up
+// to the diagonal are computed, each tile below it is written transposed as well.
+//
+// ONE launch does all products of all steps on the CTA pairs of plane_gemm.cuh (256 x tn tiles, a ring of operand tiles, two
+// accumulators, the epilogue in eight warps).  The tiles of all products form one list, step by step, product by product, block by
+// block; pair i takes tiles i, i + pairs, ..  A tile's loader waits until the product before it in its block is complete (a counter
+// per block that every epilogue warp adds to when its stores have landed); the tiles of other blocks fill the time.  The launch is
+// cooperative: all CTAs are resident, and a tile only ever waits for tiles before it in the list.  As fifteen launches each product
+// cost 8 to 11 us beside its MMAs: code and tensor maps fetched anew, the pipeline filled and drained (4 blocks of 1024 x 1024, bf16:
+// 446 us).
+// A product of fewer tiles than there are pairs is cut along K as well: the parts' sums go to memory, and when all parts of a tile
+// are there, each pair that made one adds up some of its columns, always in the same order (all of them added up by the last to
+// finish: 112 us a step for one 1024 x 1024 block in bf16).
 constexpr float kBeta = kB / (2.0f * kC), kGamma = kA - kC * kBeta * kBeta;
 constexpr int kNormParts = 256;
 
@@ -785,182 +794,359 @@ struct Planes {
     }
 };
 
-enum Role { kRoleS = 0, kRoleP = 1, kRoleX = 2, kRoleOut = 3 };
+// ---- the products
+struct Product {
+    int rows, cols, kchunks;
+    int a_mn, b_mn;                // operands stored with K along their rows
+    int tn, sub, lower;            // columns of a tile; tiles in 256 columns; symmetric result
+    int mtiles, ntiles, tiles;     // of a block
+    int splits, per_split;         // parts of K, chunks in one
+    int publishers;                // warps that publish something of a tile
+    float scale, diagonal;         // of the result
+    unsigned *parts_done;          // [blocks][tiles][16 warps], where splits > 1
+};
 
-// what becomes of a sum at (row, col)
-template <int ROLE> __device__ __forceinline__ float finished(float v, int row, int col)
+struct alignas(64) OrthoMaps {
+    CUtensorMap s_a[2], s_b[2], p_a, p_b, x_a[2], x_b[2], s_to, p_to, x_to[2];            // [2]: by the X that is read (s, x_a, x_b), written (x_to)
+};
+
+struct OrthoRun {
+    unsigned *status, *done;       // done: [blocks]
+    Product prod[3];
+    int blocks, steps;
+    int rows, cols;                // of a block
+    float *part;                   // [blocks][part_units: tiles, splits][16 warps][128][32 lanes]; a block's place serves its products in turn
+    int64_t part_units;
+};
+
+constexpr int kRunStage = 3, kRunSlots = pg_slots(kRunStage), kRunSmem = pg_smem(kRunStage);
+
+__device__ __forceinline__ unsigned ld_acquire(const unsigned *p)
 {
-    if (ROLE == kRoleS) return row == col ? v + kBeta : v;
-    if (ROLE == kRoleP) return row == col ? fmaf(kC, v, kGamma) : kC * v;
+    unsigned v;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
     return v;
 }
-
-template <typename T, int PL, int ROLE> struct EpiPlanes {
-    static constexpr int kStage = ROLE == kRoleOut ? 3 : ROLE == kRoleX ? PL : 4;            // S, P: a plane and its transpose, twice
-    struct Args {
-        Planes to;                 // also the sizes of the result
-        Io<T> io;                  // kRoleOut
-    };
-    __device__ __forceinline__ void begin(const Args &, const PgTile &) {}
-    template <class Stage> __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], Stage &st)
-    {
-        const Planes &m = a.to;
-        const int col = t.col + c, row0 = t.row & ~31;
-        if (row0 >= m.rows || col >= m.cols) return;                           // the same in all lanes; TMA clips the rest
-        if constexpr (ROLE == kRoleOut) {
-            const size_t at = ((size_t)t.z * m.rows + row0) * m.cols + col + st.lane;
-            const int rows = col + st.lane < m.cols ? m.rows - row0 : 0;
-            st.rows(
-                v, [&](int r) { return r < rows ? a.io.old(at + (size_t)r * m.cols) : 0.0f; },
-                [&](int r, float x, float w) {
-                    if (r < rows) a.io.write(at + (size_t)r * m.cols, x, w);
-                });
-        } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = finished<ROLE>(v[i], t.row, col + i);
-            auto next_plane = [&](uint32_t (&w)[16]) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-                    v[2 * i] -= __uint_as_float(w[i] << 16);
-                    v[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
-                }
-            };
-            if constexpr (ROLE == kRoleX) {
-                st.begin();
-#pragma unroll
-                for (int q = 0; q < PL; ++q) {
-                    uint32_t w[16];
-                    next_plane(w);
-                    st.row(q, w);
-                }
-                st.ready();
-#pragma unroll
-                for (int q = 0; q < PL; ++q) st.send(q, col, row0, t.z * PL + q);
-                st.close();
-            } else {
-                // two planes behind one fence, then the third (fp32): more pieces would be taken from the operands' ring
-#pragma unroll
-                for (int q0 = 0; q0 < PL; q0 += 2) {
-                    st.begin();
-#pragma unroll
-                    for (int q = q0; q < q0 + 2 && q < PL; ++q) {
-                        uint32_t w[16];
-                        next_plane(w);
-                        st.row(q - q0, w);
-                    }
-                    if (t.mirror) {
-                        __syncwarp();
-#pragma unroll
-                        for (int q = q0; q < q0 + 2 && q < PL; ++q) st.transpose(q - q0, 2 + q - q0);
-                    }
-                    st.ready();
-#pragma unroll
-                    for (int q = q0; q < q0 + 2 && q < PL; ++q) {
-                        st.send(q - q0, col, row0, t.z * PL + q);
-                        if (t.mirror) st.send(2 + q - q0, row0, col, t.z * PL + q);
-                    }
-                    st.close();
-                }
-            }
-        }
-    }
-    __device__ __forceinline__ void end(const Args &, const PgTile &) {}
-};
-
-// a part of K, float32
-struct EpiPart {
-    static constexpr int kStage = 3;
-    struct Args {
-        float *out;                // [blocks][splits][rows][cols]
-        int rows, cols;
-    };
-    __device__ __forceinline__ void begin(const Args &, const PgTile &) {}
-    template <class Stage> __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], Stage &st)
-    {
-        const int col = t.col + c, row0 = t.row & ~31;
-        if (row0 >= a.rows || col >= a.cols) return;
-        float *out = a.out + ((size_t)t.z * a.rows + row0) * a.cols + col + st.lane;
-        const int rows = col + st.lane < a.cols ? a.rows - row0 : 0;
-        st.rows(
-            v, [](int) { return 0.0f; },
-            [&](int r, float x, float) {
-                if (r < rows) out[(size_t)r * a.cols] = x;
-            });
-    }
-    __device__ __forceinline__ void end(const Args &, const PgTile &) {}
-};
-
-// The parts added up, and what the epilogues do.  Tiles of 32 x 32, for S~ and P those up to the diagonal, the ones off it written
-// transposed as well.
-template <typename T, int PL, int ROLE>
-__global__ void __launch_bounds__(256) finish_kernel(const float *__restrict__ part, int splits, const typename EpiPlanes<T, PL, ROLE>::Args a)
+// bounded wait until *ctr >= need; what its writers published may then be loaded by TMA
+__device__ __noinline__ bool wait_published(const unsigned *ctr, unsigned need, unsigned *status, volatile int *dead)
 {
-    __shared__ float tile[32][33];
-    constexpr bool kSym = ROLE == kRoleS || ROLE == kRoleP;
-    depend_wait();
-    depend_launch();
-    const Planes &m = a.to;
-    const int tr = (m.rows + 31) / 32, tc = (m.cols + 31) / 32, per = kSym ? tr * (tr + 1) / 2 : tr * tc;
-    const int block = blockIdx.x / per, t = blockIdx.x % per;
-    int I, J;
-    if (kSym) {
-        I = (int)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
-        while (I * (I + 1) / 2 > t) --I;
-        while ((I + 1) * (I + 2) / 2 <= t) ++I;
-        J = t - I * (I + 1) / 2;
-    } else {
-        I = t / tc;
-        J = t % tc;
-    }
-    const size_t size = (size_t)m.rows * m.cols;
-    const float *from = part + (size_t)block * splits * size;
-    const int lr = threadIdx.x >> 3, lc = (threadIdx.x & 7) * 4, r = I * 32 + lr, c = J * 32 + lc;
-    float v[4] = {};
-    if (r < m.rows && c < m.cols) {
-        const size_t at = (size_t)r * m.cols + c;
-        if (m.cols % 4 == 0) {
-#pragma unroll 8
-            for (int s = 0; s < splits; ++s) {
-                const float4 q = *reinterpret_cast<const float4 *>(from + s * size + at);
-                v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w;
+    if (ld_acquire(ctr) < need) {
+        const unsigned long long t0 = global_timer_ns(), limit = wait_limit_ns(status);
+        while (ld_acquire(ctr) < need) {
+            if (*dead || global_timer_ns() - t0 > limit) {
+                *dead = 1;
+                atomicCAS(status, 0u, (unsigned)kErrPeerWait);
+                return false;
             }
-        } else {
-            for (int s = 0; s < splits; ++s)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (c + e < m.cols) v[e] += from[s * size + at + e];
+            __nanosleep(32);
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            v[e] = finished<ROLE>(v[e], r, c + e);
-            if (c + e >= m.cols) break;
-            if (ROLE == kRoleOut) {
-                const size_t i = (size_t)block * size + at + e;
-                a.io.write(i, v[e], a.io.old(i));
-            }
-        }
-        // four columns or what is left of the row's multiple of sixteen: the columns behind the last are never read
-        if (ROLE != kRoleOut) put_planes4<PL>(m.template element<PL>(block, r, c), m.plane(), v);
     }
-    if (!kSym || I == J) return;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) tile[lr][lc + e] = v[e];
-    __syncthreads();
-    const int rr = J * 32 + lr, cc = I * 32 + lc;                            // of the transposed tile
-    if (rr < m.rows && cc < m.cols) {
-        const float w[4] = {tile[lc][lr], tile[lc + 1][lr], tile[lc + 2][lr], tile[lc + 3][lr]};
-        put_planes4<PL>(m.template element<PL>(block, rr, cc), m.plane(), w);
-    }
+    asm volatile("fence.proxy.async.global;" ::: "memory");
+    return true;
 }
 
-// sums of squares of `parts` parts of each block, and the new momentum
+struct Tile {
+    int step, ph, block, tile, split, mt, nt, c0, c1, mirror;
+};
+
+template <typename T, int PL, int SCHEME>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPgThreads, 1)
+ortho_run_kernel(const __grid_constant__ OrthoMaps maps, const __grid_constant__ OrthoRun p, const Io<T> io)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) PgBars bars;
+    __shared__ uint32_t tmem_base_s;
+    __shared__ int dead_s;
+
+    const uint32_t ring0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+    volatile int *dead = &dead_s;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kRunSlots; ++s) {
+            mbar_init(smem_u32(&bars.full[s]), 1);
+            mbar_init(smem_u32(&bars.empty[s]), 1);
+        }
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(smem_u32(&bars.acc_full[a]), 1);
+            mbar_init(smem_u32(&bars.acc_empty[a]), 2 * kPgEpiWarps);
+        }
+        fence_mbar_init();
+        dead_s = 0;
+    }
+    if (warp == 0) {
+        tmem_alloc_pair(smem_u32(&tmem_base_s), 512);
+        tmem_relinquish_pair();
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_arrive_release();
+    cluster_wait_acquire();
+    tc_fence_after();
+    const uint32_t tmem_base = __shfl_sync(~0u, tmem_base_s, 0);
+    const uint32_t full0 = smem_u32(bars.full), empty0 = smem_u32(bars.empty);
+    const uint32_t accf0 = smem_u32(bars.acc_full), acce0 = smem_u32(bars.acc_empty);
+    constexpr int kLoads = pg_loads(SCHEME), kSeg = SCHEME == kP3x3 ? pg_seg(SCHEME) : 16;            // bf16 results: 192 steps
+
+    const int u0 = p.prod[0].tiles * p.prod[0].splits, u1 = p.prod[1].tiles * p.prod[1].splits, u2 = p.prod[2].tiles * p.prod[2].splits;
+    const long long per_step = (long long)p.blocks * (u0 + u1 + u2), total = per_step * p.steps;
+    auto locate = [&](long long g) {
+        Tile t;
+        t.step = (int)(g / per_step);
+        long long r = g - t.step * per_step;
+        t.ph = 0;
+        int u = u0;
+        if (r >= (long long)p.blocks * u0) { r -= (long long)p.blocks * u0; t.ph = 1; u = u1; }
+        if (t.ph == 1 && r >= (long long)p.blocks * u1) { r -= (long long)p.blocks * u1; t.ph = 2; u = u2; }
+        const Product &q = p.prod[t.ph];
+        t.block = (int)(r / u);
+        const int v = (int)(r - (long long)t.block * u);
+        t.tile = v / q.splits;
+        t.split = v - t.tile * q.splits;
+        t.mirror = 0;
+        if (q.lower) {
+            const int w = t.tile / q.sub;
+            int m = (int)((sqrtf(8.0f * (float)w + 1.0f) - 1.0f) * 0.5f);
+            while (m * (m + 1) / 2 > w) --m;
+            while ((m + 1) * (m + 2) / 2 <= w) ++m;
+            const int n = w - m * (m + 1) / 2;
+            t.mt = m;
+            t.nt = n * q.sub + t.tile % q.sub;
+            t.mirror = n < m;
+        } else {
+            t.mt = t.tile / q.ntiles;
+            t.nt = t.tile - t.mt * q.ntiles;
+        }
+        t.c0 = min(t.split * q.per_split, q.kchunks);
+        t.c1 = min(t.c0 + q.per_split, q.kchunks);
+        return t;
+    };
+
+    if (warp == 8) {
+        // ------------------------------------------------------------ loader (both CTAs)
+        if (elect_one()) {
+            uint32_t slot = 0, phase = 1;
+            bool ok = true;
+            for (long long g = pair; ok && g < total; g += npairs) {
+                const Tile t = locate(g);
+                const Product &q = p.prod[t.ph];
+                // what the products before this one in its block have published
+                const unsigned of_s = p.prod[0].tiles * p.prod[0].publishers, of_p = p.prod[1].tiles * p.prod[1].publishers, of_x = p.prod[2].tiles * p.prod[2].publishers;
+                const unsigned need = (unsigned)t.step * (of_s + of_p + of_x) + (t.ph > 0 ? of_s : 0) + (t.ph > 1 ? of_p : 0);
+                if (!wait_published(p.done + t.block, need, p.status, dead)) break;
+                const int at = t.step & 1, m0 = t.mt * kPgTile + (int)rank * 128, n0 = t.nt * q.tn + (int)rank * (q.tn / 2);
+                const CUtensorMap *ma = t.ph == 0 ? &maps.s_a[at] : t.ph == 1 ? &maps.p_a : &maps.x_a[at];
+                const CUtensorMap *mb = t.ph == 0 ? &maps.s_b[at] : t.ph == 1 ? &maps.p_b : &maps.x_b[at];
+                for (int c = t.c0; ok && c < t.c1; ++c) {
+                    const int k0 = c * kPgChunk;
+#pragma unroll
+                    for (int l = 0; l < kLoads; ++l) {
+                        if (!pg_wait(empty0 + slot * 8, phase, p.status, dead, kErrSlotWait)) { ok = false; break; }
+                        const uint32_t dst = ring0 + slot * kPgSlotBytes, full = full0 + slot * 8;
+                        constexpr int tag[6] = {pg_load(SCHEME, 0), pg_load(SCHEME, 1), pg_load(SCHEME, 2), pg_load(SCHEME, 3),
+                                                pg_load(SCHEME, 4), pg_load(SCHEME, 5)};
+                        const bool second = tag[l] & 4;
+                        const int z = t.block * PL + (tag[l] & 3), mn = second ? q.b_mn : q.a_mn, r0 = second ? n0 : m0;
+                        const CUtensorMap *m = second ? mb : ma;
+                        if (rank == 0) mbar_expect_tx(full, second ? q.tn * (kPgChunk * 2) : 2 * kPgSlotBytes);
+                        tma_load_3d_pair(dst, m, mn ? r0 : k0, mn ? k0 : r0, z, full);
+                        if (mn && (!second || q.tn == 256)) tma_load_3d_pair(dst + 8192, m, r0 + 64, k0, z, full);
+                        if (++slot == kRunSlots) { slot = 0; phase ^= 1; }
+                    }
+                }
+            }
+            let_copies_land(dead);
+        }
+    } else if (warp == 9) {
+        if (rank == 0 && elect_one()) {
+            // ------------------------------------------------------------ even CTA: MMA issuer for the pair
+            uint32_t slot = 0, phase = 0, it = 0;
+            bool ok = true;
+            for (long long g = pair; ok && g < total; g += npairs) {
+                const Tile t = locate(g);
+                const Product &q = p.prod[t.ph];
+                const uint32_t idesc = make_idesc_bf16(256, q.tn, q.a_mn, q.b_mn), astep = q.a_mn ? 128 : 2, bstep = q.b_mn ? 128 : 2;
+                const uint64_t adesc = make_smem_desc(0, q.a_mn ? 8192 : 16, 1024, kSwizzle128), bdesc = make_smem_desc(0, q.b_mn ? 8192 : 16, 1024, kSwizzle128);
+                for (int c0 = t.c0; ok && c0 < t.c1; c0 += kSeg, ++it) {
+                    const int c1 = min(c0 + kSeg, t.c1);
+                    const uint32_t buf = it & 1;
+                    if (!pg_wait(acce0 + buf * 8, ((it >> 1) & 1) ^ 1, p.status, dead, kErrTmemWait)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t d = tmem_base + buf * 256;
+                    for (int c = c0; ok && c < c1; ++c) {
+                        uint32_t at_slot[kLoads];
+#pragma unroll
+                        for (int l = 0; l < kLoads; ++l) {
+                            at_slot[l] = slot;
+                            if (!pg_wait(full0 + slot * 8, phase, p.status, dead, kErrTmaWait)) { ok = false; break; }
+                            if (++slot == kRunSlots) { slot = 0; phase ^= 1; }
+                            tc_fence_after();
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const int w = pg_mma(SCHEME, l, i);
+                                if (w == 0xff) continue;
+                                const uint64_t ad = adesc | (uint64_t)((ring0 + at_slot[w & 15] * kPgSlotBytes) >> 4);
+                                const uint64_t bd = bdesc | (uint64_t)((ring0 + at_slot[w >> 4] * kPgSlotBytes) >> 4);
+#pragma unroll
+                                for (int kk = 0; kk < 4; ++kk)
+                                    mma_f16_ss_pair(d, ad + astep * kk, bd + bstep * kk, idesc, (uint32_t)(c != c0 || l != 1 || kk != 0));
+                            }
+#pragma unroll
+                            for (int j = 0; j < kLoads; ++j)
+                                if ((pg_done(SCHEME, l) >> j) & 1) mma_commit_pair(empty0 + at_slot[j] * 8, 3);
+                        }
+                    }
+                    if (ok) mma_commit_pair(accf0 + buf * 8, 3);
+                }
+            }
+        }
+    } else {
+        // ------------------------------------------------------------ epilogue (both CTAs; own 128 rows)
+        const uint32_t acce_leader = map_to_cta(acce0, 0);
+        uint32_t it = 0;
+        bool ok = true;
+        PgStage<kRunStage> st = {nullptr, ring0 + kRunSlots * kPgSlotBytes + warp * kRunStage * kPgStageBytes, lane};
+        for (long long g = pair; ok && g < total; g += npairs) {
+            const Tile t = locate(g);
+            const Product &q = p.prod[t.ph];
+            const int tn = q.tn;
+            const uint32_t lane_base = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)((warp >> 2) * (tn / 2));
+            float acc[4][32];
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+#pragma unroll
+                for (int i = 0; i < 32; ++i) acc[h][i] = 0.0f;
+            for (int c0 = t.c0; c0 < t.c1; c0 += kSeg, ++it) {
+                const uint32_t buf = it & 1;
+                if (!pg_wait(accf0 + buf * 8, (it >> 1) & 1, p.status, dead, kErrMmaWait)) { ok = false; break; }
+                tc_fence_after();
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    if (h * 64 >= tn) break;
+#pragma unroll
+                    for (int j = 0; j < 32; j += 16) {
+                        float v[16];
+                        tmem_ask16(lane_base + buf * 256 + h * 32 + j, v);
+                        tmem_ready(v);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[h][j + i] += v[i];
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_remote(acce_leader + buf * 8);
+            }
+            if (!ok) break;
+            const int mine = (int)rank * 8 + warp;
+            const float *part = p.part + (((size_t)t.block * p.part_units + (size_t)t.tile * q.splits) * 16 + mine) * 4096 + lane;
+            if (q.splits > 1) {
+                float *to = const_cast<float *>(part) + (size_t)t.split * 16 * 4096;
+                unsigned *ctr = q.parts_done + ((size_t)t.block * q.tiles + t.tile) * 16 + mine;
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    if (h * 64 >= tn) break;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) __stcg(to + (h * 32 + i) * 32, acc[h][i]);
+                }
+                __threadfence();
+                __syncwarp();
+                if (lane == 0) atomicAdd(ctr, 1u);
+                if (t.split * 64 >= tn) continue;                              // more parts than groups of columns
+                if (lane == 0) ok = wait_published(ctr, (unsigned)q.splits * (unsigned)(t.step + 1), p.status, dead);
+                ok = __shfl_sync(~0u, ok, 0);
+                if (!ok) break;
+                __threadfence();
+            }
+            const int row0 = t.mt * kPgTile + (int)rank * 128 + (warp & 3) * 32, col0 = t.nt * tn + (warp >> 2) * (tn / 2);
+            const bool last = t.ph == 2 && t.step + 1 == p.steps;
+            st.map = t.ph == 0 ? &maps.s_to : t.ph == 1 ? &maps.p_to : &maps.x_to[(t.step & 1) ^ 1];
+            // one copy of the conversion, the columns moved up to it
+#pragma unroll 1
+            for (int h = q.splits > 1 ? t.split : 0; h * 64 < tn; h += q.splits) {
+                const int col = col0 + h * 32;
+                if (q.splits > 1) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) acc[0][i] = 0.0f;
+#pragma unroll 1
+                    for (int s = 0; s < q.splits; ++s)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) acc[0][i] += __ldcg(part + (size_t)s * 16 * 4096 + (h * 32 + i) * 32);
+                }
+                if (row0 < q.rows && col < q.cols) {                           // the same in all lanes; TMA clips the rest
+                    float (&v)[32] = acc[0];
+                    if (last) {
+                        const size_t at = ((size_t)t.block * p.rows + row0) * p.cols + col + lane;
+                        const int rows = col + lane < p.cols ? p.rows - row0 : 0;
+                        st.rows(
+                            v, [&](int r) { return r < rows ? io.old(at + (size_t)r * p.cols) : 0.0f; },
+                            [&](int r, float x, float w) {
+                                if (r < rows) io.write(at + (size_t)r * p.cols, x, w);
+                            });
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = row0 + lane == col + i ? fmaf(q.scale, v[i], q.diagonal) : q.scale * v[i];
+                        // all planes behind one fence, or a plane and its transpose at a time: there are three pieces (a fourth would
+                        // be a slot less for the operands: fp32 4096 x 4096 7 % slower)
+                        if (!t.mirror) st.begin();
+#pragma unroll
+                        for (int b = 0; b < PL; ++b) {
+                            uint32_t w[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+                                v[2 * i] -= __uint_as_float(w[i] << 16);
+                                v[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
+                            }
+                            if (!t.mirror) {
+                                st.row(b, w);
+                            } else {
+                                st.begin();
+                                st.row(0, w);
+                                __syncwarp();
+                                st.transpose(0, 1);
+                                st.ready();
+                                st.send(0, col, row0, t.block * PL + b);
+                                st.send(1, row0, col, t.block * PL + b);
+                                st.close();
+                            }
+                        }
+                        if (!t.mirror) {
+                            st.ready();
+#pragma unroll
+                            for (int b = 0; b < PL; ++b) st.send(b, col, row0, t.block * PL + b);
+                            st.close();
+                        }
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 32; ++i) { acc[0][i] = acc[1][i]; acc[1][i] = acc[2][i]; acc[2][i] = acc[3][i]; }
+            }
+            if (lane == 0 && !last) {
+                tma_store_wait_all<0>();                                       // landed, and visible to this thread
+                __threadfence();
+                atomicAdd(p.done + t.block, 1u);
+            }
+            __syncwarp();
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    cluster_arrive_release();
+    cluster_wait_acquire();
+    if (warp == 0) tmem_dealloc_pair(tmem_base, 512);
+}
+
+// sums of squares of `parts` parts of each block, and the new momentum; the counters of the products at zero
 template <typename T>
-__global__ void __launch_bounds__(256) norm_kernel(const Io<T> io, double *part, int parts, int64_t size)
+__global__ void __launch_bounds__(256) norm_kernel(const Io<T> io, double *part, int parts, int64_t size, unsigned *zero, int64_t zeros)
 {
     __shared__ double s_part[8];
     depend_wait();
     depend_launch();
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < zeros; i += (int64_t)gridDim.x * 256) zero[i] = 0;
     const int block = blockIdx.x / parts, p = blockIdx.x % parts;
     const int64_t per = ((size + parts - 1) / parts + 3) / 4 * 4, first = p * per, last = min(size, first + per);
     const size_t base = (size_t)block * size;
@@ -1035,38 +1221,46 @@ __global__ void __launch_bounds__(256) start_kernel(const Planes x, const Io<T> 
     }
 }
 
-// How a product is cut: columns of a tile, parts of K
-struct Cut {
-    int tn, splits;
-};
-
-// by the time it takes, in cycles: rounds of the CTA pairs over tiles of `products` MMAs of 512 cycles per K chunk (narrow tiles load
-// more per MMA), 6000 for a tile's start and end, 20000 for the launch that adds parts up
-Cut cut(int64_t blocks, int m, int n, int kdim, int products, bool lower)
+// Tiles and parts of a product by the time they take on a block's share of the CTA pairs, in cycles: `products` MMAs of 512 cycles per
+// K chunk (narrow tiles load more per MMA), 4000 for a tile's start and end, 6000 and 1000 each for parts.
+Product cut(int64_t blocks, int m, int n, int kdim, int products, bool lower)
 {
-    Cut best = {256, 1};
+    Product best = {};
     double best_cost = 1e300;
-    const int64_t mt = ceil_div(m, 256), chunks = ceil_div(kdim, kPgChunk);
+    const int64_t mt = ceil_div(m, 256), chunks = ceil_div(kdim, kPgChunk), share = blocks >= kPgPairs ? 1 : kPgPairs / (blocks > 0 ? blocks : 1);
     for (int tn = 256; tn >= 128; tn /= 2) {
-        const int64_t tiles = blocks * (lower ? mt * (mt + 1) / 2 * (256 / tn) : mt * ceil_div(n, tn));
-        for (int s = 1; s <= 16 && s * 2 <= chunks + 1; ++s) {
-            if (s > 1 && tiles * (s - 1) >= 2 * kPgPairs) break;
-            const int64_t rounds = (tiles * s + kPgPairs - 1) / kPgPairs;
+        const int64_t tiles = lower ? mt * (mt + 1) / 2 * (256 / tn) : mt * ceil_div(n, tn);
+        for (int s = 1; s <= 16 && s <= chunks; ++s) {
+            if (s > 1 && tiles * s > share) break;
+            const int64_t rounds = (tiles * s + share - 1) / share, per = (chunks + s - 1) / s;
             const double chunk = 512.0 * products * tn / 256 * (tn == 128 ? 1.2 : 1.0);
-            const double cost = rounds * ((double)((chunks + s - 1) / s) * chunk + 6000.0) + (s > 1 ? 20000.0 : 0.0);
+            const double cost = rounds * (per * chunk + 4000.0) + (s > 1 ? 6000.0 + 1000.0 * s : 0.0);
             if (cost < best_cost) {
                 best_cost = cost;
-                best = {tn, s};
+                best.tn = tn;
+                best.splits = s;
+                best.tiles = (int)tiles;
             }
         }
     }
+    best.rows = m;
+    best.cols = n;
+    best.kchunks = (int)chunks;
+    best.per_split = ceil_div(chunks, best.splits);
+    best.publishers = best.splits == 1 ? 16 : 16 * (best.splits < best.tn / 64 ? best.splits : best.tn / 64);
+    best.sub = 256 / best.tn;
+    best.lower = lower;
+    best.mtiles = (int)mt;
+    best.ntiles = ceil_div(n, best.tn);
+    best.scale = 1.0f;
     return best;
 }
 
 struct Large {
     int k, n, ldx, ldk, planes, parts;
-    Cut s, p, x;
-    size_t norm, xp[2], sp, pp, part, total;
+    Product prod[3];               // S~, P, X
+    int64_t counters, part_units;
+    size_t norm, count, xp[2], sp, pp, part, total;
 };
 
 Large large_layout(int64_t blocks, int rows, int cols, int dtype)
@@ -1078,46 +1272,36 @@ Large large_layout(int64_t blocks, int rows, int cols, int dtype)
     l.ldk = (l.k + 15) / 16 * 16;
     l.planes = dtype == MONARCH_F32 ? 3 : 2;
     const int products = dtype == MONARCH_F32 ? 6 : 3;
-    l.s = cut(blocks, l.k, l.k, l.n, products, true);
-    l.p = cut(blocks, l.k, l.k, l.k, products, true);
-    l.x = cut(blocks, rows, cols, l.k, products, false);
-    const size_t kk = (size_t)l.k * l.k, rc = (size_t)rows * cols, b = (size_t)blocks;
+    const bool wide = rows <= cols;
+    l.prod[0] = cut(blocks, l.k, l.k, l.n, products, true);
+    l.prod[1] = cut(blocks, l.k, l.k, l.k, products, true);
+    l.prod[2] = cut(blocks, rows, cols, l.k, products, false);
+    l.prod[0].a_mn = l.prod[0].b_mn = !wide;
+    l.prod[2].b_mn = wide;
+    l.prod[0].diagonal = kBeta;
+    l.prod[1].scale = kC;
+    l.prod[1].diagonal = kGamma;
+    const size_t rc = (size_t)rows * cols, b = (size_t)blocks;
     const int64_t want = (int64_t)((rc + 8191) / 8192);
     l.parts = (int)(want < kNormParts ? want : kNormParts);
     size_t at = MONARCH_STATUS_BYTES + 65536;          // the status area and the counters of kernels that may share the workspace
     auto take = [&](size_t bytes) { const size_t o = at; at += up(bytes); return o; };
     l.norm = take(b * l.parts * 8);
+    l.counters = blocks;
+    for (const Product &q : l.prod)
+        if (q.splits > 1) l.counters += blocks * q.tiles * 16;
+    l.count = take((size_t)l.counters * 4);
     // two X: the last product of a step reads the one and writes the other
     l.xp[0] = take(b * l.planes * rows * l.ldx * 2);
     l.xp[1] = take(b * l.planes * rows * l.ldx * 2);
     l.sp = take(b * l.planes * l.k * l.ldk * 2);
     l.pp = take(b * l.planes * l.k * l.ldk * 2);
-    size_t part = 0;
-    if (l.s.splits > 1) part = kk * l.s.splits;
-    if (l.p.splits > 1 && kk * l.p.splits > part) part = kk * l.p.splits;
-    if (l.x.splits > 1 && rc * l.x.splits > part) part = rc * l.x.splits;
-    l.part = take(b * part * 4);
+    l.part_units = 0;
+    for (const Product &q : l.prod)
+        if (q.splits > 1 && (int64_t)q.tiles * q.splits > l.part_units) l.part_units = (int64_t)q.tiles * q.splits;
+    l.part = take(b * l.part_units * 16 * 4096 * 4);
     l.total = at;
     return l;
-}
-
-template <typename T, int PL, int SCHEME, int AMN, int BMN, int ROLE>
-int ortho_product(const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mc, PlaneGemm p, const Cut &c, int kdim, const typename EpiPlanes<T, PL, ROLE>::Args &a,
-                  float *part, cudaStream_t s)
-{
-    const Planes &m = a.to;
-    constexpr bool kSym = ROLE == kRoleS || ROLE == kRoleP;
-    p.rows = m.rows;
-    p.cols = m.cols;
-    p.kdim = kdim;
-    p.tn = c.tn;
-    p.splits = c.splits;
-    p.lower = kSym;
-    if (c.splits == 1) return launch_plane_gemm<AMN, BMN, SCHEME, true, EpiPlanes<T, PL, ROLE>>(ma, mb, mc, p, a, s);
-    const EpiPart::Args e = {part, m.rows, m.cols};
-    MONARCH_TRY((launch_plane_gemm<AMN, BMN, SCHEME, true, EpiPart>(ma, mb, mb, p, e, s)));
-    const int64_t tr = ceil_div(m.rows, 32), tc = ceil_div(m.cols, 32), tiles = kSym ? tr * (tr + 1) / 2 : tr * tc;
-    return launch_serialized(finish_kernel<T, PL, ROLE>, dim3((unsigned)(tiles * p.batches)), 256, 0, s, (const float *)part, c.splits, a);
 }
 
 template <typename T, int PL, int SCHEME>
@@ -1127,50 +1311,80 @@ int ortho_large(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, 
     char *base = (char *)ws;
     const bool wide = rows <= cols;
     double *norm = (double *)(base + l.norm);
-    float *part = (float *)(base + l.part);
+    unsigned *count = (unsigned *)(base + l.count);
     const Planes sp = {(__nv_bfloat16 *)(base + l.sp), l.k, l.k, l.ldk}, pp = {(__nv_bfloat16 *)(base + l.pp), l.k, l.k, l.ldk};
     Planes x[2];
-    CUtensorMap x_k[2], x_n[2], x_b[2], x_to[2], s_a, s_b, s_to, p_a, p_b, p_to;
+    OrthoMaps m;
+    const int64_t xz = (int64_t)rows * l.ldx, kz = (int64_t)l.k * l.ldk, z = blocks * PL;
+    const int ts = l.prod[0].tn / 2, tp = l.prod[1].tn / 2, tx = l.prod[2].tn / 2;
     for (int i = 0; i < 2; ++i) {
         x[i] = {(__nv_bfloat16 *)(base + l.xp[i]), rows, cols, l.ldx};
-        MONARCH_TRY(plane_map(&x_k[i], x[i].at, 0, rows, cols, l.ldx, (int64_t)rows * l.ldx, blocks * PL));
-        MONARCH_TRY(plane_map(&x_b[i], x[i].at, 0, rows, cols, l.ldx, (int64_t)rows * l.ldx, blocks * PL, l.s.tn / 2));
-        MONARCH_TRY(plane_map(&x_n[i], x[i].at, 1, rows, cols, l.ldx, (int64_t)rows * l.ldx, blocks * PL));
+        MONARCH_TRY(plane_map(&m.s_a[i], x[i].at, !wide, rows, cols, l.ldx, xz, z));
+        MONARCH_TRY(plane_map(&m.s_b[i], x[i].at, !wide, rows, cols, l.ldx, xz, z, ts));
+        if (wide) {
+            MONARCH_TRY(plane_map(&m.x_a[i], pp.at, 0, l.k, l.k, l.ldk, kz, z));
+            MONARCH_TRY(plane_map(&m.x_b[i], x[i].at, 1, rows, cols, l.ldx, xz, z));
+        } else {
+            MONARCH_TRY(plane_map(&m.x_a[i], x[i].at, 0, rows, cols, l.ldx, xz, z));
+            MONARCH_TRY(plane_map(&m.x_b[i], pp.at, 0, l.k, l.k, l.ldk, kz, z, tx));
+        }
+        MONARCH_TRY(plane_target(&m.x_to[i], x[i].at, rows, cols, l.ldx, xz, z));
     }
-    for (int i = 0; i < 2; ++i) MONARCH_TRY(plane_target(&x_to[i], x[i].at, rows, cols, l.ldx, (int64_t)rows * l.ldx, blocks * PL));
-    MONARCH_TRY(plane_target(&s_to, sp.at, l.k, l.k, l.ldk, (int64_t)l.k * l.ldk, blocks * PL));
-    MONARCH_TRY(plane_target(&p_to, pp.at, l.k, l.k, l.ldk, (int64_t)l.k * l.ldk, blocks * PL));
-    MONARCH_TRY(plane_map(&s_a, sp.at, 0, l.k, l.k, l.ldk, (int64_t)l.k * l.ldk, blocks * PL));
-    MONARCH_TRY(plane_map(&s_b, sp.at, 0, l.k, l.k, l.ldk, (int64_t)l.k * l.ldk, blocks * PL, l.p.tn / 2));
-    MONARCH_TRY(plane_map(&p_a, pp.at, 0, l.k, l.k, l.ldk, (int64_t)l.k * l.ldk, blocks * PL));
-    MONARCH_TRY(plane_map(&p_b, pp.at, 0, l.k, l.k, l.ldk, (int64_t)l.k * l.ldk, blocks * PL, l.x.tn / 2));
+    MONARCH_TRY(plane_map(&m.p_a, sp.at, 0, l.k, l.k, l.ldk, kz, z));
+    MONARCH_TRY(plane_map(&m.p_b, sp.at, 0, l.k, l.k, l.ldk, kz, z, tp));
+    MONARCH_TRY(plane_target(&m.s_to, sp.at, l.k, l.k, l.ldk, kz, z));
+    MONARCH_TRY(plane_target(&m.p_to, pp.at, l.k, l.k, l.ldk, kz, z));
 
-    MONARCH_TRY(launch_serialized(norm_kernel<T>, dim3((unsigned)(blocks * l.parts)), 256, 0, s, io, norm, l.parts, (int64_t)rows * cols));
+    MONARCH_TRY(launch_serialized(norm_kernel<T>, dim3((unsigned)(blocks * l.parts)), 256, 0, s, io, norm, l.parts, (int64_t)rows * cols, count, l.counters));
     int64_t ctas = ceil_div((int64_t)rows * cols, 4096), most = 148 * 8 / blocks + 1;
     if (ctas > most) ctas = most;
     MONARCH_TRY(launch_serialized(start_kernel<T, PL>, dim3((unsigned)(blocks * ctas)), 256, 0, s, x[0], io, (const double *)norm, l.parts, (int)ctas));
-    PlaneGemm p = {};
+
+    OrthoRun p = {};
     p.status = (unsigned *)ws;
-    p.batches = (int)blocks;
-    p.a_zstep = p.b_zstep = PL;
-    p.seg = SCHEME == kP3x3 ? pg_seg(SCHEME) : 16;         // bf16 results: 192 steps
-    for (int i = 0; i < steps; ++i) {
-        const int at = i & 1;
-        const typename EpiPlanes<T, PL, kRoleS>::Args es = {sp, io};
-        if (wide) MONARCH_TRY((ortho_product<T, PL, SCHEME, 0, 0, kRoleS>(x_k[at], x_b[at], s_to, p, l.s, l.n, es, part, s)));
-        else MONARCH_TRY((ortho_product<T, PL, SCHEME, 1, 1, kRoleS>(x_n[at], x_n[at], s_to, p, l.s, l.n, es, part, s)));
-        const typename EpiPlanes<T, PL, kRoleP>::Args ep = {pp, io};
-        MONARCH_TRY((ortho_product<T, PL, SCHEME, 0, 0, kRoleP>(s_a, s_b, p_to, p, l.p, l.k, ep, part, s)));
-        if (i + 1 < steps) {
-            const typename EpiPlanes<T, PL, kRoleX>::Args ex = {x[at ^ 1], io};
-            if (wide) MONARCH_TRY((ortho_product<T, PL, SCHEME, 0, 1, kRoleX>(p_a, x_n[at], x_to[at ^ 1], p, l.x, l.k, ex, part, s)));
-            else MONARCH_TRY((ortho_product<T, PL, SCHEME, 0, 0, kRoleX>(x_k[at], p_b, x_to[at ^ 1], p, l.x, l.k, ex, part, s)));
-        } else {
-            const typename EpiPlanes<T, PL, kRoleOut>::Args eo = {x[at], io};
-            if (wide) MONARCH_TRY((ortho_product<T, PL, SCHEME, 0, 1, kRoleOut>(p_a, x_n[at], x_to[at ^ 1], p, l.x, l.k, eo, part, s)));
-            else MONARCH_TRY((ortho_product<T, PL, SCHEME, 0, 0, kRoleOut>(x_k[at], p_b, x_to[at ^ 1], p, l.x, l.k, eo, part, s)));
+    p.done = count;
+    p.blocks = (int)blocks;
+    p.steps = steps;
+    p.rows = rows;
+    p.cols = cols;
+    p.part = (float *)(base + l.part);
+    p.part_units = l.part_units;
+    unsigned *next = count + blocks;
+    int64_t units = 0;
+    for (int i = 0; i < 3; ++i) {
+        p.prod[i] = l.prod[i];
+        if (l.prod[i].splits > 1) {
+            p.prod[i].parts_done = next;
+            next += blocks * l.prod[i].tiles * 16;
         }
+        const int64_t u = blocks * l.prod[i].tiles * l.prod[i].splits;
+        if (u > units) units = u;
     }
+    const auto kern = ortho_run_kernel<T, PL, SCHEME>;
+    static PerDeviceCache cache;
+    int pairs = cache.get();
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(kPgThreads);
+    cfg.dynamicSmemBytes = kRunSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeCooperative;            // all CTAs resident at once: tiles wait for one another
+    attr[1].val.cooperative = 1;
+    cfg.attrs = attr;
+    if (pairs < 0) {
+        MONARCH_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kRunSmem));
+        cfg.gridDim = dim3(2);
+        cfg.numAttrs = 1;
+        MONARCH_CUDA_TRY(cudaOccupancyMaxActiveClusters(&pairs, kern, &cfg));
+        cache.set(pairs);
+    }
+    if (pairs < 1) return MONARCH_ERR_CUDA;
+    cfg.gridDim = dim3((unsigned)(2 * (units < pairs ? units : pairs)));
+    cfg.numAttrs = 2;
+    MONARCH_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, m, p, io));
+    note_launch();
     return MONARCH_OK;
 }
 
