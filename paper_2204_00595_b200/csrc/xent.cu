@@ -42,6 +42,11 @@ struct PrepArgs {
     __nv_bfloat16 *xp;                // planes [planes][tokens][dp]
     int64_t ignore;
     int tokens, d, dp, vocab, rows_per_cta;
+    int ctas;                         // CTAs for the tokens; those behind them split the first piece of W
+    const void *W;
+    __nv_bfloat16 *wp;
+    size_t wplane;
+    int wrows;
 };
 
 // fp32 value -> bf16 planes.  The largest fp32 values round to infinity in bf16: they are cut instead.
@@ -57,20 +62,21 @@ template <int PL> __device__ __forceinline__ void split(float v, __nv_bfloat16 (
     }
 }
 
+// this warp's part of a row, padded to dp columns
 template <typename T, int PL>
-__device__ __forceinline__ void copy_row(const T *__restrict__ src, __nv_bfloat16 *dst, size_t plane, int d, int dp, int lane)
+__device__ __forceinline__ void copy_row(const T *__restrict__ src, __nv_bfloat16 *dst, size_t plane, int d, int dp, int lane, int part = 0, int parts = 1)
 {
     if constexpr (sizeof(T) == 2) {
         if (d == dp) {
 #pragma unroll 4
-            for (int c = lane * 8; c < dp; c += 256) *reinterpret_cast<uint4 *>(dst + c) = __ldg(reinterpret_cast<const uint4 *>(src + c));
+            for (int c = (part * 32 + lane) * 8; c < dp; c += parts * 256) *reinterpret_cast<uint4 *>(dst + c) = __ldg(reinterpret_cast<const uint4 *>(src + c));
             return;
         }
     }
     if constexpr (sizeof(T) == 4) {
         if (d % 4 == 0) {                                   // dp - d is 0 or 4
 #pragma unroll 4
-            for (int c = lane * 4; c < dp; c += 128) {
+            for (int c = (part * 32 + lane) * 4; c < dp; c += parts * 128) {
                 float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 if (c < d) v = __ldg(reinterpret_cast<const float4 *>(src + c));
                 __nv_bfloat16 o[4][PL];
@@ -85,7 +91,7 @@ __device__ __forceinline__ void copy_row(const T *__restrict__ src, __nv_bfloat1
         }
     }
 #pragma unroll 4
-    for (int c = lane * 2; c < dp; c += 64) {
+    for (int c = (part * 32 + lane) * 2; c < dp; c += parts * 64) {
         __nv_bfloat16 a[PL], b[PL];
         split<PL>(c < d ? elem<T>::load(src + c) : 0.0f, a);
         split<PL>(c + 1 < d ? elem<T>::load(src + c + 1) : 0.0f, b);
@@ -101,6 +107,11 @@ __global__ void __launch_bounds__(256) xent_prep_kernel(const PrepArgs p)
     depend_wait();
     depend_launch();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if ((int)blockIdx.x >= p.ctas) {
+        for (int r = ((int)blockIdx.x - p.ctas) * 8 + warp; r < p.wrows; r += ((int)gridDim.x - p.ctas) * 8)
+            copy_row<T, PL>((const T *)p.W + (size_t)r * p.d, p.wp + (size_t)r * p.dp, p.wplane, p.d, p.dp, lane);
+        return;
+    }
     const int first = blockIdx.x * p.rows_per_cta, last = min(p.tokens, first + p.rows_per_cta);
     int before = 0, total = 0;
     for (int t = tid; t < p.tokens; t += 256) {
@@ -152,16 +163,19 @@ __global__ void __launch_bounds__(256) xent_prep_kernel(const PrepArgs p)
             p.lse[t] = 0.0f;
         }
         __syncthreads();
-        for (int r = warp; r < 256 && base + r < last; r += 8) {
+        // fewer rows than warps: several warps a row
+        const int here = min(256, last - base), parts = here >= 8 ? 1 : 8 / here;
+        for (int i = warp; i < here * parts; i += 8) {
+            const int r = i / parts, part = i - r * parts;
             const int dst = s_dst[r];
             if (dst >= 0)
-                copy_row<T, PL>(x + (size_t)(base + r) * p.d, p.xp + (size_t)dst * p.dp, plane, p.d, p.dp, lane);
+                copy_row<T, PL>(x + (size_t)(base + r) * p.d, p.xp + (size_t)dst * p.dp, plane, p.d, p.dp, lane, part, parts);
             else if (BWD)
-                for (int c = lane; c < p.d; c += 32) elem<T>::store((T *)p.dx + (size_t)(base + r) * p.d + c, 0.0f);
+                for (int c = part * 32 + lane; c < p.d; c += parts * 32) elem<T>::store((T *)p.dx + (size_t)(base + r) * p.d + c, 0.0f);
             if (base + r >= total)                           // rows behind the last one that counts enter sums over tokens as zeros
-                for (int i = 0; i < PL; ++i)
-                    for (int c = lane * 8; c < p.dp; c += 256)
-                        *reinterpret_cast<uint4 *>(p.xp + i * plane + (size_t)(base + r) * p.dp + c) = make_uint4(0, 0, 0, 0);
+                for (int j = 0; j < PL; ++j)
+                    for (int c = (part * 32 + lane) * 8; c < p.dp; c += parts * 256)
+                        *reinterpret_cast<uint4 *>(p.xp + j * plane + (size_t)(base + r) * p.dp + c) = make_uint4(0, 0, 0, 0);
         }
     }
 }
@@ -284,127 +298,71 @@ template <int PL> struct EpiGrad {
 
 // rows of float32, stored or added to
 struct EpiStoreF32 {
-    static constexpr int kStage = 0;
+    static constexpr int kStage = 3;
     struct Args {
         float *out;
         int rows, cols, add;
     };
     __device__ __forceinline__ void begin(const Args &, const PgTile &) {}
-    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<1> &)
+    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<kStage> &st)
     {
-        if (t.row >= a.rows) return;
-        const int left = a.cols - t.col - c;
-        float *out = a.out + (size_t)t.row * a.cols + t.col + c;
-        if ((a.cols & 7) == 0) {
-#pragma unroll
-            for (int i = 0; i < 32; i += 8) {
-                if (i >= left) break;
-                if (a.add) {
-                    const float4 o0 = *reinterpret_cast<const float4 *>(out + i), o1 = *reinterpret_cast<const float4 *>(out + i + 4);
-                    v[i] += o0.x; v[i + 1] += o0.y; v[i + 2] += o0.z; v[i + 3] += o0.w;
-                    v[i + 4] += o1.x; v[i + 5] += o1.y; v[i + 6] += o1.z; v[i + 7] += o1.w;
-                }
-                const uint32_t *w = reinterpret_cast<const uint32_t *>(v) + i;
-                *reinterpret_cast<uint4 *>(out + i) = make_uint4(w[0], w[1], w[2], w[3]);
-                *reinterpret_cast<uint4 *>(out + i + 4) = make_uint4(w[4], w[5], w[6], w[7]);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (i < left) out[i] = a.add ? out[i] + v[i] : v[i];
-        }
+        const int col = t.col + c + st.lane, row0 = t.row & ~31, rows = col < a.cols ? a.rows - row0 : 0;
+        float *out = a.out + (size_t)row0 * a.cols + col;
+        st.rows(
+            v, [&](int r) { return a.add && r < rows ? out[(size_t)r * a.cols] : 0.0f; },
+            [&](int r, float x, float w) {
+                if (r < rows) out[(size_t)r * a.cols] = x + w;
+            });
     }
     __device__ __forceinline__ void end(const Args &, const PgTile &) {}
 };
 
 // dx: the sums of the pieces so far in float32 (compact rows), the last one to the caller's rows
 template <typename T> struct EpiDx {
-    static constexpr int kStage = 0;
+    static constexpr int kStage = 3;
     struct Args {
         float *acc;
         T *dx;
         const int *map, *count;
         int d, first, last;
     };
-    int to;
-    __device__ __forceinline__ void begin(const Args &a, const PgTile &t)
+    int n;
+    __device__ __forceinline__ void begin(const Args &a, const PgTile &) { n = *a.count; }
+    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<kStage> &st)
     {
-        to = t.row < *a.count ? (a.last ? a.map[t.row] : t.row) : -1;
-    }
-    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<1> &)
-    {
-        if (to < 0) return;
-        const int left = a.d - t.col - c;
-        const size_t col = (size_t)t.col + c;
-        float *acc = a.acc + (size_t)t.row * a.d + col;
-        const bool vec = (a.d & 7) == 0;
-#pragma unroll
-        for (int i = 0; i < 32; i += 8) {
-            if (i >= left) break;
-            if (vec) {
-                if (!a.first) {
-                    const float4 o0 = *reinterpret_cast<const float4 *>(acc + i), o1 = *reinterpret_cast<const float4 *>(acc + i + 4);
-                    v[i] += o0.x; v[i + 1] += o0.y; v[i + 2] += o0.z; v[i + 3] += o0.w;
-                    v[i + 4] += o1.x; v[i + 5] += o1.y; v[i + 6] += o1.z; v[i + 7] += o1.w;
-                }
-                const uint32_t *w = reinterpret_cast<const uint32_t *>(v) + i;
-                if (a.last && sizeof(T) == 2) {
-                    *reinterpret_cast<uint4 *>(a.dx + (size_t)to * a.d + col + i) =
-                        make_uint4(pack_bf16(v[i], v[i + 1]), pack_bf16(v[i + 2], v[i + 3]), pack_bf16(v[i + 4], v[i + 5]), pack_bf16(v[i + 6], v[i + 7]));
-                } else {
-                    float *o = a.last ? reinterpret_cast<float *>(a.dx) + (size_t)to * a.d + col + i : acc + i;
-                    *reinterpret_cast<uint4 *>(o) = make_uint4(w[0], w[1], w[2], w[3]);
-                    *reinterpret_cast<uint4 *>(o + 4) = make_uint4(w[4], w[5], w[6], w[7]);
-                }
-            } else {
-#pragma unroll
-                for (int j = i; j < i + 8; ++j)
-                    if (j < left) {
-                        const float r = a.first ? v[j] : v[j] + acc[j];
-                        if (a.last) elem<T>::store(a.dx + (size_t)to * a.d + col + j, r);
-                        else acc[j] = r;
-                    }
-            }
-        }
+        const int col = t.col + c + st.lane, row0 = t.row & ~31, rows = col < a.d ? n - row0 : 0;
+        float *acc = a.acc + (size_t)row0 * a.d + col;
+        st.rows(
+            v, [&](int r) { return !a.first && r < rows ? acc[(size_t)r * a.d] : 0.0f; },
+            [&](int r, float x, float w) {
+                if (r >= rows) return;
+                if (a.last) elem<T>::store(a.dx + (size_t)a.map[row0 + r] * a.d + col, x + w);
+                else acc[(size_t)r * a.d] = x + w;
+            });
     }
     __device__ __forceinline__ void end(const Args &, const PgTile &) {}
 };
 
 // dx where a few tiles are split along the vocabulary: a sum per part, over the pieces, in float32
 struct EpiDxPart {
-    static constexpr int kStage = 0;
+    static constexpr int kStage = 3;
     struct Args {
         float *acc;                // [parts][tokens][d]
         const int *count;
         size_t part;
         int d, first;
     };
-    float *to;
-    __device__ __forceinline__ void begin(const Args &a, const PgTile &t)
+    int n;
+    __device__ __forceinline__ void begin(const Args &a, const PgTile &) { n = *a.count; }
+    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<kStage> &st)
     {
-        to = t.row < *a.count ? a.acc + t.z * a.part + (size_t)t.row * a.d + t.col : nullptr;
-    }
-    __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<1> &)
-    {
-        if (to == nullptr) return;
-        const int left = a.d - t.col - c;
-        float *out = to + c;
-        if ((a.d & 3) == 0) {
-#pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-                if (i >= left) break;
-                float4 o = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-                if (!a.first) {
-                    const float4 q = *reinterpret_cast<const float4 *>(out + i);
-                    o.x += q.x; o.y += q.y; o.z += q.z; o.w += q.w;
-                }
-                *reinterpret_cast<float4 *>(out + i) = o;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (i < left) out[i] = a.first ? v[i] : v[i] + out[i];
-        }
+        const int col = t.col + c + st.lane, row0 = t.row & ~31, rows = col < a.d ? n - row0 : 0;
+        float *acc = a.acc + t.z * a.part + (size_t)row0 * a.d + col;
+        st.rows(
+            v, [&](int r) { return !a.first && r < rows ? acc[(size_t)r * a.d] : 0.0f; },
+            [&](int r, float x, float w) {
+                if (r < rows) acc[(size_t)r * a.d] = x + w;
+            });
     }
     __device__ __forceinline__ void end(const Args &, const PgTile &) {}
 };
@@ -473,20 +431,23 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const float2 *__restrict
 }
 
 // ------------------------------------------------------------------------------------------------ forward of few tokens
-// One launch that reads W once at the speed of memory.  A warp takes 16 rows of W straight from memory into the first operand of
-// warp MMAs (a lane's 16 bytes are eight consecutive k of one row: the order of k within a chunk of 32 is the same for both
-// operands, so it does not matter), the tokens (8 per column tile) wait in shared memory.  Every lane keeps maximum and sum of its
-// rows; lanes, warps and, in the last CTA to finish, CTAs are joined.  fp32: three planes of both, six products.
-constexpr int kFewThreads = 512, kFewMost = 32;
-constexpr size_t kFewSmem = 200 * 1024;
+// One launch that reads W once.  Rows of W go straight from memory into the first operand of warp MMAs (a lane's 16 bytes are eight
+// consecutive k of one row: the order of k within a chunk of 32 is the same for both operands, so it does not matter), the tokens
+// (8 per column tile) wait in shared memory.  The eight warps of a team share 16 rows, an eighth of d each: their sums meet in shared
+// memory, the warps take turns to turn them into maximum and sum of exponentials while the others go on.  (A warp to itself for 16
+// rows: 3142 groups of a vocabulary of 50257 on 2368 warps are two rounds, the second a third full; 26.5 us for one token of d 1024.)
+// Lanes, warps and, in the last CTA to finish, CTAs are joined.  fp32: three planes of both, six products.
+constexpr int kFewThreads = 512, kFewMost = 16, kFewTeam = 8, kFewTeams = kFewThreads / 32 / kFewTeam;
+constexpr size_t kFewSmem = 184 * 1024;         // for the tokens; the sums take up to 32 KB more
 constexpr int kFewTicket = 16;                  // word of the status area, zero between calls
 
 int few_row(int d) { return ((d * 2 + 127) / 128 * 128 + 64) / 2; }             // rows 64 bytes apart in their banks
-int few_tiles(int tokens) { return tokens <= 8 ? 1 : tokens <= 16 ? 2 : 4; }      // column tiles of 8 tokens: what the kernels are built for
-size_t few_smem(int tokens, int d, int planes) { return (size_t)few_tiles(tokens) * 8 * few_row(d) * 2 * planes; }
+int few_tiles(int tokens) { return tokens <= 8 ? 1 : 2; }                       // column tiles of 8 tokens: what the kernels are built for
+size_t few_x(int tokens, int d, int planes) { return (size_t)tokens * few_row(d) * 2 * planes; }
+size_t few_smem(int tokens, int d, int planes) { return few_x(tokens, d, planes) + (size_t)kFewTeams * 2 * kFewTeam * few_tiles(tokens) * 512; }
 bool few_fits(int64_t tokens, int d, int dtype)
 {
-    return tokens <= kFewMost && d % 8 == 0 && few_smem((int)tokens, d, dtype == MONARCH_F32 ? 3 : 1) <= kFewSmem;
+    return tokens <= kFewMost && d % 8 == 0 && few_x((int)tokens, d, dtype == MONARCH_F32 ? 3 : 1) <= kFewSmem;
 }
 
 struct FewArgs {
@@ -543,23 +504,45 @@ template <> struct FewRaw<float> {
 template <typename T, int PL, int NT>
 __global__ void __launch_bounds__(kFewThreads, 1) xent_few_kernel(const FewArgs p)
 {
-    extern __shared__ __align__(16) __nv_bfloat16 xs[];                        // [PL][8 NT][row]
+    extern __shared__ __align__(16) __nv_bfloat16 xs[];                        // [PL][tokens][row], then the sums
     __shared__ float2 s_part[kFewThreads / 32][8 * NT];
     __shared__ int s_tgt[8 * NT], s_last;
     constexpr int kStep = sizeof(T) == 2 ? 4 : 2;                               // chunks of 32 requested ahead
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-    const size_t xplane = (size_t)8 * NT * p.row;
+    const size_t xplane = (size_t)p.tokens * p.row;
+    const int groups = (p.vocab + 15) / 16, chunks = (p.d + 31) / 32;
+    const int team = warp / kFewTeam, member = warp % kFewTeam;
+    // this warp's chunks, in steps of kStep
+    const int each = (chunks + kFewTeam - 1) / kFewTeam, k0 = min(member * each, chunks), k1 = min(k0 + each, chunks), steps = (each + kStep - 1) / kStep;
+    const int first = blockIdx.x * kFewTeams + team, stride = gridDim.x * kFewTeams;
+    FewRaw<T> raw[kStep][2];
+    auto fetch = [&](int grp, int step) {
+        const T *w0 = (const T *)p.W + (size_t)min(grp * 16 + g, p.vocab - 1) * p.d, *w1 = (const T *)p.W + (size_t)min(grp * 16 + g + 8, p.vocab - 1) * p.d;
+#pragma unroll
+        for (int u = 0; u < kStep; ++u) {
+            const int k = k0 + step * kStep + u, at = k * 32 + c * 8;
+            const bool in = grp < groups && k < k1 && at < p.d;
+            raw[u][0].load(w0 + at, in);
+            raw[u][1].load(w1 + at, in);
+        }
+    };
     depend_wait();
     depend_launch();
-    for (int t = warp; t < 8 * NT; t += kFewThreads / 32) {
-        int64_t y = t < p.tokens ? p.targets[t] : p.ignore;
+    fetch(first, 0);                                                           // on its way while the tokens are prepared
+    if (threadIdx.x < 8 * NT && (int)threadIdx.x >= p.tokens) s_tgt[threadIdx.x] = -2;
+    const int parts = kFewThreads / 32 / p.tokens;                             // warps a token; tokens <= 16
+    if (const int t = warp / parts; t < p.tokens) {
+        const int part = warp - t * parts;
+        const int64_t y = p.targets[t];
         const bool keep = y != p.ignore;
-        if (lane == 0) s_tgt[t] = !keep ? -2 : y >= 0 && y < p.vocab ? (int)y : -1;
-        for (int k = lane * 2; k < p.row; k += 64) {
+        if (lane == 0 && part == 0) s_tgt[t] = !keep ? -2 : y >= 0 && y < p.vocab ? (int)y : -1;
+#pragma unroll 4
+        for (int k = (part * 32 + lane) * 2; k < p.row; k += parts * 64) {
             __nv_bfloat16 a[PL], b[PL];
             const T *src = (const T *)p.x + (size_t)t * p.d + k;
-            split<PL>(keep && k < p.d ? elem<T>::load(src) : 0.0f, a);
-            split<PL>(keep && k + 1 < p.d ? elem<T>::load(src + 1) : 0.0f, b);
+            const float v0 = k < p.d ? elem<T>::load(src) : 0.0f, v1 = k + 1 < p.d ? elem<T>::load(src + 1) : 0.0f;
+            split<PL>(keep ? v0 : 0.0f, a);
+            split<PL>(keep ? v1 : 0.0f, b);
 #pragma unroll
             for (int q = 0; q < PL; ++q) *reinterpret_cast<__nv_bfloat162 *>(xs + q * xplane + (size_t)t * p.row + k) = __nv_bfloat162(a[q], b[q]);
         }
@@ -575,60 +558,65 @@ __global__ void __launch_bounds__(kFewThreads, 1) xent_few_kernel(const FewArgs 
             m[n][e] = __int_as_float(0xff800000);
             s[n][e] = 0.0f;
         }
-    const int groups = (p.vocab + 15) / 16, chunks = (p.d + 31) / 32;
     const __nv_bfloat16 *xl = xs + (size_t)g * p.row + c * 8;
-    for (int grp = blockIdx.x * (kFewThreads / 32) + warp; grp < groups; grp += gridDim.x * (kFewThreads / 32)) {
-        const int r0 = grp * 16 + g, r1 = r0 + 8;
-        const T *w0 = (const T *)p.W + (size_t)min(r0, p.vocab - 1) * p.d + c * 8, *w1 = (const T *)p.W + (size_t)min(r1, p.vocab - 1) * p.d + c * 8;
+    float *sums = reinterpret_cast<float *>(xs + PL * xplane) + team * 2 * kFewTeam * NT * 128;      // [2][team][NT][4][32 lanes]
+    int turn = 0;
+    for (int grp = first; grp < groups; grp += stride, ++turn) {
         float z[NT][4] = {}, sum[NT][4] = {};
-        FewRaw<T> raw[kStep][2];
-#pragma unroll
-        for (int u = 0; u < kStep; ++u) {
-            raw[u][0].load(w0 + u * 32, u * 32 + c * 8 < p.d);
-            raw[u][1].load(w1 + u * 32, u * 32 + c * 8 < p.d);
-        }
-        for (int k = 0; k < chunks; k += kStep) {
-            FewRaw<T> next[kStep][2];
+        for (int step = 0; step < steps; ++step) {
+            uint32_t a[kStep][2][PL][4];
 #pragma unroll
             for (int u = 0; u < kStep; ++u) {
-                const int at = (k + kStep + u) * 32;
-                next[u][0].load(w0 + at, at + c * 8 < p.d);
-                next[u][1].load(w1 + at, at + c * 8 < p.d);
+                raw[u][0].planes(a[u][0]);
+                raw[u][1].planes(a[u][1]);
             }
+            fetch(step + 1 < steps ? grp : grp + stride, step + 1 < steps ? step + 1 : 0);
 #pragma unroll
             for (int u = 0; u < kStep; ++u) {
-                if (k + u >= chunks) break;
-                uint32_t a0[PL][4], a1[PL][4];
-                raw[u][0].planes(a0);
-                raw[u][1].planes(a1);
+                const int k = k0 + step * kStep + u;
+                if (k >= k1) break;
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     uint4 b[PL];
 #pragma unroll
-                    for (int q = 0; q < PL; ++q) b[q] = *reinterpret_cast<const uint4 *>(xl + q * xplane + (size_t)n * 8 * p.row + (k + u) * 32);
+                    for (int q = 0; q < PL; ++q)                                   // columns without a token: zeros
+                        b[q] = n * 8 + g < p.tokens ? *reinterpret_cast<const uint4 *>(xl + q * xplane + (size_t)n * 8 * p.row + k * 32) : make_uint4(0, 0, 0, 0);
 #pragma unroll
                     for (int o = PL - 1; o >= 0; --o)
 #pragma unroll
                         for (int q = o; q >= 0; --q) {
-                            const uint32_t f0[4] = {a0[q][0], a1[q][0], a0[q][1], a1[q][1]}, f1[4] = {a0[q][2], a1[q][2], a0[q][3], a1[q][3]};
+                            const uint32_t f0[4] = {a[u][0][q][0], a[u][1][q][0], a[u][0][q][1], a[u][1][q][1]},
+                                           f1[4] = {a[u][0][q][2], a[u][1][q][2], a[u][0][q][3], a[u][1][q][3]};
                             mma(z[n], f0, b[o - q].x, b[o - q].y);
                             mma(z[n], f1, b[o - q].z, b[o - q].w);
                         }
                 }
             }
-            if ((k / kStep) % 8 == 7)                                             // runs of at most 96 steps (plane_gemm.cuh)
+            if (step % 8 == 7)                                                    // runs of at most 96 steps (plane_gemm.cuh)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) { sum[n][e] += z[n][e]; z[n][e] = 0.0f; }
-#pragma unroll
-            for (int u = 0; u < kStep; ++u) { raw[u][0] = next[u][0]; raw[u][1] = next[u][1]; }
         }
+        float *mine = sums + (turn & 1) * kFewTeam * NT * 128;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
+            for (int e = 0; e < 4; ++e) mine[((member * NT + n) * 4 + e) * 32 + lane] = sum[n][e] + z[n][e];
+        asm volatile("bar.sync %0, 256;" ::"r"(team + 1) : "memory");
+        // this buffer is written again two groups on, behind the next barrier, which its reader reaches when it has read
+        if (turn % kFewTeam != member) continue;
+        const int r0 = grp * 16 + g, r1 = r0 + 8;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float t[4] = {};
+#pragma unroll
+            for (int w = 0; w < kFewTeam; ++w)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t[e] += mine[((w * NT + n) * 4 + e) * 32 + lane];
+#pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const float z0 = sum[n][e] + z[n][e], z1 = sum[n][e + 2] + z[n][e + 2];
+                const float z0 = t[e], z1 = t[e + 2];
                 if (r0 == tgt[n][e]) p.tlogit[n * 8 + 2 * c + e] = z0;
                 if (r1 == tgt[n][e]) p.tlogit[n * 8 + 2 * c + e] = z1;
                 const float v0 = r0 < p.vocab ? z0 : __int_as_float(0xff800000), v1 = r1 < p.vocab ? z1 : __int_as_float(0xff800000);
@@ -636,6 +624,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) xent_few_kernel(const FewArgs 
                 s[n][e] = s[n][e] * ex2(m[n][e] - base) + ex2(fmaf(v0, kLog2e, -base)) + ex2(fmaf(v1, kLog2e, -base));
                 m[n][e] = top;
             }
+        }
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -726,7 +715,7 @@ Layout layout(int64_t tokens, int d, int vocab, int dtype, bool bwd)
     l.gplanes = dtype == MONARCH_F32 || tokens <= kFewTokens ? 3 : 2;
     l.dp = (d + 7) / 8 * 8;
     l.chunk = (int)(tokens < kTokenChunk ? tokens : kTokenChunk);
-    l.trows = ceil_div(tokens, 256) * 256;
+    l.trows = ceil_div(tokens, 64) * 64;                                      // what dW's K chunks read; stores and loads behind it are clipped
     if (bwd) {
         l.piece = bwd_piece(tokens, d, vocab);
     } else {
@@ -773,10 +762,11 @@ Layout layout(int64_t tokens, int d, int vocab, int dtype, bool bwd)
 template <typename T, int PL, bool BWD> int prep(PrepArgs a, cudaStream_t s)
 {
     // few rows per CTA while there are SMs without one; every CTA reads all targets
-    int rows = ceil_div(a.tokens, 4 * 148);
-    rows = rows < 8 ? 8 : rows;
+    const int rows = ceil_div(a.tokens, 4 * 148);
     a.rows_per_cta = rows;
-    return launch_serialized(xent_prep_kernel<T, PL, BWD>, dim3((unsigned)ceil_div(a.tokens, rows)), 256, 0, s, a);
+    a.ctas = ceil_div(a.tokens, rows);
+    const int extra = ceil_div(a.wrows, 8);
+    return launch_serialized(xent_prep_kernel<T, PL, BWD>, dim3((unsigned)(a.ctas + (extra < 148 * 6 ? extra : 148 * 6))), 256, 0, s, a);
 }
 
 template <bool BWD> int prep_any(const PrepArgs &a, int dtype, cudaStream_t s)
@@ -824,8 +814,7 @@ template <typename T, int PL, int NT> int few_launch(const FewArgs &a, cudaStrea
 }
 template <typename T, int PL> int few_any(const FewArgs &a, cudaStream_t s)
 {
-    const int tiles = few_tiles(a.tokens);
-    return tiles == 1 ? few_launch<T, PL, 1>(a, s) : tiles == 2 ? few_launch<T, PL, 2>(a, s) : few_launch<T, PL, 4>(a, s);
+    return few_tiles(a.tokens) == 1 ? few_launch<T, PL, 1>(a, s) : few_launch<T, PL, 2>(a, s);
 }
 
 int few(const void *x, const void *W, const int64_t *targets, float *loss, float *lse, int tokens, int d, int vocab, int64_t ignore, int dtype,
@@ -868,6 +857,8 @@ int xent_fwd(const void *x, const void *W, const int64_t *targets, float *loss, 
     a.x = x; a.targets = targets; a.loss = loss; a.lse = lse;
     a.count = count; a.map = map; a.tgt = tgt; a.xp = xp;
     a.ignore = ignore_index; a.tokens = (int)tokens; a.d = d; a.dp = l.dp; a.vocab = vocab;
+    const int wfirst = vocab < l.piece ? vocab : l.piece;
+    if (!l.direct) { a.W = W; a.wp = (__nv_bfloat16 *)(base + l.w); a.wplane = (size_t)l.piece * l.dp; a.wrows = wfirst; }
     MONARCH_TRY(prep_any<false>(a, dtype, s));
 
     CUtensorMap ma, mb;
@@ -884,7 +875,8 @@ int xent_fwd(const void *x, const void *W, const int64_t *targets, float *loss, 
                 MONARCH_TRY(plane_map(&mb, W, 0, vocab, d, d, (int64_t)vocab * d, 1, l.tn / 2));
                 p.b_n0 = v0;
             } else {
-                MONARCH_TRY(split_w(W, base + l.w, v0, cols, l.piece, d, l.dp, dtype, s));
+                // the preparation has split the first piece; where there are more, another chunk of tokens splits it again
+                if (v0 > 0 || (row0 > 0 && l.piece < vocab)) MONARCH_TRY(split_w(W, base + l.w, v0, cols, l.piece, d, l.dp, dtype, s));
                 MONARCH_TRY(plane_map(&mb, base + l.w, 0, cols, l.dp, l.dp, (int64_t)l.piece * l.dp, l.planes, l.tn / 2));
             }
             const EpiStats::Args e = {part, tlogit, tgt, count, (int)row0, cols, v0, l.halves, half0};
@@ -926,7 +918,7 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
     for (int v0 = 0; v0 < vocab; v0 += l.piece) {
         const int cols = vocab - v0 < l.piece ? vocab - v0 : l.piece;
         if (!l.direct) {
-            MONARCH_TRY(split_w(W, base + l.w, v0, cols, l.piece, d, l.dp, dtype, s));
+            if (v0 > 0) MONARCH_TRY(split_w(W, base + l.w, v0, cols, l.piece, d, l.dp, dtype, s));
             MONARCH_TRY(plane_map(&w_k, base + l.w, 0, cols, l.dp, l.dp, (int64_t)l.piece * l.dp, l.planes, l.tn / 2));
             MONARCH_TRY(plane_map(&w_n, base + l.w, 1, cols, l.dp, l.dp, (int64_t)l.piece * l.dp, l.planes));
         }
@@ -991,6 +983,7 @@ int xent_bwd(const void *x, const void *W, const int64_t *targets, const float *
     a.clse = (float *)(base + l.lse); a.cdl = (float *)(base + l.dl);
     a.xp = (__nv_bfloat16 *)(base + l.x);
     a.ignore = ignore_index; a.tokens = (int)tokens; a.d = d; a.dp = l.dp; a.vocab = vocab;
+    if (!l.direct) { a.W = W; a.wp = (__nv_bfloat16 *)(base + l.w); a.wplane = (size_t)l.piece * l.dp; a.wrows = vocab < l.piece ? vocab : l.piece; }
     MONARCH_TRY(prep_any<true>(a, dtype, s));
     if (dtype == MONARCH_F32)
         return bwd_pieces<float, kP3x3, 3, kP3x3, kP3x3>(l, W, (float *)dx, dW, accumulate, tokens, d, vocab, dtype, base, s);
