@@ -891,18 +891,18 @@ ortho_run_kernel(const __grid_constant__ OrthoMaps maps, const __grid_constant__
     constexpr int kLoads = pg_loads(SCHEME), kSeg = SCHEME == kP3x3 ? pg_seg(SCHEME) : 16;            // bf16 results: 192 steps
 
     const int u0 = p.prod[0].tiles * p.prod[0].splits, u1 = p.prod[1].tiles * p.prod[1].splits, u2 = p.prod[2].tiles * p.prod[2].splits;
-    const long long per_step = (long long)p.blocks * (u0 + u1 + u2), total = per_step * p.steps;
-    auto locate = [&](long long g) {
+    const int per_step = p.blocks * (u0 + u1 + u2), total = per_step * p.steps;
+    auto locate = [&](int g) {
         Tile t;
-        t.step = (int)(g / per_step);
-        long long r = g - t.step * per_step;
+        t.step = g / per_step;
+        int r = g - t.step * per_step;
         t.ph = 0;
         int u = u0;
-        if (r >= (long long)p.blocks * u0) { r -= (long long)p.blocks * u0; t.ph = 1; u = u1; }
-        if (t.ph == 1 && r >= (long long)p.blocks * u1) { r -= (long long)p.blocks * u1; t.ph = 2; u = u2; }
+        if (r >= p.blocks * u0) { r -= p.blocks * u0; t.ph = 1; u = u1; }
+        if (t.ph == 1 && r >= p.blocks * u1) { r -= p.blocks * u1; t.ph = 2; u = u2; }
         const Product &q = p.prod[t.ph];
-        t.block = (int)(r / u);
-        const int v = (int)(r - (long long)t.block * u);
+        t.block = r / u;
+        const int v = r - t.block * u;
         t.tile = v / q.splits;
         t.split = v - t.tile * q.splits;
         t.mirror = 0;
@@ -929,7 +929,7 @@ ortho_run_kernel(const __grid_constant__ OrthoMaps maps, const __grid_constant__
         if (elect_one()) {
             uint32_t slot = 0, phase = 1;
             bool ok = true;
-            for (long long g = pair; ok && g < total; g += npairs) {
+            for (int g = pair; ok && g < total; g += npairs) {
                 const Tile t = locate(g);
                 const Product &q = p.prod[t.ph];
                 // what the products before this one in its block have published
@@ -964,7 +964,7 @@ ortho_run_kernel(const __grid_constant__ OrthoMaps maps, const __grid_constant__
             // ------------------------------------------------------------ even CTA: MMA issuer for the pair
             uint32_t slot = 0, phase = 0, it = 0;
             bool ok = true;
-            for (long long g = pair; ok && g < total; g += npairs) {
+            for (int g = pair; ok && g < total; g += npairs) {
                 const Tile t = locate(g);
                 const Product &q = p.prod[t.ph];
                 const uint32_t idesc = make_idesc_bf16(256, q.tn, q.a_mn, q.b_mn), astep = q.a_mn ? 128 : 2, bstep = q.b_mn ? 128 : 2;
@@ -1007,8 +1007,8 @@ ortho_run_kernel(const __grid_constant__ OrthoMaps maps, const __grid_constant__
         const uint32_t acce_leader = map_to_cta(acce0, 0);
         uint32_t it = 0;
         bool ok = true;
-        PgStage<kRunStage> st = {nullptr, ring0 + kRunSlots * kPgSlotBytes + warp * kRunStage * kPgStageBytes, lane};
-        for (long long g = pair; ok && g < total; g += npairs) {
+        PgStage<kRunStage> st = {nullptr, ring0 + kRunSlots * kPgSlotBytes + warp * kRunStage * kPgStageBytes, lane, 0};
+        for (int g = pair; ok && g < total; g += npairs) {
             const Tile t = locate(g);
             const Product &q = p.prod[t.ph];
             const int tn = q.tn;
@@ -1350,7 +1350,7 @@ int ortho_large(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, 
     p.part = (float *)(base + l.part);
     p.part_units = l.part_units;
     unsigned *next = count + blocks;
-    int64_t units = 0;
+    int64_t units = 0, all = 0;
     for (int i = 0; i < 3; ++i) {
         p.prod[i] = l.prod[i];
         if (l.prod[i].splits > 1) {
@@ -1359,7 +1359,9 @@ int ortho_large(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, 
         }
         const int64_t u = blocks * l.prod[i].tiles * l.prod[i].splits;
         if (u > units) units = u;
+        all += u * steps;
     }
+    if (all > 0x7ffffff0) return MONARCH_ERR_UNSUPPORTED;               // tile numbers are 32 bits
     const auto kern = ortho_run_kernel<T, PL, SCHEME>;
     static PerDeviceCache cache;
     int pairs = cache.get();

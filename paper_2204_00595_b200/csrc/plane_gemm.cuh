@@ -77,19 +77,16 @@ struct PlaneGemm {
     int kdim;                  // contraction length (clipped by *count)
     int a_k0, b_k0;            // first K coordinate of the operands
     int b_n0;                  // first N coordinate of B
-    int a_zstep, b_zstep;      // planes per matrix of a batch in the tensor maps
-    int batches, splits;       // matrices; parts of K, each a product of its own (output index batch * splits + split)
+    int splits;                // parts of K, each a product of its own
     int *splits_out;           // device: null, or `splits` is the most there may be, the kernel chooses (pg_cost) and says so here
     const int *splits_in;      // device: null, or the number of parts
-    int lower;                 // symmetric result: only tiles whose block of 256 columns is not above the diagonal
     int n_fastest;             // neighbouring pairs take neighbouring column tiles (else row tiles)
     int seg;                   // K chunks per accumulation in tensor memory (kernels with PROMOTE)
 };
 
 struct PgTile {
-    int z, row, col;           // output matrix; this thread's row; first of this warp's columns (a half of the tile)
+    int z, row, col;           // part of K; this thread's row; first of this warp's columns (a half of the tile)
     int half;                  // which half tile of the columns that is
-    int mirror;                // `lower`, off the diagonal: the transposed tile is this one's to write too
     int zero;                  // nothing was accumulated
 };
 
@@ -166,11 +163,12 @@ __device__ __forceinline__ bool elect_one()
 // each instruction would touch 32 rows of 16 or 32 bytes.
 //   bf16 planes  32 x 32 pieces (64-byte swizzle) that TMA writes, all planes of a chunk behind one proxy fence (a fence per piece
 //                took 0.5 us each); lane 0 sends and waits
-//   float32      a 32 x 33 tile in the same memory, read back a row at a time, lane = column
+//   float32      32 x 32 tiles of two pieces (128-byte swizzle) that TMA writes or adds to what is there, where rows allow it; else, and
+//                where rows go to places of their own, a 32 x 33 tile read back a row at a time, lane = column
 template <int N> struct PgStage {
     const CUtensorMap *map;
     uint32_t base;
-    int lane;
+    int lane, turn;
     __device__ __forceinline__ uint32_t piece(int i) const { return base + i * kPgStageBytes; }
     // the pieces sent last have been read
     __device__ __forceinline__ void begin() const
@@ -212,6 +210,30 @@ template <int N> struct PgStage {
     __device__ __forceinline__ void close() const
     {
         if (lane == 0) tma_store_commit();
+    }
+    // a float32 tile, the other one of two each time: this lane's row of 32 values, to (x, y, z) of the map or added to what is there; N >= 4
+    __device__ __forceinline__ void tile(const float (&v)[32], int x, int y, int z, bool add)
+    {
+        static_assert(N >= 4 || N == 0, "two tiles");
+        const uint32_t buf = base + turn * 4096;
+        turn ^= 1;
+        if (lane == 0) tma_store_wait_read<1>();
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 128 + ((j ^ (lane & 7)) << 4)), "f"(v[4 * j]), "f"(v[4 * j + 1]),
+                         "f"(v[4 * j + 2]), "f"(v[4 * j + 3])
+                         : "memory");
+        ready();
+        if (lane == 0) {
+            if (add)
+                asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(buf), "r"(x), "r"(y),
+                             "r"(z)
+                             : "memory");
+            else
+                tma_store_3d(map, buf, x, y, z);
+            tma_store_commit();
+        }
     }
     // f(row, value of column `lane` in that row, old(row)) for 32 rows, eight `old` at a time before the first of their `f`; N >= 3
     template <class G, class F> __device__ __forceinline__ void rows(const float (&v)[32], G old, F f) const
@@ -302,49 +324,37 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
         if (p.count_is_k) kdim = min(kdim, n);
         else rows = max(0, min(rows, n - p.row0));
     }
-    const int tn = p.tn, sub = kPgTile / tn;                              // sub: with `lower`, tiles of a block of 256 columns
+    const int tn = p.tn;
     const int mtiles = (rows + kPgTile - 1) / kPgTile, ntiles = (p.cols + tn - 1) / tn;
     const int kchunks = (kdim + kPgChunk - 1) / kPgChunk;
-    const long long plane_tiles = p.lower ? (long long)mtiles * (mtiles + 1) / 2 * sub : (long long)mtiles * ntiles;
+    const int plane_tiles = mtiles * ntiles;
     int splits = p.splits_in != nullptr ? *p.splits_in : p.splits;
     if (p.splits_out != nullptr) {
         // the cheapest number of parts; every warp finds the same one
         long long best = 0x7fffffffffffffffLL;
-        for (int s = lane + 1; s <= p.splits; s += 32) best = min(best, pg_cost(plane_tiles * p.batches, kchunks, s) << 10 | s);
+        for (int s = lane + 1; s <= p.splits; s += 32) best = min(best, pg_cost(plane_tiles, kchunks, s) << 10 | s);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) best = min(best, __shfl_xor_sync(~0u, best, o));
         splits = (int)(best & 1023);
         if (blockIdx.x == 0 && threadIdx.x == 0) *p.splits_out = splits;
     }
     const int per_split = (kchunks + splits - 1) / splits;
-    const long long total = plane_tiles * p.batches * splits;
+    const int total = plane_tiles * splits;                               // below 2^31 (launch_plane_gemm)
     const uint32_t full0 = smem_u32(bars.full), empty0 = smem_u32(bars.empty);
     const uint32_t accf0 = smem_u32(bars.acc_full), acce0 = smem_u32(bars.acc_empty);
     constexpr int kLoads = pg_loads(SCHEME);
     const int seg = PROMOTE ? p.seg : 0x7fffffff;
 
     struct At {
-        int z, split, mt, nt, c0, c1, mirror;
+        int split, mt, nt, c0, c1;
     };
-    auto locate = [&](long long tile) {
+    auto locate = [&](int tile) {
         At a;
-        const int zz = (int)(tile / plane_tiles), t = (int)(tile % plane_tiles);
-        a.z = zz / splits;
-        a.split = zz % splits;
-        a.mirror = 0;
-        if (p.lower) {
-            const int u = t / sub;
-            int m = (int)((sqrtf(8.0f * (float)u + 1.0f) - 1.0f) * 0.5f);
-            while (m * (m + 1) / 2 > u) --m;
-            while ((m + 1) * (m + 2) / 2 <= u) ++m;
-            const int n = u - m * (m + 1) / 2;
-            a.mt = m;
-            a.nt = n * sub + t % sub;
-            a.mirror = n < m;
-        } else {
-            a.mt = p.n_fastest ? t / ntiles : t % mtiles;
-            a.nt = p.n_fastest ? t % ntiles : t / mtiles;
-        }
+        a.split = splits > 1 ? tile / plane_tiles : 0;
+        const int t = tile - a.split * plane_tiles;
+        const int q = t / (p.n_fastest ? ntiles : mtiles), r = t - q * (p.n_fastest ? ntiles : mtiles);
+        a.mt = p.n_fastest ? q : r;
+        a.nt = p.n_fastest ? r : q;
         a.c0 = min(a.split * per_split, kchunks);
         a.c1 = min(a.c0 + per_split, kchunks);
         return a;
@@ -355,7 +365,7 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
         if (elect_one()) {
             uint32_t slot = 0, phase = 1;
             bool ok = true;
-            for (long long tile = pair; ok && tile < total; tile += npairs) {
+            for (int tile = pair; ok && tile < total; tile += npairs) {
                 const At at = locate(tile);
                 const int m0 = p.row0 + at.mt * kPgTile + (int)rank * 128, n0 = p.b_n0 + at.nt * tn + (int)rank * (tn / 2);
                 for (int c = at.c0; ok && c < at.c1; ++c) {
@@ -370,7 +380,7 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
                         // the even CTA announces the bytes of both halves; either CTA's may land first
                         if (rank == 0) mbar_expect_tx(full, (tag[l] & 4) ? tn * (kPgChunk * 2) : 2 * kPgSlotBytes);
                         if (tag[l] & 4) {
-                            const int z = at.z * p.b_zstep + plane;
+                            const int z = plane;
                             if constexpr (BMN) {
                                 tma_load_3d_pair(dst, &tm_b, n0, kb, z, full);
                                 if (tn == 256) tma_load_3d_pair(dst + 8192, &tm_b, n0 + 64, kb, z, full);
@@ -378,7 +388,7 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
                                 tma_load_3d_pair(dst, &tm_b, kb, n0, z, full);
                             }
                         } else {
-                            const int z = at.z * p.a_zstep + plane;
+                            const int z = plane;
                             if constexpr (AMN) {
                                 tma_load_3d_pair(dst, &tm_a, m0, ka, z, full);
                                 tma_load_3d_pair(dst + 8192, &tm_a, m0 + 64, ka, z, full);
@@ -401,7 +411,7 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
             const uint64_t bdesc = BMN ? make_smem_desc(0, 8192, 1024, kSwizzle128) : make_smem_desc(0, 16, 1024, kSwizzle128);
             uint32_t slot = 0, phase = 0, it = 0;
             bool ok = true;
-            for (long long tile = pair; ok && tile < total; tile += npairs) {
+            for (int tile = pair; ok && tile < total; tile += npairs) {
                 const At at = locate(tile);
                 for (int c0 = at.c0; ok && c0 < at.c1; c0 = (at.c1 - c0 > seg) ? c0 + seg : at.c1, ++it) {
                     const int c1 = (at.c1 - c0 > seg) ? c0 + seg : at.c1;
@@ -442,12 +452,11 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
         const uint32_t lane_base = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)((warp >> 2) * (tn / 2));
         uint32_t it = 0;
         bool ok = true;
-        PgStage<(Epi::kStage > 0 ? Epi::kStage : 1)> stage = {&tm_c, ring0 + kPgSlots * kPgSlotBytes + warp * Epi::kStage * kPgStageBytes, lane};
-        for (long long tile = pair; ok && tile < total; tile += npairs) {
+        PgStage<(Epi::kStage > 0 ? Epi::kStage : 1)> stage = {&tm_c, ring0 + kPgSlots * kPgSlotBytes + warp * Epi::kStage * kPgStageBytes, lane, 0};
+        for (int tile = pair; ok && tile < total; tile += npairs) {
             const At at = locate(tile);
             PgTile t;
-            t.z = at.z * splits + at.split;
-            t.mirror = at.mirror;
+            t.z = at.split;
             t.half = at.nt * 2 + (warp >> 2);
             t.row = p.row0 + at.mt * kPgTile + (int)rank * 128 + (warp & 3) * 32 + lane;
             t.col = at.nt * tn + (warp >> 2) * (tn / 2);
@@ -546,6 +555,15 @@ inline int plane_target(CUtensorMap *m, const void *base, int64_t rows, int64_t 
     return encode_tmap_nd(m, base, 2, 3, dims, strides, box, 64);
 }
 
+// as the target of PgStage::tile (cols a multiple of 4)
+inline int tile_target(CUtensorMap *m, const void *base, int64_t rows, int64_t cols, int64_t zstride, int64_t z)
+{
+    const uint64_t dims[3] = {(uint64_t)cols, (uint64_t)rows, (uint64_t)z};
+    const uint64_t strides[2] = {(uint64_t)cols * 4, (uint64_t)zstride * 4};
+    const uint32_t box[3] = {32, 32, 1};
+    return encode_tmap_nd(m, base, 4, 3, dims, strides, box, 128);
+}
+
 // tm_c: the target of an epilogue that has a stage (any map for the others)
 template <int AMN, int BMN, int SCHEME, bool PROMOTE, class Epi>
 int launch_plane_gemm(const CUtensorMap &tm_a, const CUtensorMap &tm_b, const CUtensorMap &tm_c, const PlaneGemm &p, const typename Epi::Args &args, cudaStream_t s)
@@ -570,8 +588,9 @@ int launch_plane_gemm(const CUtensorMap &tm_a, const CUtensorMap &tm_b, const CU
     }
     if (pairs < 1) return MONARCH_ERR_CUDA;
     const long long mt = (p.rows + kPgTile - 1) / kPgTile;
-    const long long total = (p.lower ? mt * (mt + 1) / 2 * (kPgTile / p.tn) : mt * ((p.cols + p.tn - 1) / p.tn)) * p.batches * p.splits;
+    const long long total = mt * ((p.cols + p.tn - 1) / p.tn) * p.splits;
     if (total <= 0) return MONARCH_OK;
+    if (total > 0x7ffffff0) return MONARCH_ERR_UNSUPPORTED;
     const int grid = 2 * (int)(total < pairs ? total : pairs);
     return launch_serialized(kern, dim3((unsigned)grid), kPgThreads, kPgSmem, s, tm_a, tm_b, tm_c, p, args);
 }

@@ -298,14 +298,19 @@ template <int PL> struct EpiGrad {
 
 // rows of float32, stored or added to
 struct EpiStoreF32 {
-    static constexpr int kStage = 3;
+    static constexpr int kStage = 4;
     struct Args {
         float *out;
         int rows, cols, add;
+        int y0;                    // of these rows in the map that TMA writes by; -1: none
     };
     __device__ __forceinline__ void begin(const Args &, const PgTile &) {}
     __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<kStage> &st)
     {
+        if (a.y0 >= 0) {
+            if ((t.row & ~31) < a.rows && t.col + c < a.cols) st.tile(v, t.col + c, a.y0 + (t.row & ~31), 0, a.add);
+            return;
+        }
         const int col = t.col + c + st.lane, row0 = t.row & ~31, rows = col < a.cols ? a.rows - row0 : 0;
         float *out = a.out + (size_t)row0 * a.cols + col;
         st.rows(
@@ -345,17 +350,21 @@ template <typename T> struct EpiDx {
 
 // dx where a few tiles are split along the vocabulary: a sum per part, over the pieces, in float32
 struct EpiDxPart {
-    static constexpr int kStage = 3;
+    static constexpr int kStage = 4;
     struct Args {
         float *acc;                // [parts][tokens][d]
         const int *count;
         size_t part;
-        int d, first;
+        int d, first, tma;
     };
     int n;
     __device__ __forceinline__ void begin(const Args &a, const PgTile &) { n = *a.count; }
     __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<kStage> &st)
     {
+        if (a.tma) {
+            if ((t.row & ~31) < n && t.col + c < a.d) st.tile(v, t.col + c, t.row & ~31, t.z, !a.first);
+            return;
+        }
         const int col = t.col + c + st.lane, row0 = t.row & ~31, rows = col < a.d ? n - row0 : 0;
         float *acc = a.acc + t.z * a.part + (size_t)row0 * a.d + col;
         st.rows(
@@ -787,7 +796,7 @@ PlaneGemm gemm(unsigned *status)
 {
     PlaneGemm g = {};
     g.status = status;
-    g.batches = g.splits = 1;
+    g.splits = 1;
     return g;
 }
 
@@ -870,7 +879,6 @@ int xent_fwd(const void *x, const void *W, const int64_t *targets, float *loss, 
             const int cols = vocab - v0 < l.piece ? vocab - v0 : l.piece;
             PlaneGemm p = gemm(status);
             p.count = count; p.row0 = (int)row0; p.rows = rows; p.cols = cols; p.kdim = d; p.tn = l.tn;
-            p.a_zstep = p.b_zstep = l.planes;
             if (l.direct) {
                 MONARCH_TRY(plane_map(&mb, W, 0, vocab, d, d, (int64_t)vocab * d, 1, l.tn / 2));
                 p.b_n0 = v0;
@@ -905,7 +913,14 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
     int *splits = (int *)(base + l.splits);
     const size_t gplane = (size_t)l.trows * l.piece;
 
-    CUtensorMap x_k, x_n, w_k, w_n, g_m, g_k, g_to;
+    CUtensorMap x_k, x_n, w_k, w_n, g_m, g_k, g_to, dw_to, dx_to;
+    if (d % 4 == 0) {
+        MONARCH_TRY(tile_target(&dw_to, dW, vocab, d, (int64_t)vocab * d, 1));
+        MONARCH_TRY(tile_target(&dx_to, acc, tokens, d, tokens * d, l.dx_parts));
+    } else {
+        MONARCH_TRY(plane_map(&dw_to, xp, 0, tokens, l.dp, l.dp, tokens * l.dp, l.planes));                    // not used
+        dx_to = dw_to;
+    }
     MONARCH_TRY(plane_target(&g_to, g, l.trows, l.piece, l.piece, (int64_t)gplane, l.gplanes));
     MONARCH_TRY(plane_map(&x_k, xp, 0, tokens, l.dp, l.dp, tokens * l.dp, l.planes));
     MONARCH_TRY(plane_map(&x_n, xp, 1, tokens, l.dp, l.dp, tokens * l.dp, l.planes));
@@ -925,22 +940,19 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
         // g
         PlaneGemm p = gemm(status);
         p.count = count; p.rows = (int)tokens; p.cols = cols; p.kdim = d; p.tn = l.tn;
-        p.a_zstep = p.b_zstep = l.planes;
         p.b_n0 = l.direct ? v0 : 0;
         const typename EpiGrad<GP>::Args eg = {cols, v0, tgt, count, clse, cdl};
         MONARCH_TRY((logits<LOGITS, EpiGrad<GP>>(x_k, w_k, g_to, p, eg, true, s)));
         // dW = g^T x
         p = gemm(status);
         p.count = count; p.count_is_k = 1; p.rows = cols; p.cols = d; p.kdim = (int)tokens; p.tn = l.tn_dw;
-        p.a_zstep = GP; p.b_zstep = l.planes;
         p.n_fastest = 1;
         p.seg = pg_seg(DW);
-        const EpiStoreF32::Args ew = {dW + (size_t)v0 * d, cols, d, accumulate};
-        MONARCH_TRY((launch_plane_gemm<1, 1, DW, true, EpiStoreF32>(g_m, x_n, x_n, p, ew, s)));
+        const EpiStoreF32::Args ew = {dW + (size_t)v0 * d, cols, d, accumulate, d % 4 == 0 ? v0 : -1};
+        MONARCH_TRY((launch_plane_gemm<1, 1, DW, true, EpiStoreF32>(g_m, x_n, dw_to, p, ew, s)));
         // dx += g W
         p = gemm(status);
         p.count = count; p.rows = (int)tokens; p.cols = d; p.kdim = cols; p.tn = l.tn_dx;
-        p.a_zstep = GP; p.b_zstep = l.planes;
         p.b_k0 = l.direct ? v0 : 0;
         p.n_fastest = 1;
         p.seg = pg_seg(DX);
@@ -952,8 +964,8 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
             p.splits = l.dx_parts;
             p.splits_out = v0 == 0 ? splits : nullptr;
             p.splits_in = v0 == 0 ? nullptr : splits;
-            const EpiDxPart::Args ex = {acc, count, (size_t)tokens * d, d, v0 == 0};
-            MONARCH_TRY((launch_plane_gemm<0, 1, DX, DX != kP1, EpiDxPart>(g_k, w_n, w_n, p, ex, s)));
+            const EpiDxPart::Args ex = {acc, count, (size_t)tokens * d, d, v0 == 0, d % 4 == 0};
+            MONARCH_TRY((launch_plane_gemm<0, 1, DX, DX != kP1, EpiDxPart>(g_k, w_n, dx_to, p, ex, s)));
         }
     }
     if (l.dx_parts > 1) {
