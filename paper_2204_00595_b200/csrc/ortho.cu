@@ -1,6 +1,8 @@
 // Orthogonalisation of every block of a stack by Newton-Schulz products, and the optimiser step that uses it:
 //   X0 = U / (||U||_F + 1e-7);  steps times: S = X X^T (X^T X where rows > cols), X <- a X + (b S + c S^2) X
 // for the gradients of the factors L, R (each block is a matrix of its own: with orthogonal blocks M = P L P^T R is orthogonal).
+#include <type_traits>
+
 #include "plane_gemm.cuh"
 
 namespace monarch {
@@ -121,8 +123,9 @@ struct Walk {
     }
 };
 
-// ------------------------------------------------------------------------------------------------ blocks that fit one SM
-// X (k x n, the smaller side first) twice and one k x k matrix in shared memory; S lives in the buffer of the next X.
+// ------------------------------------------------------------------------------------------------ long, narrow blocks
+// k up to 32, n over 256: X (k x n, the smaller side first) twice and one k x k matrix in shared memory in fp32, plain FMA; S lives in
+// the buffer of the next X.  A few MACs per value: tensor core tiles of 128 or 256 rows would be nearly empty.
 constexpr int kSmallThreads = 256;
 
 __host__ __device__ constexpr int pad4(int v) { return (v + 3) / 4 * 4; }
@@ -133,7 +136,7 @@ __host__ __device__ inline size_t small_floats(int k, int n)
     return (size_t)kp * (2 * ldn) + (size_t)kp * ldk;
 }
 constexpr size_t kSmallMax = 220 * 1024;
-bool fits_small(int k, int n) { return small_floats(k, n) * 4 <= kSmallMax; }
+bool fits_small(int k, int n) { return k <= 32 && small_floats(k, n) * 4 <= kSmallMax; }
 
 template <typename T>
 __global__ void __launch_bounds__(kSmallThreads) ortho_small_kernel(const Io<T> io, int rows, int cols, int steps)
@@ -247,9 +250,8 @@ __global__ void __launch_bounds__(kSmallThreads) ortho_small_kernel(const Io<T> 
 // ------------------------------------------------------------------------------------------------ blocks up to 64 x 256
 // One CTA per block, everything on chip: X, S and P = b S + c S^2 are bf16 planes in shared memory (PL = 2 for bf16 results, 3 for
 // fp32), their fp32 values stay in the registers of the thread that holds them as an accumulator, warp-level MMAs (m16n8k16).
-// S is symmetric, so S and P serve as either operand as stored; only P X needs X transposed (ldmatrix.trans).  tcgen05 is little gain
-// here: 15 dependent products of 64 x 64 x 64.  128 blocks of 64 x 64, optimiser step: bf16 15.3 us (1.8 a step), fp32 22.2 (3.3 a step);
-// with fp32 FMA 75.
+// S is symmetric, so S and P serve as either operand as stored; only P X needs X transposed (ldmatrix.trans).  For k up to 32, and for
+// n of 129 to 256 with k up to 64, where X does not fit what the kernel below has; 32 x 32, bf16, 64 blocks: XX us.
 // KP, NP: k and n rounded up; warps: KP / 16 rows of tiles times two column halves.
 template <int KP, int NP, int PL> struct BlockCfg {
     static constexpr int kRows = KP / 16, kThreads = kRows * 2 * 32;
@@ -432,28 +434,32 @@ template <typename T, int PL> int ortho_block(const Io<T> &io, int64_t blocks, i
         if (n <= 128) return launch_block<T, 32, 128, PL>(io, blocks, rows, cols, steps, s);
         return launch_block<T, 32, 256, PL>(io, blocks, rows, cols, steps, s);
     }
-    if (n <= 64) return launch_block<T, 64, 64, PL>(io, blocks, rows, cols, steps, s);
-    if (n <= 128) return launch_block<T, 64, 128, PL>(io, blocks, rows, cols, steps, s);
     return launch_block<T, 64, 256, PL>(io, blocks, rows, cols, steps, s);
 }
 
 // ------------------------------------------------------------------------------------------------ blocks up to 128 x 128
-// One CTA per block on the tcgen05 tensor cores, everything on chip: X and S in registers (thread = row and 16 columns of either
-// half), accumulators in tensor memory, operands as planes: the second one in shared memory as 128 x 64 slabs in the 128-byte
-// swizzle (K-major as stored; MN-major for the X of P X, whose rows are K), the first one in tensor memory, whose rows are the
-// threads' (both from shared memory take 8 KB for the 64 cycles of an MMA of 128 x 128 x 16, and 6 for the 32 of half of it: all
-// that an SM can read).  There is room there for two planes; of three, the third is read from shared
-// memory.  All 128 rows and columns are computed; those behind the block are zeros.
+// One CTA per block on the tcgen05 tensor cores, everything on chip: X and S in registers (thread = row and a quarter of either
+// column half), accumulators in tensor memory, operands as planes: the second one in shared memory as slabs of 64 columns in the
+// 128-byte swizzle (K-major as stored; MN-major for the X of P X, whose rows are K), the first one in tensor memory, whose rows are
+// the threads' (both from shared memory take 8 KB for the 64 cycles of an MMA of 128 x 128 x 16: all that an SM can read).  There is
+// room there for two planes; of three, the third is read from shared memory.  KP x NP: k and n rounded up to 64 or 128; all of it is
+// computed, what stands behind the block is zeros.  (KP = 64: the MMAs have 128 rows all the same, nobody reads the others.)
 //
-// A product is 8 K steps of 128 x 128 x 16 for each plane product, then: tensor memory -> fp32 -> planes of the next operand.  The
-// two overlap by column halves: the K steps that read the first 64 columns of an operand are issued as soon as those are written,
-// the others finish the first half of the result before the second, so that its values are converted meanwhile.
-// What a conversion overwrites (P over S, X over X) is the half that no MMA still under way reads.
+// After a product: tensor memory -> fp32 -> planes of the next operand.  Products and conversions overlap by column halves: the K
+// steps that read the first half of an operand are issued as soon as it is written, the others finish the first half of a result of
+// 128 columns before the second, so that its values are converted meanwhile.  What a conversion overwrites (P over S, X over X) is the
+// half that no MMA still under way reads.
 // Measured, 128 blocks of 128 x 128, optimiser step: bf16 27.5 us (3.7 a step: 2360 cycles a product, 1536 of them MMAs of three
 // plane products), fp32 43.6 (6.6 a step); with fp32 FMA 525.  The one thread that issues has to keep its operands in uniform
 // registers (elect_one): picked as thread 0 it took 60 cycles per MMA, 33.3 and 51.1 us.
-constexpr int kTcThreads = 512, kTcPlane = 128 * 128 * 2, kTcSlab = 128 * 128;
-template <int PL> constexpr int kTcSmem = 2 * PL * kTcPlane + 1024;
+constexpr int kTcThreads = 512;
+template <int KP, int NP, int PL> struct TcCfg {
+    static constexpr int kSlab = KP * 128;                                   // KP rows of 64 columns
+    static constexpr int kXPlane = KP * NP * 2, kSPlane = KP * KP * 2;
+    // MMAs that take the first operand's third plane from shared memory read 128 rows: with 64, what stands behind as well
+    static constexpr int kSmem = PL * (kXPlane + kSPlane) + (PL > 2 && KP < 128 ? kSlab : 0) + 1024;
+    static constexpr int kCs = KP / 8, kCx = NP / 8;                         // columns of a thread in a half of S, of X
+};
 
 struct KMajor { static constexpr bool value = false; };
 struct NMajor { static constexpr bool value = true; };
@@ -467,29 +473,47 @@ __device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uin
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8])
+template <int C> __device__ __forceinline__ void tmem_put(uint32_t taddr, const uint32_t (&r)[C])
 {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
-                 "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-                 : "memory");
+    static_assert(C == 4 || C == 8, "8 or 16 columns of packed values");
+    if constexpr (C == 8)
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+                     "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                     : "memory");
+    else
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// C columns of this thread's lane
+template <int C> __device__ __forceinline__ void tmem_get(uint32_t taddr, float (&f)[C])
+{
+    static_assert(C == 8 || C == 16, "8 or 16 columns");
+    if constexpr (C == 16) {
+        tmem_ask16(taddr, f);
+        tmem_ready(f);
+    } else {
+        tmem_ld8(taddr, reinterpret_cast<uint32_t (&)[8]>(f));
+        asm volatile("tcgen05.wait::ld.sync.aligned;"
+                     : "+f"(f[0]), "+f"(f[1]), "+f"(f[2]), "+f"(f[3]), "+f"(f[4]), "+f"(f[5]), "+f"(f[6]), "+f"(f[7])::"memory");
+    }
+}
 
-// K half `kh` of A B for columns n0 .. n0 + N of B, all plane products, the small ones first.  A: planes 0 and 1 in tensor memory
-// (64 columns each), plane 2 in shared memory at `a2`.
-template <int PL, bool BMN, int N> __device__ __forceinline__ void tc_part(uint32_t d, uint32_t a, uint32_t a2, uint32_t b, int kh, int n0, uint32_t more)
+// K columns k0 .. k0 + 16 STEPS of A B for columns n0 .. n0 + N of B, all plane products, the small ones first.  A: planes 0 and 1 in
+// tensor memory (64 columns each), plane 2 in shared memory at `a2`; planes of A there `aplane` bytes apart, of B `bplane`.
+template <int PL, bool BMN, int N, int STEPS, int SLAB>
+__device__ __forceinline__ void tc_part(uint32_t d, uint32_t a, uint32_t a2, uint32_t aplane, uint32_t b, uint32_t bplane, int k0, int n0, uint32_t more)
 {
     constexpr uint32_t idesc = make_idesc_bf16(128, N, 0, BMN);
-    a += kh * 32;
-    a2 += 2 * kTcPlane + kh * kTcSlab;
-    b += BMN ? (n0 >> 6) * kTcSlab + kh * 64 * 128 : kh * kTcSlab + n0 * 128;
+    a += k0 / 2;
+    a2 += 2 * aplane + (k0 >> 6) * SLAB + (k0 & 63) * 2;
+    b += BMN ? (n0 >> 6) * SLAB + k0 * 128 : (k0 >> 6) * SLAB + (k0 & 63) * 2 + n0 * 128;
 #pragma unroll
     for (int o = PL - 1; o >= 0; --o)
 #pragma unroll
         for (int q = o; q >= 0; --q) {
-            const uint64_t bd = BMN ? make_smem_desc(b + (o - q) * kTcPlane, kTcSlab, 1024, kSwizzle128) : make_smem_desc(b + (o - q) * kTcPlane, 16, 1024, kSwizzle128);
+            const uint64_t bd = BMN ? make_smem_desc(b + (o - q) * bplane, SLAB, 1024, kSwizzle128) : make_smem_desc(b + (o - q) * bplane, 16, 1024, kSwizzle128);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < STEPS; ++k) {
                 if (q < 2) mma_f16_ts(d + n0, a + q * 64 + k * 8, bd + (BMN ? 128 : 2) * k, idesc, more);
                 else mma_f16_ss(d + n0, make_smem_desc(a2, 16, 1024, kSwizzle128) + 2 * k, bd + (BMN ? 128 : 2) * k, idesc, more);
                 more = 1;
@@ -497,43 +521,45 @@ template <int PL, bool BMN, int N> __device__ __forceinline__ void tc_part(uint3
         }
 }
 
-// 16 values of a row (columns c .. c + 15 of a half) as planes: the first operand (tensor memory at `a`, the third plane in shared
-// memory), and if BOTH the second one (shared memory)
-template <int PL, bool BOTH> __device__ __forceinline__ void tc_put(uint32_t planes, uint32_t a, int row, int half, int c, float (&v)[16])
+// C values of a row from column `col` as planes: the first operand (tensor memory at `a`, the third plane in shared memory), and if
+// BOTH the second one (shared memory)
+template <int PL, bool BOTH, int SLAB, int C> __device__ __forceinline__ void tc_put(uint32_t planes, uint32_t plane, uint32_t a, int row, int col, float (&v)[C])
 {
 #pragma unroll
     for (int q = 0; q < PL; ++q) {
-        uint32_t w[8];
+        uint32_t w[C / 2];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < C / 2; ++e) {
             w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
             v[2 * e] -= __uint_as_float(w[e] << 16);
             v[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
         }
-        if (q < 2) tmem_st8(a + q * 64, w);
+        if (q < 2) tmem_put(a + q * 64 + col / 2, w);
         if (BOTH || q >= 2) {
-            const uint32_t at = planes + q * kTcPlane + half * kTcSlab + row * 128;
+            const uint32_t at = planes + q * plane + (col >> 6) * SLAB + row * 128;
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + ((((c >> 3) + j) ^ (row & 7)) << 4)), "r"(w[4 * j]), "r"(w[4 * j + 1]),
+            for (int j = 0; j < C / 8; ++j)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + (((((col & 63) >> 3) + j) ^ (row & 7)) << 4)), "r"(w[4 * j]), "r"(w[4 * j + 1]),
                              "r"(w[4 * j + 2]), "r"(w[4 * j + 3])
                              : "memory");
         }
     }
 }
 
-template <typename T, int PL>
+template <typename T, int PL, int KP, int NP>
 __global__ void __launch_bounds__(kTcThreads, 1) ortho_tc_kernel(const Io<T> io, int rows, int cols, int steps, unsigned *status)
 {
+    using C = TcCfg<KP, NP, PL>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bar_s[2];
     __shared__ double s_norm[kTcThreads / 32];
     __shared__ uint32_t tmem_base_s;
     __shared__ int dead_s;
-    const uint32_t X = (smem_u32(smem_raw) + 1023u) & ~1023u, S = X + PL * kTcPlane, bar = smem_u32(bar_s);
-    float *stage = reinterpret_cast<float *>(smem_raw + (X - smem_u32(smem_raw)));       // 128 x 128 floats over the planes of X
+    const uint32_t X = (smem_u32(smem_raw) + 1023u) & ~1023u, S = X + PL * C::kXPlane, bar = smem_u32(bar_s);
+    float *stage = reinterpret_cast<float *>(smem_raw + (X - smem_u32(smem_raw)));       // KP x NP floats over the planes of X
     const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;     // the same in all lanes, for the compiler too
-    const int row = (warp & 3) * 32 + lane, c0 = (warp >> 2) * 16;
+    const int row = (warp & 3) * 32 + lane, cs = (warp >> 2) * C::kCs, cx = (warp >> 2) * C::kCx;
+    const bool holds = KP == 128 || (warp & 3) < KP / 32;                                 // this warp has rows
     const bool wide = rows <= cols;
     const int size = rows * cols;
     const size_t base = (size_t)blockIdx.x * size;
@@ -549,8 +575,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) ortho_tc_kernel(const Io<T> io,
         tmem_alloc(smem_u32(&tmem_base_s), 512);
         tmem_relinquish();
     }
-    if (size < 128 * 128)
-        for (int i = tid * 4; i < 128 * 128; i += kTcThreads * 4) *reinterpret_cast<float4 *>(stage + i) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (size < KP * NP)
+        for (int i = tid * 4; i < KP * NP; i += kTcThreads * 4) *reinterpret_cast<float4 *>(stage + i) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -558,17 +584,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) ortho_tc_kernel(const Io<T> io,
     depend_wait();
     depend_launch();
 
-    // X[i][j] at stage[i * 128 + (j ^ (i & 31))]: consecutive values of G and one column of all rows are both in different banks
+    // X[i][j] at stage[i * NP + (j ^ (i & 31))]: consecutive values of G and one column of all rows are both in different banks
     double q = 0.0;
     const bool four = cols % 4 == 0;           // four values of a row at a time
     Walk at(four ? 4 * tid : tid, four ? 4 * kTcThreads : kTcThreads, cols);
     if (four) {
-        typename Io<T>::In4 f[8];
+        constexpr int kMost = KP * NP / 4 / kTcThreads;
+        typename Io<T>::In4 f[kMost];
 #pragma unroll
-        for (int a = 0; a < 8; ++a)
+        for (int a = 0; a < kMost; ++a)
             if ((tid + a * kTcThreads) * 4 < size) f[a] = io.fetch4(base + (tid + a * kTcThreads) * 4);
 #pragma unroll
-        for (int a = 0; a < 8; ++a) {
+        for (int a = 0; a < kMost; ++a) {
             if ((tid + a * kTcThreads) * 4 >= size) break;
             float u[4];
             io.u4(base + (tid + a * kTcThreads) * 4, f[a], u);
@@ -576,7 +603,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) ortho_tc_kernel(const Io<T> io,
             for (int b = 0; b < 4; ++b) {
                 const int i = wide ? at.r : at.c + b, j = wide ? at.c + b : at.r;
                 q += (double)u[b] * u[b];
-                stage[i * 128 + (j ^ (i & 31))] = u[b];
+                stage[i * NP + (j ^ (i & 31))] = u[b];
             }
             at.next();
         }
@@ -592,7 +619,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) ortho_tc_kernel(const Io<T> io,
             const int i = wide ? at.r : at.c, j = wide ? at.c : at.r;
             const float u = io.u(base + e0 + a * kTcThreads, f[a], true);
             q += (double)u * u;
-            stage[i * 128 + (j ^ (i & 31))] = u;
+            stage[i * NP + (j ^ (i & 31))] = u;
             at.next();
         }
     }
@@ -604,15 +631,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) ortho_tc_kernel(const Io<T> io,
 #pragma unroll
     for (int w = 0; w < kTcThreads / 32; ++w) q += s_norm[w];
     const double inv = 1.0 / (sqrt(q) + (double)kEps);                       // fp64: norms beyond the fp32 range
-    float x[2][16];
+    float x[2][C::kCx];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) x[h][j] = (float)((double)stage[row * 128 + ((h * 64 + c0 + j) ^ lane)] * inv);
+        for (int j = 0; j < C::kCx; ++j) x[h][j] = holds ? (float)((double)stage[row * NP + ((h * (NP / 2) + cx + j) ^ lane)] * inv) : 0.0f;
     __syncthreads();
 
-    const uint32_t d_s = tmem, d_t = tmem + 128, d_x = tmem + 256, A = tmem + 384;
-    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, mine = lanes + c0, a_mine = A + lanes + c0 / 2;
+    // the first operand of P X (and of S S) beside that of X X^T where their halves are not the same columns: X is written while P is read
+    const uint32_t d_s = tmem, d_t = tmem + KP, d_x = tmem + 256, a_x = tmem + 384, a_s = KP == NP ? a_x : tmem + 128;
+    static_assert(KP == NP || KP == 64, "room for a second first operand");
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     uint32_t phase = 0;
     bool ok = true, stop = false;               // stop: some thread's wait ran out, the same in all threads
     auto written = [&]() {                     // this half of the operands is written, and its accumulators are read
@@ -626,71 +655,84 @@ __global__ void __launch_bounds__(kTcThreads, 1) ortho_tc_kernel(const Io<T> io,
         if (!mbar_wait(bar + h * 8, phase, status, dead, kErrMmaWait)) ok = false;
         tc_fence_after();
     };
-    // MMAs of a product with B at `b` (the third plane of A at `a2`): what the first half of the operands allows, or the rest
-    auto issue = [&](auto bmn, int h, uint32_t d, uint32_t a2, uint32_t b) {
+    // the MMAs of a product of N columns over K: what the first half of the operands allows (h = 0), or the rest
+    auto issue = [&](auto bmn, auto n, auto k, int h, uint32_t d, uint32_t A, uint32_t a2, uint32_t aplane, uint32_t b, uint32_t bplane) {
         if (warp != 0 || !elect_one()) return;
         constexpr bool kBmn = decltype(bmn)::value;
+        constexpr int N = decltype(n)::value, K = decltype(k)::value, kSteps = K / 32;
         if (h == 0) {
-            tc_part<PL, kBmn, 128>(d, A, a2, b, 0, 0, 0);
-        } else {
-            tc_part<PL, kBmn, 64>(d, A, a2, b, 1, 0, 1);
+            tc_part<PL, kBmn, N, kSteps, C::kSlab>(d, A, a2, aplane, b, bplane, 0, 0, 0);
+        } else if (N == 128) {
+            tc_part<PL, kBmn, 64, kSteps, C::kSlab>(d, A, a2, aplane, b, bplane, K / 2, 0, 1);
             mma_commit(bar);
-            tc_part<PL, kBmn, 64>(d, A, a2, b, 1, 64, 1);
+            tc_part<PL, kBmn, 64, kSteps, C::kSlab>(d, A, a2, aplane, b, bplane, K / 2, 64, 1);
+            mma_commit(bar + 8);
+        } else {
+            tc_part<PL, kBmn, N, kSteps, C::kSlab>(d, A, a2, aplane, b, bplane, K / 2, 0, 1);
+            mma_commit(bar);
             mma_commit(bar + 8);
         }
     };
+    using Kp = std::integral_constant<int, KP>;
+    using Np = std::integral_constant<int, NP>;
+    auto gram = [&](int h) { issue(KMajor(), Kp(), Np(), h, d_s, a_x, X, C::kXPlane, X, C::kXPlane); };
+    auto square = [&](int h) { issue(KMajor(), Kp(), Kp(), h, d_t, a_s, S, C::kSPlane, S, C::kSPlane); };
+    auto update = [&](int h) { issue(NMajor(), Np(), Kp(), h, d_x, a_s, S, C::kSPlane, X, C::kXPlane); };
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        float v[16];
+        float v[C::kCx];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = x[h][j];
-        tc_put<PL, true>(X, a_mine + h * 32, row, h, c0, v);
+        for (int j = 0; j < C::kCx; ++j) v[j] = x[h][j];
+        if (holds) tc_put<PL, true, C::kSlab>(X, C::kXPlane, a_x + lanes, row, h * (NP / 2) + cx, v);
     }
     written();
-    issue(KMajor(), 0, d_s, X, X);
-    issue(KMajor(), 1, d_s, X, X);
+    gram(0);
+    gram(1);
     for (int it = 0; it < steps; ++it) {
-        float s[2][16];
+        float s[2][C::kCs];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            float v[16];
             arrived(h);
-            tmem_ask16(d_s + mine + h * 64, v);
-            tmem_ready(v);
+            if (holds) {
+                float v[C::kCs];
+                tmem_get(d_s + lanes + h * (KP / 2) + cs, v);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) s[h][j] = v[j];
-            tc_put<PL, true>(S, a_mine + h * 32, row, h, c0, v);
+                for (int j = 0; j < C::kCs; ++j) s[h][j] = v[j];
+                tc_put<PL, true, C::kSlab>(S, C::kSPlane, a_s + lanes, row, h * (KP / 2) + cs, v);
+            }
             written();
-            issue(KMajor(), h, d_t, S, S);
+            square(h);
         }
         phase ^= 1;
         // P = b S + c S^2
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            float v[16];
             arrived(h);
-            tmem_ask16(d_t + mine + h * 64, v);
-            tmem_ready(v);
+            if (holds) {
+                float v[C::kCs];
+                tmem_get(d_t + lanes + h * (KP / 2) + cs, v);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) v[j] = fmaf(kB, s[h][j], kC * v[j]);
-            tc_put<PL, false>(S, a_mine + h * 32, row, h, c0, v);
+                for (int j = 0; j < C::kCs; ++j) v[j] = fmaf(kB, s[h][j], kC * v[j]);
+                tc_put<PL, false, C::kSlab>(S, C::kSPlane, a_s + lanes, row, h * (KP / 2) + cs, v);
+            }
             written();
-            issue(NMajor(), h, d_x, S, X);
+            update(h);
         }
         phase ^= 1;
         // X = a X + P X
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            float v[16];
             arrived(h);
-            tmem_ask16(d_x + mine + h * 64, v);
-            tmem_ready(v);
+            if (holds) {
+                float v[C::kCx];
+                tmem_get(d_x + lanes + h * (NP / 2) + cx, v);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) x[h][j] = v[j] = fmaf(kA, x[h][j], v[j]);
+                for (int j = 0; j < C::kCx; ++j) x[h][j] = v[j] = fmaf(kA, x[h][j], v[j]);
+                if (it + 1 < steps) tc_put<PL, true, C::kSlab>(X, C::kXPlane, a_x + lanes, row, h * (NP / 2) + cx, v);
+            }
             if (it + 1 < steps) {
-                tc_put<PL, true>(X, a_mine + h * 32, row, h, c0, v);
                 written();
-                issue(KMajor(), h, d_s, X, X);
+                gram(h);
             }
         }
         phase ^= 1;
@@ -702,25 +744,27 @@ __global__ void __launch_bounds__(kTcThreads, 1) ortho_tc_kernel(const Io<T> io,
     tc_fence_before();
     __syncthreads();
     if (warp == 0) tmem_dealloc(tmem, 512);
+    if (holds)
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) stage[row * 128 + ((h * 64 + c0 + j) ^ lane)] = x[h][j];
+            for (int j = 0; j < C::kCx; ++j) stage[row * NP + ((h * (NP / 2) + cx + j) ^ lane)] = x[h][j];
     __syncthreads();
     at = Walk(four ? 4 * tid : tid, four ? 4 * kTcThreads : kTcThreads, cols);
     if (four) {
-        float w[8][4];
+        constexpr int kMost = KP * NP / 4 / kTcThreads;
+        float w[kMost][4];
 #pragma unroll
-        for (int a = 0; a < 8; ++a)
+        for (int a = 0; a < kMost; ++a)
             if ((tid + a * kTcThreads) * 4 < size) io.old4(base + (tid + a * kTcThreads) * 4, w[a]);
 #pragma unroll
-        for (int a = 0; a < 8; ++a) {
+        for (int a = 0; a < kMost; ++a) {
             if ((tid + a * kTcThreads) * 4 >= size) break;
             float o[4];
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
                 const int i = wide ? at.r : at.c + b, j = wide ? at.c + b : at.r;
-                o[b] = stage[i * 128 + (j ^ (i & 31))];
+                o[b] = stage[i * NP + (j ^ (i & 31))];
             }
             io.write4(base + (tid + a * kTcThreads) * 4, o, w[a]);
             at.next();
@@ -735,10 +779,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) ortho_tc_kernel(const Io<T> io,
         for (int a = 0; a < 8; ++a) {
             if (e0 + a * kTcThreads >= size) break;
             const int i = wide ? at.r : at.c, j = wide ? at.c : at.r;
-            io.write(base + e0 + a * kTcThreads, stage[i * 128 + (j ^ (i & 31))], w[a]);
+            io.write(base + e0 + a * kTcThreads, stage[i * NP + (j ^ (i & 31))], w[a]);
             at.next();
         }
     }
+}
+
+template <typename T, int PL, int KP, int NP>
+int launch_tc(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, void *ws, cudaStream_t s)
+{
+    return launch_serialized(ortho_tc_kernel<T, PL, KP, NP>, dim3((unsigned)blocks), kTcThreads, TcCfg<KP, NP, PL>::kSmem, s, io, rows, cols, steps, (unsigned *)ws);
 }
 
 // ------------------------------------------------------------------------------------------------ larger blocks
@@ -1335,6 +1385,13 @@ int ortho_large(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, 
     MONARCH_TRY(plane_target(&m.s_to, sp.at, l.k, l.k, l.ldk, kz, z));
     MONARCH_TRY(plane_target(&m.p_to, pp.at, l.k, l.k, l.ldk, kz, z));
 
+    int64_t units = 0, all = 0;
+    for (const Product &q : l.prod) {
+        const int64_t u = blocks * q.tiles * q.splits;
+        if (u > units) units = u;
+        all += u * steps;
+    }
+    if (all > 0x7ffffff0) return MONARCH_ERR_UNSUPPORTED;               // tile numbers are 32 bits
     MONARCH_TRY(launch_serialized(norm_kernel<T>, dim3((unsigned)(blocks * l.parts)), 256, 0, s, io, norm, l.parts, (int64_t)rows * cols, count, l.counters));
     int64_t ctas = ceil_div((int64_t)rows * cols, 4096), most = 148 * 8 / blocks + 1;
     if (ctas > most) ctas = most;
@@ -1350,18 +1407,13 @@ int ortho_large(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, 
     p.part = (float *)(base + l.part);
     p.part_units = l.part_units;
     unsigned *next = count + blocks;
-    int64_t units = 0, all = 0;
     for (int i = 0; i < 3; ++i) {
         p.prod[i] = l.prod[i];
         if (l.prod[i].splits > 1) {
             p.prod[i].parts_done = next;
             next += blocks * l.prod[i].tiles * 16;
         }
-        const int64_t u = blocks * l.prod[i].tiles * l.prod[i].splits;
-        if (u > units) units = u;
-        all += u * steps;
     }
-    if (all > 0x7ffffff0) return MONARCH_ERR_UNSUPPORTED;               // tile numbers are 32 bits
     const auto kern = ortho_run_kernel<T, PL, SCHEME>;
     static PerDeviceCache cache;
     int pairs = cache.get();
@@ -1390,16 +1442,31 @@ int ortho_large(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, 
     return MONARCH_OK;
 }
 
+// Which kernel serves blocks whose smaller side is k and larger side n; not by their number, so that a workspace for many blocks
+// serves fewer.
+enum Kernel { kWarpMma, kTcgen05, kFma, kRun };
+Kernel kernel_for(int k, int n)
+{
+    if (k > 32 && n <= 128) return kTcgen05;
+    if (fits_block(k, n)) return kWarpMma;
+    return fits_small(k, n) ? kFma : kRun;
+}
+
 template <typename T, int PL, int SCHEME>
 int ortho_any(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, int dtype, void *ws, cudaStream_t s)
 {
     if (blocks == 0) return MONARCH_OK;
     const int k = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
-    if (fits_block(k, n)) return ortho_block<T, PL>(io, blocks, rows, cols, steps, s);
-    if (n <= 128)
-        return launch_serialized(ortho_tc_kernel<T, PL>, dim3((unsigned)blocks), kTcThreads, kTcSmem<PL>, s, io, rows, cols, steps, (unsigned *)ws);
-    if (!fits_small(k, n)) return ortho_large<T, PL, SCHEME>(io, blocks, rows, cols, steps, dtype, ws, s);
-    return launch_serialized(ortho_small_kernel<T>, dim3((unsigned)blocks), kSmallThreads, (int)(small_floats(k, n) * 4), s, io, rows, cols, steps);
+    switch (kernel_for(k, n)) {
+        case kTcgen05:
+            if (k > 64) return launch_tc<T, PL, 128, 128>(io, blocks, rows, cols, steps, ws, s);
+            if (n > 64) return launch_tc<T, PL, 64, 128>(io, blocks, rows, cols, steps, ws, s);
+            return launch_tc<T, PL, 64, 64>(io, blocks, rows, cols, steps, ws, s);
+        case kWarpMma: return ortho_block<T, PL>(io, blocks, rows, cols, steps, s);
+        case kFma:
+            return launch_serialized(ortho_small_kernel<T>, dim3((unsigned)blocks), kSmallThreads, (int)(small_floats(k, n) * 4), s, io, rows, cols, steps);
+        default: return ortho_large<T, PL, SCHEME>(io, blocks, rows, cols, steps, dtype, ws, s);
+    }
 }
 
 }  // namespace
@@ -1408,7 +1475,7 @@ int ortho_any(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, in
 size_t ortho_workspace_bytes(int64_t blocks, int32_t rows, int32_t cols, int dtype)
 {
     const int k = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
-    return tc::fits_small(k, n) ? (size_t)MONARCH_STATUS_BYTES : tc::large_layout(blocks, rows, cols, dtype).total;
+    return tc::kernel_for(k, n) != tc::kRun ? (size_t)MONARCH_STATUS_BYTES : tc::large_layout(blocks, rows, cols, dtype).total;
 }
 
 int orthogonalize(const void *G, void *O, int64_t blocks, int32_t rows, int32_t cols, int32_t steps, int dtype, void *ws, cudaStream_t s)

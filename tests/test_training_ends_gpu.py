@@ -430,6 +430,7 @@ BLOCKS = [
     (1, 1, 1), (5, 1, 9), (5, 9, 1), (3, 2, 2), (7, 3, 5), (4, 16, 16), (33, 8, 12), (3, 17, 15), (2, 31, 33), (6, 32, 32), (3, 33, 80),
     (2, 64, 64), (5, 63, 65), (2, 64, 20), (2, 100, 127), (2, 128, 128), (1, 127, 128), (2, 128, 64), (3, 4, 1000), (3, 1000, 4), (1, 129, 129),
     (2, 130, 256), (2, 256, 130), (1, 200, 301), (1, 301, 200), (2, 256, 256), (1, 512, 640), (1, 65, 2000), (1, 2000, 65), (1, 1030, 1031),
+    (2, 1, 20000), (1, 20000, 2), (3, 64, 200), (2, 200, 40), (5, 32, 256), (2, 257, 32), (200, 33, 64), (150, 5, 6), (2, 64, 129), (90, 130, 131),
 ]
 
 
@@ -464,6 +465,33 @@ def test_blocks_stand_alone(rows, cols):
     near(O[fine], newton_schulz(G[fine].double()), "f32", "O")
     want = newton_schulz(G[5:6].double())                  # about a^5 U / 1e-7
     near(O[5:6], want, "f32", "O")
+
+
+def test_two_streams_at_once():
+    """Calls that overlap on the GPU, each with a workspace of its own; the stacks of large blocks are launches whose CTAs wait for
+    one another."""
+    T, d, V = 700, 256, 5000
+    x, W, y, dloss = make(T, d, V, "bf16", 0.1, seed=30)
+    G = [gradient(3, 300, 520, 31 + i).to(dt) for i, dt in enumerate((torch.bfloat16, torch.float32))]
+    want = [ortho(g) for g in G]
+    loss, lse = forward(x, W, y)
+    dx, dW = backward(x, W, y, lse, dloss)
+    ws = [P.Workspace(P.monarch_ortho_workspace_bytes(3, 300, 520, c)) for c in (P.BF16, P.F32)]
+    wf, wb = P.Workspace(P.monarch_xent_workspace_bytes(T, d, V, P.BF16)), P.Workspace(P.monarch_xent_bwd_workspace_bytes(T, d, V, P.BF16))
+    out = [torch.empty_like(g) for g in G]
+    l2, s2, dx2, dW2 = torch.empty_like(loss), torch.empty_like(lse), torch.empty_like(dx), torch.empty_like(dW)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i in range(2):
+            P.monarch_orthogonalize(G[i], out[i], 3, 300, 520, 5, ws[i], streams[i])
+        P.monarch_xent_fwd(x, W, y, l2, s2, T, d, V, IGNORE, wf, streams[2])
+        P.monarch_xent_bwd(x, W, y, s2, dloss, dx2, dW2, 0, T, d, V, IGNORE, wb, streams[2])
+    torch.cuda.synchronize()
+    for w in ws + [wf, wb]:
+        assert P.monarch_last_device_status(w) == 0
+    for a, b in zip(want + [loss, lse, dx, dW], out + [l2, s2, dx2, dW2]):
+        assert torch.equal(a.view(-1), b.view(-1))
 
 
 def test_result_is_nearly_orthogonal():
