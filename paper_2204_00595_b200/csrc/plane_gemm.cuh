@@ -82,6 +82,7 @@ struct PlaneGemm {
     const int *splits_in;      // device: null, or the number of parts
     int n_fastest;             // neighbouring pairs take neighbouring column tiles (else row tiles)
     int seg;                   // K chunks per accumulation in tensor memory (kernels with PROMOTE)
+    int half;                  // the operands' 16-bit values are fp16
 };
 
 struct PgTile {
@@ -164,7 +165,7 @@ __device__ __forceinline__ bool elect_one()
 //   bf16 planes  32 x 32 pieces (64-byte swizzle) that TMA writes, all planes of a chunk behind one proxy fence (a fence per piece
 //                took 0.5 us each); lane 0 sends and waits
 //   float32      32 x 32 tiles of two pieces (128-byte swizzle) that TMA writes or adds to what is there, where rows allow it; else, and
-//                where rows go to places of their own, a 32 x 33 tile read back a row at a time, lane = column
+//                where rows go to places of their own, a tile read back a row at a time, lane = column
 template <int N> struct PgStage {
     const CUtensorMap *map;
     uint32_t base;
@@ -235,13 +236,13 @@ template <int N> struct PgStage {
             tma_store_commit();
         }
     }
-    // f(row, value of column `lane` in that row, old(row)) for 32 rows, eight `old` at a time before the first of their `f`; N >= 3
+    // f(row, value of column `lane` in that row, old(row)) for 32 rows, eight `old` at a time before the first of their `f`; N >= 2
     template <class G, class F> __device__ __forceinline__ void rows(const float (&v)[32], G old, F f) const
     {
-        static_assert(N * kPgStageBytes >= 32 * 33 * 4, "a 32 x 33 tile of floats");
+        static_assert(N * kPgStageBytes >= 32 * 32 * 4, "a tile of floats");
         __syncwarp();
 #pragma unroll
-        for (int j = 0; j < 32; ++j) asm volatile("st.shared.f32 [%0], %1;" ::"r"(base + (lane * 33 + j) * 4), "f"(v[j]) : "memory");
+        for (int j = 0; j < 32; ++j) asm volatile("st.shared.f32 [%0], %1;" ::"r"(base + (lane * 32 + (j ^ lane)) * 4), "f"(v[j]) : "memory");
         __syncwarp();
 #pragma unroll 1
         for (int r0 = 0; r0 < 32; r0 += 8) {
@@ -249,7 +250,7 @@ template <int N> struct PgStage {
 #pragma unroll
             for (int k = 0; k < 8; ++k) w[k] = old(r0 + k);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[k]) : "r"(base + ((r0 + k) * 33 + lane) * 4) : "memory");
+            for (int k = 0; k < 8; ++k) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[k]) : "r"(base + ((r0 + k) * 32 + (lane ^ (r0 + k))) * 4) : "memory");
 #pragma unroll
             for (int k = 0; k < 8; ++k) f(r0 + k, x[k], w[k]);
         }
@@ -405,7 +406,7 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
     } else if (warp == 9) {
         if (rank == 0 && elect_one()) {
             // ------------------------------------------------------------ even CTA: MMA issuer for the pair
-            const uint32_t idesc = make_idesc_bf16(256, tn, AMN, BMN);
+            const uint32_t idesc = make_idesc_bf16(256, tn, AMN, BMN) & (p.half ? ~((1u << 7) | (1u << 10)) : ~0u);     // formats of A and B: 1 bf16, 0 fp16
             constexpr uint32_t astep = AMN ? 128 : 2, bstep = BMN ? 128 : 2;
             const uint64_t adesc = AMN ? make_smem_desc(0, 8192, 1024, kSwizzle128) : make_smem_desc(0, 16, 1024, kSwizzle128);
             const uint64_t bdesc = BMN ? make_smem_desc(0, 8192, 1024, kSwizzle128) : make_smem_desc(0, 16, 1024, kSwizzle128);

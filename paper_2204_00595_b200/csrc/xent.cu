@@ -9,10 +9,15 @@
 //   forward   logits tile in tensor memory -> per row the maximum and the sum of exponentials of its 128 columns -> one pair per
 //             row and half tile in memory -> a warp per row joins them
 //   backward  per piece of the vocabulary: logits again, g as bf16 planes in memory, then dW = g^T x and dx += g W from them.
-// Planes of g.  fp32: three, all six plane products.  bf16: two for dW, a float32 result, whose terms of 2^-17 error each (rms
-// 4e-6) average out over the tokens (2.7e-6 of dW's norm at 2900 tokens, logits' errors included); up to kFewTokens tokens, where
-// they do not, three, which costs nothing there: the time goes into reading W and writing dW.  A bf16 dx takes the first plane
-// (2^-8 per term, as much as its own rounding), of few tokens two.
+// Parts of g.  fp32: three bf16 planes, all six plane products.  bf16: dx takes one bf16 plane (2^-8 per term, as much as its own
+// rounding), of up to kFewTokens tokens two.  dW is a float32 result: two bf16 planes leave 2^-16 of a term (2.7e-6 of dW's norm at
+// 2900 tokens), a third costs a quarter of the call's time.  Two FP16 parts leave 2^-22, and x, bf16, fits fp16 once its exponents
+// are near 1.  Tokens are what dW sums over, so each may have a power of two of its own: x' = x 2^-a[t] with the row's largest value
+// in [1, 2), g' = g 2^(a[t] - E + 13), E the same for all, so that every |g'| is below 2^14 where exp(z - lse) <= 1; dW = 2^(E - 13) sum g' x'.
+// What fp16 cannot hold of them is 2^-25 of the row's largest x and 2^-39 of the largest g.  Up to kFewTokens tokens take three bf16
+// planes, which cost nothing there: the time goes into reading W and writing dW.
+#include <cuda_fp16.h>
+
 #include "plane_gemm.cuh"
 
 namespace monarch {
@@ -20,7 +25,7 @@ namespace tc {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kFewTokens = 64;
+constexpr int kFewTokens = 64, kBias = 1024;
 constexpr int kTokenChunk = 32768;              // tokens whose partial sums are in memory at a time (forward)
 
 __device__ __forceinline__ float ex2(float x)
@@ -39,6 +44,8 @@ struct PrepArgs {
     void *dx;                         // backward: likewise
     int *count, *map, *tgt;           // rows that count; compact row -> row; compact row -> target (-1: out of range)
     float *clse, *cdl;                // backward: lse and dloss of the compact rows
+    __half *xh;                       // backward, bf16, many tokens: x' [tokens][dp], a[t], and the largest a[t] + exponent of dloss[t]
+    int *exponent, *largest;          // (+ kBias, so that zero is below all)
     __nv_bfloat16 *xp;                // planes [planes][tokens][dp]
     int64_t ignore;
     int tokens, d, dp, vocab, rows_per_cta;
@@ -97,6 +104,49 @@ __device__ __forceinline__ void copy_row(const T *__restrict__ src, __nv_bfloat1
         split<PL>(c + 1 < d ? elem<T>::load(src + c + 1) : 0.0f, b);
 #pragma unroll
         for (int i = 0; i < PL; ++i) *reinterpret_cast<__nv_bfloat162 *>(dst + i * plane + c) = __nv_bfloat162(a[i], b[i]);
+    }
+}
+
+// exponent of a value by its bits; zeros, values below the normal range and infinities take the ends of the scale
+__device__ __forceinline__ int exponent_of(float v) { return min(max((int)(__float_as_uint(v) >> 23) - 127, -100), 100); }
+
+// x' of a row (one warp), its exponent, and its part in E
+__device__ __forceinline__ void scaled_row(const __nv_bfloat16 *__restrict__ src, __half *to, int d, int dp, float dl, int *exponent, int *largest, int lane)
+{
+    float top = 0.0f;
+    if (d == dp) {
+#pragma unroll 4
+        for (int c = lane * 8; c < d; c += 256) {
+            const uint4 v = __ldg(reinterpret_cast<const uint4 *>(src + c));
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xffff0000u))));
+        }
+    } else {
+        for (int c = lane; c < d; c += 32) top = fmaxf(top, fabsf(__bfloat162float(src[c])));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+    const int a = exponent_of(top);
+    const float down = __uint_as_float((uint32_t)(127 - a) << 23);
+    if (d == dp) {
+#pragma unroll 4
+        for (int c = lane * 8; c < d; c += 256) {
+            const uint4 v = __ldg(reinterpret_cast<const uint4 *>(src + c));
+            uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const __half2 h = __floats2half2_rn(__uint_as_float(w[i] << 16) * down, __uint_as_float(w[i] & 0xffff0000u) * down);
+                w[i] = *reinterpret_cast<const uint32_t *>(&h);
+            }
+            *reinterpret_cast<uint4 *>(to + c) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    } else {
+        for (int c = lane; c < dp; c += 32) to[c] = __float2half_rn(c < d ? __bfloat162float(src[c]) * down : 0.0f);
+    }
+    if (lane == 0) {
+        *exponent = a;
+        if (dl > 0.0f) atomicMax(largest, a + exponent_of(dl) + kBias);
     }
 }
 
@@ -172,6 +222,11 @@ __global__ void __launch_bounds__(256) xent_prep_kernel(const PrepArgs p)
                 copy_row<T, PL>(x + (size_t)(base + r) * p.d, p.xp + (size_t)dst * p.dp, plane, p.d, p.dp, lane, part, parts);
             else if (BWD)
                 for (int c = part * 32 + lane; c < p.d; c += parts * 32) elem<T>::store((T *)p.dx + (size_t)(base + r) * p.d + c, 0.0f);
+            if (BWD && p.xh != nullptr && part == 0 && dst >= 0)
+                scaled_row((const __nv_bfloat16 *)p.x + (size_t)(base + r) * p.d, p.xh + (size_t)dst * p.dp, p.d, p.dp, fabsf(p.dloss[base + r]),
+                           p.exponent + dst, p.largest, lane);
+            if (BWD && p.xh != nullptr && part == 0 && base + r >= total)
+                for (int c = lane; c < p.dp; c += 32) p.xh[(size_t)(base + r) * p.dp + c] = __float2half_rn(0.0f);
             if (base + r >= total)                           // rows behind the last one that counts enter sums over tokens as zeros
                 for (int j = 0; j < PL; ++j)
                     for (int c = (part * 32 + lane) * 8; c < p.dp; c += parts * 256)
@@ -247,14 +302,16 @@ struct EpiStats {
 };
 
 // g of a piece of the vocabulary; zeros behind the last row and the last column
-template <int PL> struct EpiGrad {
+// HALF: the bf16 plane for dx, then g' in two fp16 parts for dW; else PL bf16 planes
+template <int PL, bool HALF> struct EpiGrad {
     static constexpr int kStage = PL;
     struct Args {
         int cols, v0;
         const int *tgt, *count;
         const float *lse, *dl;
+        const int *exponent, *largest;
     };
-    float r_hi, r_lo, dl;
+    float r_hi, r_lo, dl, up;
     int y;
     bool live;
     __device__ __forceinline__ void begin(const Args &a, const PgTile &t)
@@ -265,6 +322,11 @@ template <int PL> struct EpiGrad {
         r_lo = fmaf(l, kLog2e, -r_hi);
         dl = live ? a.dl[t.row] : 0.0f;
         y = live ? a.tgt[t.row] - a.v0 - t.col : -1;
+        if (HALF) {
+            // 2^(a[t] - E + 13); below the normal range of fp32 the whole row is below 2^-100 of the largest
+            const int e = live ? a.exponent[t.row] - (*a.largest - kBias) + 13 : 0;
+            up = e < -126 ? 0.0f : __uint_as_float((uint32_t)(127 + min(e, 127)) << 23);
+        }
     }
     __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<kStage> &st)
     {
@@ -275,18 +337,42 @@ template <int PL> struct EpiGrad {
             v[i] = i >= left ? 0.0f : dl * (at == i ? e - 1.0f : e);
         }
         st.begin();
-#pragma unroll
-        for (int q = 0; q < PL; ++q) {
+        if constexpr (HALF) {
             uint32_t w[16];
 #pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+            st.row(0, w);
+#pragma unroll
             for (int i = 0; i < 16; ++i) {
-                w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-                if (q + 1 < PL) {
-                    v[2 * i] -= __uint_as_float(w[i] << 16);
-                    v[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
-                }
+                v[2 * i] *= up;
+                v[2 * i + 1] *= up;
+                const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+                const float2 f = __half22float2(h);
+                v[2 * i] -= f.x;
+                v[2 * i + 1] -= f.y;
+                w[i] = *reinterpret_cast<const uint32_t *>(&h);
             }
-            st.row(q, w);
+            st.row(1, w);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+                w[i] = *reinterpret_cast<const uint32_t *>(&h);
+            }
+            st.row(2, w);
+        } else {
+#pragma unroll
+            for (int q = 0; q < PL; ++q) {
+                uint32_t w[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+                    if (q + 1 < PL) {
+                        v[2 * i] -= __uint_as_float(w[i] << 16);
+                        v[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
+                    }
+                }
+                st.row(q, w);
+            }
         }
         st.ready();
 #pragma unroll
@@ -303,10 +389,17 @@ struct EpiStoreF32 {
         float *out;
         int rows, cols, add;
         int y0;                    // of these rows in the map that TMA writes by; -1: none
+        const int *largest;        // E of fp16 parts, or null
     };
-    __device__ __forceinline__ void begin(const Args &, const PgTile &) {}
+    int e;
+    __device__ __forceinline__ void begin(const Args &a, const PgTile &) { e = a.largest != nullptr ? *a.largest - kBias - 13 : 0; }
     __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<kStage> &st)
     {
+        // times 2^(E - 13), in two steps: it need not be in the normal range itself (no weights at all: E is far below)
+        const int e1 = max(-126, min(127, e / 2)), e2 = max(-126, min(127, e - e / 2));
+        const float f1 = __uint_as_float((uint32_t)(127 + e1) << 23), f2 = __uint_as_float((uint32_t)(127 + e2) << 23);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = v[i] * f1 * f2;
         if (a.y0 >= 0) {
             if ((t.row & ~31) < a.rows && t.col + c < a.cols) st.tile(v, t.col + c, a.y0 + (t.row & ~31), 0, a.add);
             return;
@@ -324,7 +417,7 @@ struct EpiStoreF32 {
 
 // dx: the sums of the pieces so far in float32 (compact rows), the last one to the caller's rows
 template <typename T> struct EpiDx {
-    static constexpr int kStage = 3;
+    static constexpr int kStage = 2;
     struct Args {
         float *acc;
         T *dx;
@@ -688,15 +781,16 @@ struct Layout {
     int chunk, halves, trows;
     int tn, tn_dw, tn_dx;                       // columns of a tile: logits, dW, dx
     int dx_parts;                               // most parts of the vocabulary in dx; 1: no parts
-    size_t count, splits, map, tgt, lse, dl, tlogit, x, w, part, g, dx, total;
+    bool half;                                  // dW from fp16 parts
+    size_t count, splits, largest, exponent, xh, map, tgt, lse, dl, tlogit, x, w, part, g, dx, total;
 };
 
-// Vocabulary entries per piece of the backward pass: whole 256-entry tiles, a plane of g within a quarter of a gigabyte, and
+// Vocabulary entries per piece of the backward pass: whole 256-entry tiles, a plane of g within 160 MB, and
 // as few rounds of the pairs over the tiles of the three products as can be had.
 int bwd_piece(int64_t tokens, int d, int vocab)
 {
     const int mt = tokens > 0 ? ceil_div(tokens, 256) : 1, nt = ceil_div(d, 256), vt = ceil_div(vocab, 256);
-    int most = (int)(((size_t)256 << 20) / ((size_t)mt * 256 * 256 * 2));
+    int most = (int)(((size_t)160 << 20) / ((size_t)mt * 256 * 256 * 2));
     most = most < 1 ? 1 : most > vt ? vt : most;
     int best = most;
     double best_cost = 1e300;
@@ -721,7 +815,8 @@ Layout layout(int64_t tokens, int d, int vocab, int dtype, bool bwd)
     Layout l;
     l.direct = dtype == MONARCH_BF16 && d % 8 == 0;
     l.planes = dtype == MONARCH_F32 ? 3 : 1;
-    l.gplanes = dtype == MONARCH_F32 || tokens <= kFewTokens ? 3 : 2;
+    l.gplanes = 3;
+    l.half = bwd && dtype == MONARCH_BF16 && tokens > kFewTokens;
     l.dp = (d + 7) / 8 * 8;
     l.chunk = (int)(tokens < kTokenChunk ? tokens : kTokenChunk);
     l.trows = ceil_div(tokens, 64) * 64;                                      // what dW's K chunks read; stores and loads behind it are clipped
@@ -751,6 +846,12 @@ Layout layout(int64_t tokens, int d, int vocab, int dtype, bool bwd)
     const size_t t = (size_t)tokens;
     l.count = take(4);
     l.splits = take(4);
+    l.largest = take(4);
+    l.exponent = l.xh = 0;
+    if (l.half) {
+        l.exponent = take(t * 4);
+        l.xh = take(t * l.dp * 2);
+    }
     l.map = take(t * 4);
     l.tgt = take(t * 4);
     l.lse = l.dl = l.tlogit = l.part = l.g = l.dx = 0;
@@ -902,7 +1003,7 @@ int xent_fwd(const void *x, const void *W, const int64_t *targets, float *loss, 
 namespace tc {
 namespace {
 
-template <typename T, int LOGITS, int GP, int DW, int DX>
+template <typename T, bool HALF, int LOGITS, int DW, int DX>
 int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate, int64_t tokens, int32_t d, int32_t vocab, int dtype, char *base, cudaStream_t s)
 {
     unsigned *status = (unsigned *)base;
@@ -912,8 +1013,10 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
     float *acc = (float *)(base + l.dx);
     int *splits = (int *)(base + l.splits);
     const size_t gplane = (size_t)l.trows * l.piece;
+    const int *largest = (const int *)(base + l.largest), *exponent = (const int *)(base + l.exponent);
+    constexpr int GP = 3;
 
-    CUtensorMap x_k, x_n, w_k, w_n, g_m, g_k, g_to, dw_to, dx_to;
+    CUtensorMap x_k, x_n, w_k, w_n, g_m, g_k, g_to, dw_to, dx_to, x_h;
     if (d % 4 == 0) {
         MONARCH_TRY(tile_target(&dw_to, dW, vocab, d, (int64_t)vocab * d, 1));
         MONARCH_TRY(tile_target(&dx_to, acc, tokens, d, tokens * d, l.dx_parts));
@@ -925,7 +1028,10 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
     MONARCH_TRY(plane_map(&x_k, xp, 0, tokens, l.dp, l.dp, tokens * l.dp, l.planes));
     MONARCH_TRY(plane_map(&x_n, xp, 1, tokens, l.dp, l.dp, tokens * l.dp, l.planes));
     MONARCH_TRY(plane_map(&g_k, g, 0, l.trows, l.piece, l.piece, (int64_t)gplane, l.gplanes));
-    MONARCH_TRY(plane_map(&g_m, g, 1, l.trows, l.piece, l.piece, (int64_t)gplane, l.gplanes));
+    // dW: all planes, or the two fp16 parts behind the bf16 one
+    MONARCH_TRY(plane_map(&g_m, g + (HALF ? gplane : 0), 1, l.trows, l.piece, l.piece, (int64_t)gplane, HALF ? 2 : l.gplanes));
+    if (HALF) MONARCH_TRY(plane_map(&x_h, base + l.xh, 1, tokens, l.dp, l.dp, tokens * l.dp, 1));
+    else x_h = x_n;
     if (l.direct) {
         MONARCH_TRY(plane_map(&w_k, W, 0, vocab, d, d, (int64_t)vocab * d, 1, l.tn / 2));
         MONARCH_TRY(plane_map(&w_n, W, 1, vocab, d, d, (int64_t)vocab * d, 1));
@@ -941,15 +1047,16 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
         PlaneGemm p = gemm(status);
         p.count = count; p.rows = (int)tokens; p.cols = cols; p.kdim = d; p.tn = l.tn;
         p.b_n0 = l.direct ? v0 : 0;
-        const typename EpiGrad<GP>::Args eg = {cols, v0, tgt, count, clse, cdl};
-        MONARCH_TRY((logits<LOGITS, EpiGrad<GP>>(x_k, w_k, g_to, p, eg, true, s)));
+        const typename EpiGrad<GP, HALF>::Args eg = {cols, v0, tgt, count, clse, cdl, exponent, largest};
+        MONARCH_TRY((logits<LOGITS, EpiGrad<GP, HALF>>(x_k, w_k, g_to, p, eg, true, s)));
         // dW = g^T x
         p = gemm(status);
         p.count = count; p.count_is_k = 1; p.rows = cols; p.cols = d; p.kdim = (int)tokens; p.tn = l.tn_dw;
         p.n_fastest = 1;
         p.seg = pg_seg(DW);
-        const EpiStoreF32::Args ew = {dW + (size_t)v0 * d, cols, d, accumulate, d % 4 == 0 ? v0 : -1};
-        MONARCH_TRY((launch_plane_gemm<1, 1, DW, true, EpiStoreF32>(g_m, x_n, dw_to, p, ew, s)));
+        const EpiStoreF32::Args ew = {dW + (size_t)v0 * d, cols, d, accumulate, d % 4 == 0 ? v0 : -1, HALF ? largest : nullptr};
+        p.half = HALF;
+        MONARCH_TRY((launch_plane_gemm<1, 1, DW, true, EpiStoreF32>(g_m, x_h, dw_to, p, ew, s)));
         // dx += g W
         p = gemm(status);
         p.count = count; p.rows = (int)tokens; p.cols = d; p.kdim = cols; p.tn = l.tn_dx;
@@ -996,12 +1103,16 @@ int xent_bwd(const void *x, const void *W, const int64_t *targets, const float *
     a.xp = (__nv_bfloat16 *)(base + l.x);
     a.ignore = ignore_index; a.tokens = (int)tokens; a.d = d; a.dp = l.dp; a.vocab = vocab;
     if (!l.direct) { a.W = W; a.wp = (__nv_bfloat16 *)(base + l.w); a.wplane = (size_t)l.piece * l.dp; a.wrows = vocab < l.piece ? vocab : l.piece; }
+    if (l.half) {
+        a.xh = (__half *)(base + l.xh); a.exponent = (int *)(base + l.exponent); a.largest = (int *)(base + l.largest);
+        MONARCH_CUDA_TRY(cudaMemsetAsync(a.largest, 0, 4, s));
+    }
     MONARCH_TRY(prep_any<true>(a, dtype, s));
     if (dtype == MONARCH_F32)
-        return bwd_pieces<float, kP3x3, 3, kP3x3, kP3x3>(l, W, (float *)dx, dW, accumulate, tokens, d, vocab, dtype, base, s);
-    if (l.gplanes == 3)
-        return bwd_pieces<__nv_bfloat16, kP1, 3, kP3x1, kP2x1>(l, W, (__nv_bfloat16 *)dx, dW, accumulate, tokens, d, vocab, dtype, base, s);
-    return bwd_pieces<__nv_bfloat16, kP1, 2, kP2x1, kP1>(l, W, (__nv_bfloat16 *)dx, dW, accumulate, tokens, d, vocab, dtype, base, s);
+        return bwd_pieces<float, false, kP3x3, kP3x3, kP3x3>(l, W, (float *)dx, dW, accumulate, tokens, d, vocab, dtype, base, s);
+    if (!l.half)
+        return bwd_pieces<__nv_bfloat16, false, kP1, kP3x1, kP2x1>(l, W, (__nv_bfloat16 *)dx, dW, accumulate, tokens, d, vocab, dtype, base, s);
+    return bwd_pieces<__nv_bfloat16, true, kP1, kP2x1, kP1>(l, W, (__nv_bfloat16 *)dx, dW, accumulate, tokens, d, vocab, dtype, base, s);
 }
 
 }  // namespace monarch

@@ -4,7 +4,7 @@ Tolerances of the loss are bounds, computed per element from the operands (``acc
 off by at most (steps) * 2^-23 of the sum of their absolute values, a step being 16 products of one plane pair and a run at most
 96 steps before it is added up to nearest; exponentials, logarithms and their arguments add 2^-20 relative.  Half a step of bf16
 is 2^-8 of the value, so one, two or three parts leave 2^-8, 2^-16 or 2^-24: g is held to three in fp32 and for up to 64 tokens,
-else to two, a bf16 dx takes one; fp32 operands in three parts (2^-24 each) leave out two products of 2^-8 2^-16 as well, 2^-22 in
+else dW takes two fp16 parts (2^-11 each: 2^-22, and x, in fp16, is off by at most 2^-25 of its row's largest), a bf16 dx one; fp32 operands in three parts (2^-24 each) leave out two products of 2^-8 2^-16 as well, 2^-22 in
 all; a bf16 result is off by 2^-8.
 The orthogonalised update is compared normwise per block.  To first order an error of X grows by at most max |p'| = 3.9 a step
 (p(s) = a s + b s^3 + c s^5 on [0, 1.2]) while X itself grows from norm 1 to 0.9 sqrt(k), and each step adds its own rounding, some
@@ -115,7 +115,7 @@ def exact(x, W, y, dloss=None, ignore=IGNORE):
     onehot = torch.zeros_like(p).scatter_(1, yk[:, None], 1.0)
     gr = w * (p - onehot)
     three = f32 or x.shape[0] <= 64
-    dg = w * p * (dz + 2.0 ** -20 * (1.0 + z.abs() / 16)) + gr.abs() * ((2.0 ** -24 if three else 2.0 ** -16) + 2.0 ** -23)
+    dg = w * p * (dz + 2.0 ** -20 * (1.0 + z.abs() / 16)) + gr.abs() * ((2.0 ** -24 if three else 2.0 ** -22) + 2.0 ** -23)
     dg1 = dg if f32 else dg + gr.abs() * 2.0 ** -8
     xa, Wa = xk.abs(), Wd.abs()
     w_planes = 2.0 ** -22 if f32 else 0.0
@@ -124,7 +124,13 @@ def exact(x, W, y, dloss=None, ignore=IGNORE):
                          + (gr @ Wd).abs() * (2.0 ** -23 if f32 else 2.0 ** -8))
     out["dW"] = gr.T @ xk
     T = rows.numel()
-    out["dW_err"] = dg.T @ xa + (gr.abs().T @ xa) * (acc(T, 6 if f32 else 3) + w_planes) + out["dW"].abs() * 2.0 ** -23
+    if not three:                                          # x in fp16, and g' = g 2^(a - E + 13) below 2^14 to 2^-25 of its unit
+        top = xa.amax(1, keepdim=True)
+        big = float((top[:, 0] * w[:, 0].abs()).max())
+        extra = gr.abs().T @ (top * 2.0 ** -24).expand_as(xk) + 2.0 ** -37 * big * rows.numel()
+    else:
+        extra = 0.0
+    out["dW_err"] = extra + dg.T @ xa + (gr.abs().T @ xa) * (acc(T, 6 if f32 else 3) + w_planes) + out["dW"].abs() * 2.0 ** -23
     return out
 
 
@@ -205,6 +211,27 @@ def test_accumulate_adds(dtype):
     before = torch.randn(V, d, device="cuda")
     _, dW = backward(x, W, y, e["lse"].float(), dloss, dW0=before)
     within(dW, e["dW"] + before.double(), e["dW_err"] + (before.double().abs() + e["dW"].abs()) * 2.0 ** -23, "dW")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_tokens_of_very_different_size(dtype):
+    """Rows of x from 1e-12 to 1e6, zero rows, weights of tokens from 0 to 1e8 and down to 1e-30: each token has its own scale on the way."""
+    T, d, V = 200, 96, 700
+    x, W, y, dloss = make(T, d, V, dtype, 0.1, seed=13)
+    g = gen(14)
+    s = 10.0 ** (torch.rand(T, 1, generator=g, device="cuda") * 18 - 12)
+    x = (x.double() * s.double()).to(x.dtype)
+    x[7] = 0.0
+    x[9, 1:] = 0.0
+    W = (W.double() * 1e-6).to(W.dtype)                    # logits stay moderate
+    dloss = (dloss.double() * 10.0 ** (torch.rand(T, generator=g, device="cuda").double() * 38 - 30)).float()
+    dloss[3] = 0.0
+    e = exact(x, W, y, dloss)
+    dx, dW = backward(x, W, y, e["lse"].float(), dloss)
+    within(dx, e["dx"], e["dx_err"], "dx")
+    within(dW, e["dW"], e["dW_err"], "dW")
+    _, dW = backward(x, W, y, e["lse"].float(), torch.zeros_like(dloss))
+    assert (dW == 0).all()
 
 
 def test_targets_out_of_range_and_any_ignore_index():
