@@ -171,10 +171,10 @@ template <int N> struct PgStage {
     uint32_t base;
     int lane, turn;
     __device__ __forceinline__ uint32_t piece(int i) const { return base + i * kPgStageBytes; }
-    // the pieces sent last have been read
-    __device__ __forceinline__ void begin() const
+    // the pieces sent have been read, but for those of the last PENDING groups
+    template <int PENDING = 0> __device__ __forceinline__ void begin() const
     {
-        if (lane == 0) tma_store_wait_read<0>();
+        if (lane == 0) tma_store_wait_read<PENDING>();
         __syncwarp();
     }
     // 16 packed words: this lane's row of 32 values
@@ -273,7 +273,7 @@ __device__ __forceinline__ bool pg_wait(uint32_t bar, uint32_t parity, unsigned 
     return mbar_try_wait_cluster_acquire(bar, parity) || pg_wait_on(bar, parity, status, dead, code);
 }
 
-// Epi: struct with  begin(const Epi::Args &, const PgTile &),  chunk(args, tile, c, float (&v)[32], stage)  for c = 0, 32, .. < tn / 2,
+// Epi: struct with  begin(const Epi::Args &, const PgTile &) (a tile ahead: loads),  start(args, tile),  chunk(args, tile, c, float (&v)[32], stage)  for c = 0, 32, .. < tn / 2,
 // end(args, tile); kStage: pieces in `stage`, its warp's PgStage (0: none).  PROMOTE: at most p.seg chunks are accumulated in tensor memory, sums of those in fp32 registers.
 template <int AMN, int BMN, int SCHEME, bool PROMOTE, class Epi>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPgThreads, 1)
@@ -454,16 +454,30 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
         uint32_t it = 0;
         bool ok = true;
         PgStage<(Epi::kStage > 0 ? Epi::kStage : 1)> stage = {&tm_c, ring0 + kPgSlots * kPgSlotBytes + warp * Epi::kStage * kPgStageBytes, lane, 0};
-        for (int tile = pair; ok && tile < total; tile += npairs) {
-            const At at = locate(tile);
+        auto place = [&](const At &at) {
             PgTile t;
             t.z = at.split;
             t.half = at.nt * 2 + (warp >> 2);
             t.row = p.row0 + at.mt * kPgTile + (int)rank * 128 + (warp & 3) * 32 + lane;
             t.col = at.nt * tn + (warp >> 2) * (tn / 2);
             t.zero = at.c0 >= at.c1;
-            Epi e;
-            e.begin(args, t);
+            return t;
+        };
+        // what a tile's rows bring along is asked for a tile ahead
+        At at_next = locate(min(pair, max(total - 1, 0)));
+        PgTile t_next = place(at_next);
+        Epi e_next;
+        if (pair < total) e_next.begin(args, t_next);
+        for (int tile = pair; ok && tile < total; tile += npairs) {
+            const At at = at_next;
+            const PgTile t = t_next;
+            Epi e = e_next;
+            if (tile + npairs < total) {
+                at_next = locate(tile + npairs);
+                t_next = place(at_next);
+                e_next.begin(args, t_next);
+            }
+            e.start(args, t);
             if constexpr (!PROMOTE) {
                 uint32_t buf = it & 1;
                 if (!t.zero) {

@@ -264,8 +264,9 @@ struct EpiStats {
         m = __int_as_float(0xff800000);
         s = 0.0f;
         live = t.row < *a.count;
-        y = live ? a.tgt[t.row] - a.v0 - t.col : -1;
+        y = live ? a.tgt[t.row] : -1;
     }
+    __device__ __forceinline__ void start(const Args &a, const PgTile &t) { y -= a.v0 + t.col; }
     __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<1> &)
     {
         const int left = a.cols - t.col - c;
@@ -312,20 +313,26 @@ template <int PL, bool HALF> struct EpiGrad {
         const int *exponent, *largest;
     };
     float r_hi, r_lo, dl, up;
-    int y;
+    int y, e;
     bool live;
     __device__ __forceinline__ void begin(const Args &a, const PgTile &t)
     {
         live = t.row < *a.count;
-        const float l = live ? a.lse[t.row] : 0.0f;
+        r_hi = live ? a.lse[t.row] : 0.0f;
+        dl = live ? a.dl[t.row] : 0.0f;
+        y = live ? a.tgt[t.row] : -1;
+        if (HALF) e = live ? a.exponent[t.row] - *a.largest : 0;
+    }
+    __device__ __forceinline__ void start(const Args &a, const PgTile &t)
+    {
+        const float l = r_hi;
         r_hi = l * kLog2e;
         r_lo = fmaf(l, kLog2e, -r_hi);
-        dl = live ? a.dl[t.row] : 0.0f;
-        y = live ? a.tgt[t.row] - a.v0 - t.col : -1;
+        y -= a.v0 + t.col;
         if (HALF) {
             // 2^(a[t] - E + 13); below the normal range of fp32 the whole row is below 2^-100 of the largest
-            const int e = live ? a.exponent[t.row] - (*a.largest - kBias) + 13 : 0;
-            up = e < -126 ? 0.0f : __uint_as_float((uint32_t)(127 + min(e, 127)) << 23);
+            const int x = e + kBias + 13;
+            up = x < -126 ? 0.0f : __uint_as_float((uint32_t)(127 + min(x, 127)) << 23);
         }
     }
     __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<kStage> &st)
@@ -393,6 +400,7 @@ struct EpiStoreF32 {
     };
     int e;
     __device__ __forceinline__ void begin(const Args &a, const PgTile &) { e = a.largest != nullptr ? *a.largest - kBias - 13 : 0; }
+    __device__ __forceinline__ void start(const Args &, const PgTile &) {}
     __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<kStage> &st)
     {
         // times 2^(E - 13), in two steps: it need not be in the normal range itself (no weights at all: E is far below)
@@ -426,6 +434,7 @@ template <typename T> struct EpiDx {
     };
     int n;
     __device__ __forceinline__ void begin(const Args &a, const PgTile &) { n = *a.count; }
+    __device__ __forceinline__ void start(const Args &, const PgTile &) {}
     __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<kStage> &st)
     {
         const int col = t.col + c + st.lane, row0 = t.row & ~31, rows = col < a.d ? n - row0 : 0;
@@ -452,6 +461,7 @@ struct EpiDxPart {
     };
     int n;
     __device__ __forceinline__ void begin(const Args &a, const PgTile &) { n = *a.count; }
+    __device__ __forceinline__ void start(const Args &, const PgTile &) {}
     __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<kStage> &st)
     {
         if (a.tma) {
@@ -834,8 +844,8 @@ Layout layout(int64_t tokens, int d, int vocab, int dtype, bool bwd)
     // half tiles of all pieces
     l.halves = 2 * (vocab / l.piece * ceil_div(l.piece, l.tn) + ceil_div(vocab % l.piece, l.tn));
     l.tn_dw = pg_tile(ceil_div(l.piece, 256), d, false);
-    l.tn_dx = pg_tile(mt, d, false);
-    // dx of few tiles is split along the vocabulary: as far as the parts stay within L2
+    l.tn_dx = d > 128 ? 256 : 128;
+    // dx of few tiles is split along the vocabulary, which costs less than narrow tiles: as far as the parts stay within L2
     const int64_t tiles = mt * ceil_div(d, l.tn_dx), part = tokens * d * 4;
     int64_t parts = part > 0 ? ((int64_t)64 << 20) / part : 1;
     if (parts > l.piece / 256) parts = l.piece / 256;
