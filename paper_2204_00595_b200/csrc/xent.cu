@@ -844,8 +844,8 @@ Layout layout(int64_t tokens, int d, int vocab, int dtype, bool bwd)
     // half tiles of all pieces
     l.halves = 2 * (vocab / l.piece * ceil_div(l.piece, l.tn) + ceil_div(vocab % l.piece, l.tn));
     l.tn_dw = pg_tile(ceil_div(l.piece, 256), d, false);
-    l.tn_dx = d > 128 ? 256 : 128;
-    // dx of few tiles is split along the vocabulary, which costs less than narrow tiles: as far as the parts stay within L2
+    // dx of few tiles is split along the vocabulary, as far as the parts stay within L2; narrow tiles where there would be many parts
+    l.tn_dx = mt * ceil_div(d, 256) >= 8 ? 256 : 128;
     const int64_t tiles = mt * ceil_div(d, l.tn_dx), part = tokens * d * 4;
     int64_t parts = part > 0 ? ((int64_t)64 << 20) / part : 1;
     if (parts > l.piece / 256) parts = l.piece / 256;
