@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(kSmallThreads) ortho_small_kernel(const Io<T> 
 // One CTA per block, everything on chip: X, S and P = b S + c S^2 are bf16 planes in shared memory (PL = 2 for bf16 results, 3 for
 // fp32), their fp32 values stay in the registers of the thread that holds them as an accumulator, warp-level MMAs (m16n8k16).
 // S is symmetric, so S and P serve as either operand as stored; only P X needs X transposed (ldmatrix.trans).  For k up to 32, and for
-// n of 129 to 256 with k up to 64, where X does not fit what the kernel below has; 32 x 32, bf16, 64 blocks: XX us.
+// n of 129 to 256 with k up to 64, where X does not fit what the kernel below has.  64 blocks of 32 x 32, five steps: bf16 4.8 us, fp32 5.9, of which 3.5 is the launch.
 // KP, NP: k and n rounded up; warps: KP / 16 rows of tiles times two column halves.
 template <int KP, int NP, int PL> struct BlockCfg {
     static constexpr int kRows = KP / 16, kThreads = kRows * 2 * 32;
@@ -449,8 +449,9 @@ template <typename T, int PL> int ortho_block(const Io<T> &io, int64_t blocks, i
 // steps that read the first half of an operand are issued as soon as it is written, the others finish the first half of a result of
 // 128 columns before the second, so that its values are converted meanwhile.  What a conversion overwrites (P over S, X over X) is the
 // half that no MMA still under way reads.
-// Measured, 128 blocks of 128 x 128, optimiser step: bf16 27.5 us (3.7 a step: 2360 cycles a product, 1536 of them MMAs of three
-// plane products), fp32 43.6 (6.6 a step); with fp32 FMA 525.  The one thread that issues has to keep its operands in uniform
+// Measured, 128 blocks of 128 x 128, optimiser step: bf16 27.6 us (3.7 a step: 2360 cycles a product, 1536 of them MMAs of three
+// plane products), fp32 43.0 (6.6 a step); with fp32 FMA 525.  128 of 64 x 64: 14.2 and 19.4 us (1.9 and 2.9 a step; on warp MMAs
+// 15.1 and 22.1): a product is 384 (768) cycles of MMAs and some 800 of hand-over, two barriers and two waits.  The one thread that issues has to keep its operands in uniform
 // registers (elect_one): picked as thread 0 it took 60 cycles per MMA, 33.3 and 51.1 us.
 constexpr int kTcThreads = 512;
 template <int KP, int NP, int PL> struct TcCfg {

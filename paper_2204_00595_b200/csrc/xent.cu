@@ -622,25 +622,28 @@ __global__ void __launch_bounds__(kFewThreads, 1) xent_few_kernel(const FewArgs 
     constexpr int kStep = sizeof(T) == 2 ? 4 : 2;                               // chunks of 32 requested ahead
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     const size_t xplane = (size_t)p.tokens * p.row;
-    const int groups = (p.vocab + 15) / 16, chunks = (p.d + 31) / 32;
+    const int chunks = (p.d + 31) / 32;
     const int team = warp / kFewTeam, member = warp % kFewTeam;
     // this warp's chunks, in steps of kStep
     const int each = (chunks + kFewTeam - 1) / kFewTeam, k0 = min(member * each, chunks), k1 = min(k0 + each, chunks), steps = (each + kStep - 1) / kStep;
-    const int first = blockIdx.x * kFewTeams + team, stride = gridDim.x * kFewTeams;
+    // this team's rows: as many as every other's, the last group of 16 may be part of one (3142 groups on 296 teams are 10 or 11 each)
+    const int teams = gridDim.x * kFewTeams, rows = (p.vocab + teams - 1) / teams;
+    const int row0 = min((int)(blockIdx.x * kFewTeams + team) * rows, p.vocab), row1 = min(row0 + rows, p.vocab), groups = (row1 - row0 + 15) / 16;
     FewRaw<T> raw[kStep][2];
     auto fetch = [&](int grp, int step) {
-        const T *w0 = (const T *)p.W + (size_t)min(grp * 16 + g, p.vocab - 1) * p.d, *w1 = (const T *)p.W + (size_t)min(grp * 16 + g + 8, p.vocab - 1) * p.d;
+        const int r = row0 + grp * 16 + g;
+        const T *w = (const T *)p.W + (size_t)r * p.d;
 #pragma unroll
         for (int u = 0; u < kStep; ++u) {
             const int k = k0 + step * kStep + u, at = k * 32 + c * 8;
-            const bool in = grp < groups && k < k1 && at < p.d;
-            raw[u][0].load(w0 + at, in);
-            raw[u][1].load(w1 + at, in);
+            const bool in = k < k1 && at < p.d;
+            raw[u][0].load(w + at, in && r < row1);
+            raw[u][1].load(w + (size_t)8 * p.d + at, in && r + 8 < row1);
         }
     };
     depend_wait();
     depend_launch();
-    fetch(first, 0);                                                           // on its way while the tokens are prepared
+    fetch(0, 0);                                                           // on its way while the tokens are prepared
     if (threadIdx.x < 8 * NT && (int)threadIdx.x >= p.tokens) s_tgt[threadIdx.x] = -2;
     const int parts = kFewThreads / 32 / p.tokens;                             // warps a token; tokens <= 16
     if (const int t = warp / parts; t < p.tokens) {
@@ -673,7 +676,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) xent_few_kernel(const FewArgs 
     const __nv_bfloat16 *xl = xs + (size_t)g * p.row + c * 8;
     float *sums = reinterpret_cast<float *>(xs + PL * xplane) + team * 2 * kFewTeam * NT * 128;      // [2][team][NT][4][32 lanes]
     int turn = 0;
-    for (int grp = first; grp < groups; grp += stride, ++turn) {
+    for (int grp = 0; grp < groups; ++grp, ++turn) {
         float z[NT][4] = {}, sum[NT][4] = {};
         for (int step = 0; step < steps; ++step) {
             uint32_t a[kStep][2][PL][4];
@@ -682,7 +685,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) xent_few_kernel(const FewArgs 
                 raw[u][0].planes(a[u][0]);
                 raw[u][1].planes(a[u][1]);
             }
-            fetch(step + 1 < steps ? grp : grp + stride, step + 1 < steps ? step + 1 : 0);
+            fetch(step + 1 < steps ? grp : grp + 1, step + 1 < steps ? step + 1 : 0);
 #pragma unroll
             for (int u = 0; u < kStep; ++u) {
                 const int k = k0 + step * kStep + u;
@@ -718,7 +721,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) xent_few_kernel(const FewArgs 
         asm volatile("bar.sync %0, 256;" ::"r"(team + 1) : "memory");
         // this buffer is written again two groups on, behind the next barrier, which its reader reaches when it has read
         if (turn % kFewTeam != member) continue;
-        const int r0 = grp * 16 + g, r1 = r0 + 8;
+        const int r0 = row0 + grp * 16 + g, r1 = r0 + 8;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             float t[4] = {};
@@ -729,9 +732,9 @@ __global__ void __launch_bounds__(kFewThreads, 1) xent_few_kernel(const FewArgs 
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const float z0 = t[e], z1 = t[e + 2];
-                if (r0 == tgt[n][e]) p.tlogit[n * 8 + 2 * c + e] = z0;
-                if (r1 == tgt[n][e]) p.tlogit[n * 8 + 2 * c + e] = z1;
-                const float v0 = r0 < p.vocab ? z0 : __int_as_float(0xff800000), v1 = r1 < p.vocab ? z1 : __int_as_float(0xff800000);
+                if (r0 == tgt[n][e] && r0 < row1) p.tlogit[n * 8 + 2 * c + e] = z0;
+                if (r1 == tgt[n][e] && r1 < row1) p.tlogit[n * 8 + 2 * c + e] = z1;
+                const float v0 = r0 < row1 ? z0 : __int_as_float(0xff800000), v1 = r1 < row1 ? z1 : __int_as_float(0xff800000);
                 const float top = fmaxf(m[n][e], fmaxf(v0, v1) * kLog2e), base = top == __int_as_float(0xff800000) ? 0.0f : top;
                 s[n][e] = s[n][e] * ex2(m[n][e] - base) + ex2(fmaf(v0, kLog2e, -base)) + ex2(fmaf(v1, kLog2e, -base));
                 m[n][e] = top;
