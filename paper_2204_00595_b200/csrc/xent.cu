@@ -547,19 +547,30 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const float2 *__restrict
 // consecutive k of one row: the order of k within a chunk of 32 is the same for both operands, so it does not matter), the tokens
 // (8 per column tile) wait in shared memory.  The eight warps of a team share 16 rows, an eighth of d each: their sums meet in shared
 // memory, the warps take turns to turn them into maximum and sum of exponentials while the others go on.  (A warp to itself for 16
-// rows: 3142 groups of a vocabulary of 50257 on 2368 warps are two rounds, the second a third full; 26.5 us for one token of d 1024.)
-// Lanes, warps and, in the last CTA to finish, CTAs are joined.  fp32: three planes of both, six products.
-constexpr int kFewThreads = 512, kFewMost = 16, kFewTeam = 8, kFewTeams = kFewThreads / 32 / kFewTeam;
-constexpr size_t kFewSmem = 184 * 1024;         // for the tokens; the sums take up to 32 KB more
+// rows: 3142 groups of a vocabulary of 50257 on 2368 warps are two rounds, the second a third full; 26.5 us for one token of d 1024,
+// now 23.2.)  Lanes, warps and, in the last CTA to finish, CTAs are joined.  fp32: three planes of both, six products; there up to three
+// launches, of up to 16 tokens each, are taken before the tile kernels, whose planes of W alone cost as much: 32 tokens, d 1024, a
+// vocabulary of 50257: 245 us on tiles; a launch of 16 tokens 60.  bf16: 33 us on tiles, 25 a launch, so one launch only.
+constexpr int kFewMost = 16, kFewTeam = 8;
+// 24 warps have 96 KB under way, 16 have 64; fp32 and a second column tile need the registers
+__host__ __device__ constexpr int few_threads(int planes, int tiles) { return planes == 1 && tiles == 1 ? 768 : 512; }
+__host__ __device__ constexpr int few_teams(int planes, int tiles) { return few_threads(planes, tiles) / 32 / kFewTeam; }
 constexpr int kFewTicket = 16;                  // word of the status area, zero between calls
 
 int few_row(int d) { return ((d * 2 + 127) / 128 * 128 + 64) / 2; }             // rows 64 bytes apart in their banks
 int few_tiles(int tokens) { return tokens <= 8 ? 1 : 2; }                       // column tiles of 8 tokens: what the kernels are built for
 size_t few_x(int tokens, int d, int planes) { return (size_t)tokens * few_row(d) * 2 * planes; }
-size_t few_smem(int tokens, int d, int planes) { return few_x(tokens, d, planes) + (size_t)kFewTeams * 2 * kFewTeam * few_tiles(tokens) * 512; }
-bool few_fits(int64_t tokens, int d, int dtype)
+size_t few_smem(int tokens, int d, int planes) { return few_x(tokens, d, planes) + (size_t)few_teams(planes, few_tiles(tokens)) * 2 * kFewTeam * few_tiles(tokens) * 512; }
+// launches of few tokens that the call takes; 0: tiles
+int few_launches(int64_t tokens, int d, int dtype)
 {
-    return tokens <= kFewMost && d % 8 == 0 && few_x((int)tokens, d, dtype == MONARCH_F32 ? 3 : 1) <= kFewSmem;
+    const bool f32 = dtype == MONARCH_F32;
+    if (d % 8 != 0 || tokens > (f32 ? 3 : 1) * kFewMost) return 0;
+    int most = kFewMost;                                                        // 227 KB of shared memory, 4 of them static
+    while (most > 0 && few_smem(most, d, f32 ? 3 : 1) > 223 * 1024) --most;
+    if (most == 0) return 0;
+    const int n = ((int)tokens + most - 1) / most;
+    return n <= (f32 ? 3 : 1) ? n : 0;
 }
 
 struct FewArgs {
@@ -614,8 +625,9 @@ template <> struct FewRaw<float> {
 };
 
 template <typename T, int PL, int NT>
-__global__ void __launch_bounds__(kFewThreads, 1) xent_few_kernel(const FewArgs p)
+__global__ void __launch_bounds__(few_threads(PL, NT), 1) xent_few_kernel(const FewArgs p)
 {
+    constexpr int kFewThreads = few_threads(PL, NT), kFewTeams = few_teams(PL, NT);
     extern __shared__ __align__(16) __nv_bfloat16 xs[];                        // [PL][tokens][row], then the sums
     __shared__ float2 s_part[kFewThreads / 32][8 * NT];
     __shared__ int s_tgt[8 * NT], s_last;
@@ -679,17 +691,13 @@ __global__ void __launch_bounds__(kFewThreads, 1) xent_few_kernel(const FewArgs 
     for (int grp = 0; grp < groups; ++grp, ++turn) {
         float z[NT][4] = {}, sum[NT][4] = {};
         for (int step = 0; step < steps; ++step) {
-            uint32_t a[kStep][2][PL][4];
-#pragma unroll
-            for (int u = 0; u < kStep; ++u) {
-                raw[u][0].planes(a[u][0]);
-                raw[u][1].planes(a[u][1]);
-            }
-            fetch(step + 1 < steps ? grp : grp + 1, step + 1 < steps ? step + 1 : 0);
 #pragma unroll
             for (int u = 0; u < kStep; ++u) {
                 const int k = k0 + step * kStep + u;
                 if (k >= k1) break;
+                uint32_t a0[PL][4], a1[PL][4];
+                raw[u][0].planes(a0);
+                raw[u][1].planes(a1);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     uint4 b[PL];
@@ -700,13 +708,13 @@ __global__ void __launch_bounds__(kFewThreads, 1) xent_few_kernel(const FewArgs 
                     for (int o = PL - 1; o >= 0; --o)
 #pragma unroll
                         for (int q = o; q >= 0; --q) {
-                            const uint32_t f0[4] = {a[u][0][q][0], a[u][1][q][0], a[u][0][q][1], a[u][1][q][1]},
-                                           f1[4] = {a[u][0][q][2], a[u][1][q][2], a[u][0][q][3], a[u][1][q][3]};
+                            const uint32_t f0[4] = {a0[q][0], a1[q][0], a0[q][1], a1[q][1]}, f1[4] = {a0[q][2], a1[q][2], a0[q][3], a1[q][3]};
                             mma(z[n], f0, b[o - q].x, b[o - q].y);
                             mma(z[n], f1, b[o - q].z, b[o - q].w);
                         }
                 }
             }
+            fetch(step + 1 < steps ? grp : grp + 1, step + 1 < steps ? step + 1 : 0);
             if (step % 8 == 7)                                                    // runs of at most 96 steps (plane_gemm.cuh)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
@@ -933,23 +941,31 @@ constexpr int kFewCtas = 148;
 
 template <typename T, int PL, int NT> int few_launch(const FewArgs &a, cudaStream_t s)
 {
-    return launch_serialized(xent_few_kernel<T, PL, NT>, dim3(kFewCtas), kFewThreads, (int)few_smem(a.tokens, a.d, PL), s, a);
+    return launch_serialized(xent_few_kernel<T, PL, NT>, dim3(kFewCtas), few_threads(PL, NT), (int)few_smem(a.tokens, a.d, PL), s, a);
 }
 template <typename T, int PL> int few_any(const FewArgs &a, cudaStream_t s)
 {
     return few_tiles(a.tokens) == 1 ? few_launch<T, PL, 1>(a, s) : few_launch<T, PL, 2>(a, s);
 }
 
-int few(const void *x, const void *W, const int64_t *targets, float *loss, float *lse, int tokens, int d, int vocab, int64_t ignore, int dtype,
+int few(int launches, const void *x, const void *W, const int64_t *targets, float *loss, float *lse, int tokens, int d, int vocab, int64_t ignore, int dtype,
         void *ws, cudaStream_t s)
 {
     FewArgs a = {};
-    a.x = x; a.W = W; a.targets = targets; a.loss = loss; a.lse = lse;
+    a.W = W;
     a.tlogit = (float *)((char *)ws + kHead);
     a.part = (float2 *)(a.tlogit + kFewMost);
     a.ticket = (unsigned *)ws + kFewTicket;
-    a.ignore = ignore; a.tokens = tokens; a.d = d; a.vocab = vocab; a.row = few_row(d);
-    return dtype == MONARCH_F32 ? few_any<float, 3>(a, s) : few_any<__nv_bfloat16, 1>(a, s);
+    a.ignore = ignore; a.d = d; a.vocab = vocab; a.row = few_row(d);
+    const int each = (tokens + launches - 1) / launches;
+    for (int t0 = 0; t0 < tokens; t0 += each) {
+        a.x = (const char *)x + (size_t)t0 * d * (dtype == MONARCH_F32 ? 4 : 2);
+        a.targets = targets + t0; a.loss = loss + t0; a.lse = lse + t0;
+        a.tokens = tokens - t0 < each ? tokens - t0 : each;
+        const int rc = dtype == MONARCH_F32 ? few_any<float, 3>(a, s) : few_any<__nv_bfloat16, 1>(a, s);
+        MONARCH_TRY(rc);
+    }
+    return MONARCH_OK;
 }
 
 }  // namespace
@@ -967,7 +983,7 @@ int xent_fwd(const void *x, const void *W, const int64_t *targets, float *loss, 
 {
     using namespace tc;
     if (tokens == 0) return MONARCH_OK;
-    if (few_fits(tokens, d, dtype)) return few(x, W, targets, loss, lse, (int)tokens, d, vocab, ignore_index, dtype, ws, s);
+    if (const int launches = few_launches(tokens, d, dtype)) return few(launches, x, W, targets, loss, lse, (int)tokens, d, vocab, ignore_index, dtype, ws, s);
     const Layout l = layout(tokens, d, vocab, dtype, false);
     char *base = (char *)ws;
     unsigned *status = (unsigned *)ws;

@@ -163,6 +163,20 @@ def test_loss_and_gradient(T, d, V, ignored, dtype):
     within(dW, e["dW"], e["dW_err"], "dW")
 
 
+@pytest.mark.parametrize("T,d,V", [(17, 1024, 3001), (32, 520, 999), (33, 520, 999), (47, 72, 5000), (48, 128, 257), (49, 128, 257), (8, 4096, 600),
+                                   (9, 4096, 600), (24, 4096, 600), (25, 4096, 600), (16, 2048, 600), (40, 2048, 600)])
+def test_loss_of_few_fp32_tokens(T, d, V):
+    """one, two or three launches of few tokens each, and the first sizes beyond them"""
+    x, W, y, _ = make(T, d, V, "f32", 0.1, seed=T + d)
+    e = exact(x, W, y)
+    loss, lse = forward(x, W, y)
+    within(loss, e["loss"], e["loss_err"], "loss")
+    within(lse, e["lse"], e["lse_err"], "lse")
+    for t in range(0, T, 5):                               # a token's result does not depend on its neighbours' launch
+        alone, _ = forward(x[t:t + 1].contiguous(), W, y[t:t + 1].contiguous())
+        within(alone, e["loss"][t:t + 1], e["loss_err"][t:t + 1], "loss of one")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_ignored_rows_may_hold_anything(dtype):
     T, d, V = 200, 96, 700
