@@ -548,9 +548,8 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const float2 *__restrict
 // (8 per column tile) wait in shared memory.  The eight warps of a team share 16 rows, an eighth of d each: their sums meet in shared
 // memory, the warps take turns to turn them into maximum and sum of exponentials while the others go on.  (A warp to itself for 16
 // rows: 3142 groups of a vocabulary of 50257 on 2368 warps are two rounds, the second a third full; 26.5 us for one token of d 1024,
-// now 23.2.)  Lanes, warps and, in the last CTA to finish, CTAs are joined.  fp32: three planes of both, six products; there up to three
-// launches, of up to 16 tokens each, are taken before the tile kernels, whose planes of W alone cost as much: 32 tokens, d 1024, a
-// vocabulary of 50257: 245 us on tiles; a launch of 16 tokens 60.  bf16: 33 us on tiles, 25 a launch, so one launch only.
+// now 23.2.)  Lanes, warps and, in the last CTA to finish, CTAs are joined.  fp32: three planes of both, six products; there several
+// launches are taken before the tile kernels, whose planes of W alone cost as much.  bf16: 41 us on tiles, 29 a launch of 16: one only.
 constexpr int kFewMost = 16, kFewTeam = 8;
 // 24 warps have 96 KB under way, 16 have 64; fp32 and a second column tile need the registers
 __host__ __device__ constexpr int few_threads(int planes, int tiles) { return planes == 1 && tiles == 1 ? 768 : 512; }
@@ -561,16 +560,18 @@ int few_row(int d) { return ((d * 2 + 127) / 128 * 128 + 64) / 2; }             
 int few_tiles(int tokens) { return tokens <= 8 ? 1 : 2; }                       // column tiles of 8 tokens: what the kernels are built for
 size_t few_x(int tokens, int d, int planes) { return (size_t)tokens * few_row(d) * 2 * planes; }
 size_t few_smem(int tokens, int d, int planes) { return few_x(tokens, d, planes) + (size_t)few_teams(planes, few_tiles(tokens)) * 2 * kFewTeam * few_tiles(tokens) * 512; }
-// launches of few tokens that the call takes; 0: tiles
-int few_launches(int64_t tokens, int d, int dtype)
+// launches of few tokens that the call takes; 0: tiles.  fp32, d 1024 / 4096 (launches of 16 / 8 tokens), vocabularies of 50257 / 32768:
+// a launch 68 / 136 us forward and 184 / 365 backward, the tile kernels 245 / 826 and 455 / 950
+int few_launches(int64_t tokens, int d, int dtype, bool bwd)
 {
     const bool f32 = dtype == MONARCH_F32;
     if (d % 8 != 0 || tokens > (f32 ? 3 : 1) * kFewMost) return 0;
     int most = kFewMost;                                                        // 227 KB of shared memory, 4 of them static
     while (most > 0 && few_smem(most, d, f32 ? 3 : 1) > 223 * 1024) --most;
     if (most == 0) return 0;
-    const int n = ((int)tokens + most - 1) / most;
-    return n <= (f32 ? 3 : 1) ? n : 0;
+    const bool all = most == kFewMost;
+    const int n = ((int)tokens + most - 1) / most, limit = !f32 ? 1 : bwd ? (all ? 2 : 1) : (all ? 3 : 6);
+    return n <= limit ? n : 0;
 }
 
 struct FewArgs {
@@ -579,6 +580,8 @@ struct FewArgs {
     float *loss, *lse, *tlogit;
     float2 *part;                               // [tokens][CTAs]
     unsigned *ticket;
+    const float *lse_in, *dloss;                // backward: g [vocab][8 or 16] in place of loss and lse
+    float *g;
     int64_t ignore;
     int tokens, d, vocab, row;
 };
@@ -624,13 +627,14 @@ template <> struct FewRaw<float> {
     }
 };
 
-template <typename T, int PL, int NT>
+template <typename T, int PL, int NT, bool BWD>
 __global__ void __launch_bounds__(few_threads(PL, NT), 1) xent_few_kernel(const FewArgs p)
 {
     constexpr int kFewThreads = few_threads(PL, NT), kFewTeams = few_teams(PL, NT);
     extern __shared__ __align__(16) __nv_bfloat16 xs[];                        // [PL][tokens][row], then the sums
     __shared__ float2 s_part[kFewThreads / 32][8 * NT];
     __shared__ int s_tgt[8 * NT], s_last;
+    __shared__ float s_lse[8 * NT], s_dl[8 * NT];
     constexpr int kStep = sizeof(T) == 2 ? 4 : 2;                               // chunks of 32 requested ahead
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     const size_t xplane = (size_t)p.tokens * p.row;
@@ -662,7 +666,14 @@ __global__ void __launch_bounds__(few_threads(PL, NT), 1) xent_few_kernel(const 
         const int part = warp - t * parts;
         const int64_t y = p.targets[t];
         const bool keep = y != p.ignore;
-        if (lane == 0 && part == 0) s_tgt[t] = !keep ? -2 : y >= 0 && y < p.vocab ? (int)y : -1;
+        if (lane == 0 && part == 0) {
+            const bool good = y >= 0 && y < p.vocab;
+            s_tgt[t] = !keep ? -2 : good ? (int)y : -1;
+            if (BWD) {
+                s_lse[t] = p.lse_in[t];
+                s_dl[t] = good ? p.dloss[t] : __int_as_float(0x7fffffff);
+            }
+        }
 #pragma unroll 4
         for (int k = (part * 32 + lane) * 2; k < p.row; k += parts * 64) {
             __nv_bfloat16 a[PL], b[PL];
@@ -738,6 +749,22 @@ __global__ void __launch_bounds__(few_threads(PL, NT), 1) xent_few_kernel(const 
 #pragma unroll
                 for (int e = 0; e < 4; ++e) t[e] += mine[((w * NT + n) * 4 + e) * 32 + lane];
 #pragma unroll
+            for (int e = 0; e < 2 && BWD; ++e) {
+                const int at = n * 8 + 2 * c + e;
+                const float l = s_lse[at], hi = l * kLog2e, lo = fmaf(l, kLog2e, -hi), dl = s_dl[at];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float x = ex2(fmaf(t[e + 2 * h], kLog2e, -hi) - lo);
+                    t[e + 2 * h] = tgt[n][e] == -2 ? 0.0f : dl * (tgt[n][e] == r0 + 8 * h ? x - 1.0f : x);
+                }
+            }
+            if (BWD) {
+                float *to = p.g + (size_t)r0 * (8 * NT) + n * 8 + 2 * c;
+                if (r0 < row1) *reinterpret_cast<float2 *>(to) = make_float2(t[0], t[1]);
+                if (r1 < row1) *reinterpret_cast<float2 *>(to + 64 * NT) = make_float2(t[2], t[3]);
+                continue;
+            }
+#pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const float z0 = t[e], z1 = t[e + 2];
                 if (r0 == tgt[n][e] && r0 < row1) p.tlogit[n * 8 + 2 * c + e] = z0;
@@ -749,6 +776,7 @@ __global__ void __launch_bounds__(few_threads(PL, NT), 1) xent_few_kernel(const 
             }
         }
     }
+    if (BWD) return;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -787,6 +815,188 @@ __global__ void __launch_bounds__(few_threads(PL, NT), 1) xent_few_kernel(const 
             p.loss[t] = y == -2 ? 0.0f : y >= 0 ? l - __ldcg(p.tlogit + t) : __int_as_float(0x7fffffff);
         }
     }
+}
+
+// ------------------------------------------------------------------------------------------------ gradients of few tokens
+// With g [vocab][8 or 16] from the kernel above: dW = g^T x and dx = g W in one pass over W and dW, in fp32 FMAs packed over pairs of
+// tokens (dW takes (g, g') (x, x') and adds the halves at the end, dx (g, g') (w, w)).  A lane keeps x and the sums of dx for its columns
+// (4, of 16 tokens 2) in registers; a warp takes eight rows at a time (fp32: 4, for the registers: 186 -> 141 us of a call), asks for the
+// next as it goes, and its values of g wait in shared memory.  The eight warps' and then the CTAs' sums of dx are added in a fixed order.
+// d 1024, a vocabulary of 50257, us of this kernel (of the call; on tiles): 8 tokens bf16 65 (93; 153) = 309 MB at 4.7 TB/s, fp32 76
+// (142; 452) = 412 MB at 5.4 TB/s, both bound by memory; 16 tokens bf16 110 (140; 153), fp32 122 (184; 454), bound by the FMAs.
+template <typename T> constexpr int kFewRows = sizeof(T) == 2 ? 8 : 4;           // of a warp's step
+
+struct FewGradArgs {
+    const void *x, *W;
+    const int64_t *targets;
+    const float *g;
+    float *dW, *part;                           // part: [parts][tokens][d]
+    int64_t ignore;
+    int tokens, d, vocab, rows, accumulate;     // rows of W per CTA
+};
+
+// C consecutive values
+template <typename T, int C> struct FewCols;
+template <int C> struct FewCols<__nv_bfloat16, C> {
+    uint32_t v[C / 2];
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p, bool in)
+    {
+        if constexpr (C == 4) {
+            const uint2 w = in ? __ldcs(reinterpret_cast<const uint2 *>(p)) : make_uint2(0, 0);
+            v[0] = w.x; v[1] = w.y;
+        } else {
+            v[0] = in ? __ldcs(reinterpret_cast<const uint32_t *>(p)) : 0u;
+        }
+    }
+    __device__ __forceinline__ float at(int i) const { return __uint_as_float(i & 1 ? v[i / 2] & 0xffff0000u : v[i / 2] << 16); }
+};
+template <int C> struct FewCols<float, C> {
+    float2 v[C / 2];
+    __device__ __forceinline__ void load(const float *p, bool in)
+    {
+        if constexpr (C == 4) {
+            const float4 w = in ? __ldcs(reinterpret_cast<const float4 *>(p)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            v[0] = make_float2(w.x, w.y); v[1] = make_float2(w.z, w.w);
+        } else {
+            v[0] = in ? __ldcs(reinterpret_cast<const float2 *>(p)) : make_float2(0.0f, 0.0f);
+        }
+    }
+    __device__ __forceinline__ float at(int i) const { return i & 1 ? v[i / 2].y : v[i / 2].x; }
+};
+
+template <typename T, int TP>
+__global__ void __launch_bounds__(256, 2) xent_few_grad_kernel(const FewGradArgs p)
+{
+    constexpr int R = kFewRows<T>, C = 32 / TP, G = R * TP / 32;               // columns of a lane, values of g it fetches
+    __shared__ __align__(16) float s_g[8][R][TP];
+    __shared__ float s_dx[TP][32 * C];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = blockIdx.x * 32 * C + lane * C;
+    const bool live = col < p.d;                                               // d % 8 == 0
+    const int row0 = blockIdx.y * p.rows, row1 = min(row0 + p.rows, p.vocab);
+    depend_wait();
+    depend_launch();
+    FewCols<T, C> w[R];
+    float g[G];
+    const int r_g = lane * G / TP;                                             // the row of this lane's values of g
+    auto fetch_g = [&](int r) {
+        const float *from = p.g + (size_t)r * TP + lane * G;
+        const bool in = r + r_g < row1;
+        if constexpr (G == 4) {
+            const float4 v = in ? *reinterpret_cast<const float4 *>(from) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            g[0] = v.x; g[1] = v.y; g[2] = v.z; g[3] = v.w;
+        } else if constexpr (G == 1) {
+            g[0] = in ? *from : 0.0f;
+        } else {
+            const float2 v = in ? *reinterpret_cast<const float2 *>(from) : make_float2(0.0f, 0.0f);
+            g[0] = v.x; g[1] = v.y;
+        }
+    };
+    auto fetch_w = [&](int r, int u) { w[u].load((const T *)p.W + (size_t)(r + u) * p.d + col, live && r + u < row1); };
+    int r = row0 + warp * R;
+#pragma unroll
+    for (int u = 0; u < R; ++u) fetch_w(r, u);
+    fetch_g(r);
+    f32x2 x[TP / 2][C], dx[TP / 2][C];                                         // pairs of tokens
+#pragma unroll
+    for (int t = 0; t < TP; t += 2) {
+        FewCols<T, C> v[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            v[k].load((const T *)p.x + (size_t)(t + k) * p.d + col, live && t + k < p.tokens && p.targets[t + k < p.tokens ? t + k : 0] != p.ignore);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            x[t / 2][c] = pack2(v[0].at(c), v[1].at(c));
+            dx[t / 2][c] = pack2(0.0f, 0.0f);
+        }
+    }
+    for (; r < row1; r += 8 * R) {
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < G; ++i) s_g[warp][r_g][lane * G % TP + i] = g[i];
+        __syncwarp();
+        fetch_g(r + 8 * R);
+#pragma unroll
+        for (int u = 0; u < R; ++u) {
+            f32x2 v[C], o[C];
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const float f = w[u].at(c);
+                v[c] = pack2(f, f);
+                o[c] = pack2(0.0f, 0.0f);
+            }
+            fetch_w(r + 8 * R, u);
+#pragma unroll
+            for (int t = 0; t < TP / 2; t += 2) {
+                const ulonglong2 gg = *reinterpret_cast<const ulonglong2 *>(&s_g[warp][u][2 * t]);
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    o[c] = fma2(gg.x, x[t][c], o[c]);
+                    dx[t][c] = fma2(gg.x, v[c], dx[t][c]);
+                    o[c] = fma2(gg.y, x[t + 1][c], o[c]);
+                    dx[t + 1][c] = fma2(gg.y, v[c], dx[t + 1][c]);
+                }
+            }
+            if (live && r + u < row1) {
+                float *to = p.dW + (size_t)(r + u) * p.d + col;
+                float f[C];
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    const float2 h = unpack2(o[c]);
+                    f[c] = h.x + h.y;
+                }
+                if (p.accumulate) {                                            // one addition of one thread to each value; nothing waits for it
+                    if constexpr (C == 4)
+                        asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(to), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]) : "memory");
+                    else
+                        asm volatile("red.relaxed.gpu.global.add.v2.f32 [%0], {%1, %2};" ::"l"(to), "f"(f[0]), "f"(f[1]) : "memory");
+                } else if constexpr (C == 4) {
+                    __stcs(reinterpret_cast<float4 *>(to), make_float4(f[0], f[1], f[2], f[3]));
+                } else {
+                    __stcs(reinterpret_cast<float2 *>(to), make_float2(f[0], f[1]));
+                }
+            }
+        }
+    }
+    for (int q = 0; q < 8; ++q) {
+        if (warp == q)
+#pragma unroll
+            for (int t = 0; t < TP; t += 2)
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    float2 v = unpack2(dx[t / 2][c]);
+                    float *to = &s_dx[t][lane * C + c];
+                    if (q > 0) { v.x += to[0]; v.y += to[32 * C]; }
+                    to[0] = v.x;
+                    to[32 * C] = v.y;
+                }
+        __syncthreads();
+    }
+    for (int i = threadIdx.x; i < p.tokens * 32 * C; i += 256) {
+        const int t = i / (32 * C), c = blockIdx.x * 32 * C + i % (32 * C);
+        if (c < p.d) p.part[((size_t)blockIdx.y * p.tokens + t) * p.d + c] = s_dx[t][i % (32 * C)];
+    }
+}
+
+// the CTAs' sums: a CTA per 32 columns of a token, eight warps an eighth of the parts each
+template <typename T>
+__global__ void __launch_bounds__(256) xent_few_dx_kernel(const float *part, const int64_t *targets, int64_t ignore, T *dx, int tokens, int d, int parts)
+{
+    __shared__ float s[8][32];
+    depend_wait();
+    depend_launch();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = blockIdx.x * 32 + lane, t = blockIdx.y;
+    const size_t step = (size_t)tokens * d;
+    const float *in = part + (size_t)t * d + c;
+    float v = 0.0f;
+    if (c < d)
+#pragma unroll 8
+        for (int q = warp; q < parts; q += 8) v += in[q * step];
+    s[warp][lane] = v;
+    __syncthreads();
+    if (warp != 0 || c >= d) return;
+#pragma unroll
+    for (int q = 1; q < 8; ++q) v += s[q][lane];
+    elem<T>::store(dx + (size_t)t * d + c, targets[t] == ignore ? 0.0f : v);
 }
 
 // ------------------------------------------------------------------------------------------------ host side
@@ -939,13 +1149,13 @@ namespace {
 
 constexpr int kFewCtas = 148;
 
-template <typename T, int PL, int NT> int few_launch(const FewArgs &a, cudaStream_t s)
+template <typename T, int PL, int NT, bool BWD> int few_launch(const FewArgs &a, cudaStream_t s)
 {
-    return launch_serialized(xent_few_kernel<T, PL, NT>, dim3(kFewCtas), few_threads(PL, NT), (int)few_smem(a.tokens, a.d, PL), s, a);
+    return launch_serialized(xent_few_kernel<T, PL, NT, BWD>, dim3(kFewCtas), few_threads(PL, NT), (int)few_smem(a.tokens, a.d, PL), s, a);
 }
-template <typename T, int PL> int few_any(const FewArgs &a, cudaStream_t s)
+template <typename T, int PL, bool BWD> int few_any(const FewArgs &a, cudaStream_t s)
 {
-    return few_tiles(a.tokens) == 1 ? few_launch<T, PL, 1>(a, s) : few_launch<T, PL, 2>(a, s);
+    return few_tiles(a.tokens) == 1 ? few_launch<T, PL, 1, BWD>(a, s) : few_launch<T, PL, 2, BWD>(a, s);
 }
 
 int few(int launches, const void *x, const void *W, const int64_t *targets, float *loss, float *lse, int tokens, int d, int vocab, int64_t ignore, int dtype,
@@ -962,7 +1172,49 @@ int few(int launches, const void *x, const void *W, const int64_t *targets, floa
         a.x = (const char *)x + (size_t)t0 * d * (dtype == MONARCH_F32 ? 4 : 2);
         a.targets = targets + t0; a.loss = loss + t0; a.lse = lse + t0;
         a.tokens = tokens - t0 < each ? tokens - t0 : each;
-        const int rc = dtype == MONARCH_F32 ? few_any<float, 3>(a, s) : few_any<__nv_bfloat16, 1>(a, s);
+        const int rc = dtype == MONARCH_F32 ? few_any<float, 3, false>(a, s) : few_any<__nv_bfloat16, 1, false>(a, s);
+        MONARCH_TRY(rc);
+    }
+    return MONARCH_OK;
+}
+
+// CTAs along the vocabulary for two per SM
+int few_parts(int d, int vocab, int tiles)
+{
+    const int wide = ceil_div(d, 128 / tiles), most = ceil_div(vocab, 64), want = 2 * kFewCtas / wide;
+    return want < 1 ? 1 : want < most ? want : most;
+}
+size_t few_bwd_bytes(int d, int vocab) { return kHead + up((size_t)vocab * kFewMost * 4) + (size_t)few_parts(d, vocab, 1) * kFewMost * d * 4; }
+
+template <typename T, int TP> int few_grad_launch(FewGradArgs a, T *dx, cudaStream_t s)
+{
+    const int parts = few_parts(a.d, a.vocab, TP / 8);
+    a.rows = ceil_div(a.vocab, parts);
+    const int used = ceil_div(a.vocab, a.rows);
+    MONARCH_TRY(launch_serialized(xent_few_grad_kernel<T, TP>, dim3(ceil_div(a.d, 1024 / TP), used), 256, 0, s, a));
+    return launch_serialized(xent_few_dx_kernel<T>, dim3(ceil_div(a.d, 32), a.tokens), 256, 0, s, a.part, a.targets, a.ignore, dx, a.tokens, a.d, used);
+}
+
+template <typename T, int PL>
+int few_bwd(int launches, const T *x, const T *W, const int64_t *targets, const float *lse, const float *dloss, T *dx, float *dW, int accumulate, int tokens,
+            int d, int vocab, int64_t ignore, void *ws, cudaStream_t s)
+{
+    FewArgs a = {};
+    a.W = W;
+    a.g = (float *)((char *)ws + kHead);
+    a.ignore = ignore; a.d = d; a.vocab = vocab; a.row = few_row(d);
+    FewGradArgs b = {};
+    b.W = W; b.g = a.g; b.dW = dW; b.part = (float *)((char *)ws + kHead + up((size_t)vocab * kFewMost * 4));
+    b.ignore = ignore; b.d = d; b.vocab = vocab;
+    const int each = (tokens + launches - 1) / launches;
+    for (int t0 = 0; t0 < tokens; t0 += each) {
+        b.x = a.x = x + (size_t)t0 * d;
+        b.targets = a.targets = targets + t0; a.lse_in = lse + t0; a.dloss = dloss + t0;
+        b.tokens = a.tokens = tokens - t0 < each ? tokens - t0 : each;
+        b.accumulate = accumulate || t0 > 0;
+        int rc = few_any<T, PL, true>(a, s);
+        MONARCH_TRY(rc);
+        rc = few_tiles(a.tokens) == 1 ? few_grad_launch<T, 8>(b, dx + (size_t)t0 * d, s) : few_grad_launch<T, 16>(b, dx + (size_t)t0 * d, s);
         MONARCH_TRY(rc);
     }
     return MONARCH_OK;
@@ -974,7 +1226,8 @@ int few(int launches, const void *x, const void *W, const int64_t *targets, floa
 size_t xent_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab, int dtype, int bwd)
 {
     // a workspace sized for a batch serves every smaller one, on whichever kernels: also the few tokens' parts
-    const size_t few = tc::kHead + tc::kFewMost * (4 + 8 * tc::kFewCtas), need = tc::layout(tokens, d, vocab, dtype, bwd != 0).total;
+    const size_t few = bwd ? tc::few_bwd_bytes(d, vocab) : tc::kHead + tc::kFewMost * (4 + 8 * tc::kFewCtas);
+    const size_t need = tc::layout(tokens, d, vocab, dtype, bwd != 0).total;
     return need > few ? need : few;
 }
 
@@ -983,7 +1236,7 @@ int xent_fwd(const void *x, const void *W, const int64_t *targets, float *loss, 
 {
     using namespace tc;
     if (tokens == 0) return MONARCH_OK;
-    if (const int launches = few_launches(tokens, d, dtype)) return few(launches, x, W, targets, loss, lse, (int)tokens, d, vocab, ignore_index, dtype, ws, s);
+    if (const int launches = few_launches(tokens, d, dtype, false)) return few(launches, x, W, targets, loss, lse, (int)tokens, d, vocab, ignore_index, dtype, ws, s);
     const Layout l = layout(tokens, d, vocab, dtype, false);
     char *base = (char *)ws;
     unsigned *status = (unsigned *)ws;
@@ -1122,6 +1375,12 @@ int xent_bwd(const void *x, const void *W, const int64_t *targets, const float *
     if (tokens == 0) {
         if (!accumulate) MONARCH_CUDA_TRY(cudaMemsetAsync(dW, 0, (size_t)vocab * d * sizeof(float), s));
         return MONARCH_OK;
+    }
+    if (const int launches = few_launches(tokens, d, dtype, true)) {
+        if (dtype == MONARCH_F32)
+            return few_bwd<float, 3>(launches, (const float *)x, (const float *)W, targets, lse, dloss, (float *)dx, dW, accumulate, (int)tokens, d, vocab, ignore_index, ws, s);
+        return few_bwd<__nv_bfloat16, 1>(launches, (const __nv_bfloat16 *)x, (const __nv_bfloat16 *)W, targets, lse, dloss, (__nv_bfloat16 *)dx, dW, accumulate, (int)tokens, d, vocab,
+                                         ignore_index, ws, s);
     }
     const Layout l = layout(tokens, d, vocab, dtype, true);
     char *base = (char *)ws;

@@ -172,6 +172,11 @@ def test_loss_of_few_fp32_tokens(T, d, V):
     loss, lse = forward(x, W, y)
     within(loss, e["loss"], e["loss_err"], "loss")
     within(lse, e["lse"], e["lse_err"], "lse")
+    dloss = torch.rand(T, generator=gen(T), device="cuda")
+    b = exact(x, W, y, dloss)
+    dx, dW = backward(x, W, y, e["lse"].float(), dloss)
+    within(dx, b["dx"], b["dx_err"], "dx")
+    within(dW, b["dW"], b["dW_err"], "dW")
     for t in range(0, T, 5):                               # a token's result does not depend on its neighbours' launch
         alone, _ = forward(x[t:t + 1].contiguous(), W, y[t:t + 1].contiguous())
         within(alone, e["loss"][t:t + 1], e["loss_err"][t:t + 1], "loss of one")
@@ -215,6 +220,51 @@ def test_every_token_ignored_and_no_tokens():
     assert (dW == 0).all()
     _, dW = backward(empty, W, y[:0], lse, dloss[:0], dW0=before)
     assert torch.equal(dW, before)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d,V", [(1, 8, 1), (1, 520, 70), (3, 136, 4097), (8, 1024, 3001), (9, 1032, 600), (13, 40, 20000), (16, 64, 63), (16, 2048, 900)])
+def test_gradient_of_few_tokens(T, d, V, dtype):
+    """Up to 16 tokens: masked rows that are not numbers, targets out of range, added to what is there, the same bits again and replayed."""
+    x, W, y, dloss = make(T, d, V, dtype, 0.3, seed=T * d)
+    e = exact(x, W, y, dloss)
+    lse = e["lse"].float()
+    out = y == IGNORE
+    x[out] = float("nan")
+    dloss[out] = float("inf")
+    lse[out] = float("nan")
+    before = torch.randn(V, d, device="cuda")
+    dx, dW = backward(x, W, y, lse, dloss, dW0=before)
+    within(dx, e["dx"], e["dx_err"], "dx")
+    assert (dx[out] == 0).all()
+    within(dW, e["dW"] + before.double(), e["dW_err"] + (before.double().abs() + e["dW"].abs()) * 2.0 ** -23, "dW")
+    dx, dW = backward(x, W, y, lse, dloss)
+    within(dx, e["dx"], e["dx_err"], "dx")
+    within(dW, e["dW"], e["dW_err"], "dW")
+    ws = P.Workspace(P.monarch_xent_bwd_workspace_bytes(T, d, V, DT[dtype][1]))
+    gx, gw = torch.zeros_like(x), torch.zeros(V, d, device="cuda")
+    ys = torch.full_like(y, IGNORE)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        P.monarch_xent_bwd(x, W, ys, lse, dloss, gx, gw, 0, T, d, V, IGNORE, ws)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        P.monarch_xent_bwd(x, W, ys, lse, dloss, gx, gw, 0, T, d, V, IGNORE, ws)
+    graph.replay()
+    assert (gw == 0).all() and (gx == 0).all()
+    ys.copy_(y)
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(gx, dx) and torch.equal(gw, dW)
+    keep = torch.nonzero(~out)[:, 0]
+    if keep.numel() > 1:
+        y[keep[0]] = V
+        dx, dW = backward(x, W, y, lse, dloss)
+        assert torch.isnan(dx[keep[0]]).all() and torch.isnan(dW).all()
+        within(dx[keep[1:]], e["dx"][keep[1:]], e["dx_err"][keep[1:]], "dx")
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
