@@ -269,8 +269,10 @@ __device__ __forceinline__ void plane_mma(float (&acc)[T][4], uint32_t a, uint32
     const int lane = threadIdx.x & 31, mtx = lane >> 3, r = lane & 7;
     // A: matrices (rows 0-7, k 0-7), (rows 8-15, k 0-7), (rows 0-7, k 8-15), (rows 8-15, k 8-15)
     const uint32_t a_at = a + ((mtx & 1) * 8 + r) * lda * 2 + (mtx >> 1) * 16;
-    // B, two column tiles at a time: (n 0-7, k 0-7), (n 0-7, k 8-15), (n 8-15, k 0-7), (n 8-15, k 8-15)
-    const uint32_t b_at = TRANS ? b + ((mtx & 1) * 8 + r) * ldb * 2 + (mtx >> 1) * 16 : b + ((mtx >> 1) * 8 + r) * ldb * 2 + (mtx & 1) * 16;
+    // B, two column tiles at a time: (n 0-7, k 0-7), (n 0-7, k 8-15), (n 8-15, k 0-7), (n 8-15, k 8-15); of an odd T the last one
+    // alone, twice: what would be the other one's rows may lie behind the planes
+    const uint32_t b_at = TRANS ? b + ((mtx & 1) * 8 + r) * ldb * 2 : b + r * ldb * 2 + (mtx & 1) * 16;
+    const uint32_t second = TRANS ? (mtx >> 1) * 16 : (mtx >> 1) * 8 * ldb * 2;
 #pragma unroll
     for (int k = 0; k < KSTEPS; ++k) {
         uint32_t fa[PL][4];
@@ -278,11 +280,12 @@ __device__ __forceinline__ void plane_mma(float (&acc)[T][4], uint32_t a, uint32
         for (int q = 0; q < PL; ++q) ldm4(fa[q], a_at + q * aplane + k * 32);
 #pragma unroll
         for (int t = 0; t < T; t += 2) {
+            const uint32_t at = b_at + (t + 1 < T ? second : 0);
             uint32_t fb[PL][4];
 #pragma unroll
             for (int q = 0; q < PL; ++q) {
-                if constexpr (TRANS) ldm4t(fb[q], b_at + q * bplane + k * 16 * ldb * 2 + t * 16);
-                else ldm4(fb[q], b_at + q * bplane + t * 8 * ldb * 2 + k * 32);
+                if constexpr (TRANS) ldm4t(fb[q], at + q * bplane + k * 16 * ldb * 2 + t * 16);
+                else ldm4(fb[q], at + q * bplane + t * 8 * ldb * 2 + k * 32);
             }
             // the small products first
 #pragma unroll

@@ -532,6 +532,15 @@ def test_orthogonalize(blocks, rows, cols, dtype):
     near(ortho(G), newton_schulz(G.double()), dtype, "O")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("blocks,rows,cols", [(132, 5, 251), (3, 251, 5), (2, 16, 256), (300, 16, 129), (1, 1, 200), (2, 17, 256), (2, 16, 257), (2, 16, 128),
+                                              (2, 9, 65), (2, 33, 256), (2, 48, 130), (2, 64, 256), (2, 65, 256), (2, 32, 257)])
+def test_orthogonalize_sides_where_the_kernels_change(blocks, rows, cols, dtype):
+    """Both sides of the rules that choose a kernel and its padding; 16 x 256 has one column tile per warp and one buffer of X."""
+    G = gradient(blocks, rows, cols, seed=rows * 7 + cols).to(DT[dtype][0])
+    near(ortho(G), newton_schulz(G.double()), dtype, "O")
+
+
 @pytest.mark.parametrize("steps", [1, 2, 3, 7])
 @pytest.mark.parametrize("blocks,rows,cols", [(3, 24, 40), (2, 150, 140)])
 def test_other_numbers_of_steps(blocks, rows, cols, steps):
