@@ -263,7 +263,9 @@ template <int KP, int NP, int PL> struct BlockCfg {
 };
 
 // acc[t] += A B for T column tiles of 8.  A: planes at `a` (row-major, 16 rows of this warp), B: planes at `b`, TRANS: stored [k][n].
-template <int PL, int KSTEPS, int T, bool TRANS>
+// An MMA adds without rounding to nearest, so what a sum loses goes by the number of its products; APART: those of the first planes have a
+// sum of their own, which takes a sixth of them (fp32; bf16: a third), and the small ones are added to it at the end.
+template <int PL, int KSTEPS, int T, bool TRANS, bool APART = false>
 __device__ __forceinline__ void plane_mma(float (&acc)[T][4], uint32_t a, uint32_t aplane, int lda, uint32_t b, uint32_t bplane, int ldb)
 {
     const int lane = threadIdx.x & 31, mtx = lane >> 3, r = lane & 7;
@@ -273,6 +275,7 @@ __device__ __forceinline__ void plane_mma(float (&acc)[T][4], uint32_t a, uint32
     // alone, twice: what would be the other one's rows may lie behind the planes
     const uint32_t b_at = TRANS ? b + ((mtx & 1) * 8 + r) * ldb * 2 : b + r * ldb * 2 + (mtx & 1) * 16;
     const uint32_t second = TRANS ? (mtx >> 1) * 16 : (mtx >> 1) * 8 * ldb * 2;
+    float low[APART ? T : 1][4] = {};
 #pragma unroll
     for (int k = 0; k < KSTEPS; ++k) {
         uint32_t fa[PL][4];
@@ -292,11 +295,17 @@ __device__ __forceinline__ void plane_mma(float (&acc)[T][4], uint32_t a, uint32
             for (int o = PL - 1; o >= 0; --o)
 #pragma unroll
                 for (int q = o; q >= 0; --q) {
-                    mma(acc[t], fa[q], fb[o - q][0], fb[o - q][1]);
-                    if (t + 1 < T) mma(acc[t + 1], fa[q], fb[o - q][2], fb[o - q][3]);
+                    float (*to)[4] = APART && o > 0 ? low : acc;
+                    mma(to[t], fa[q], fb[o - q][0], fb[o - q][1]);
+                    if (t + 1 < T) mma(to[t + 1], fa[q], fb[o - q][2], fb[o - q][3]);
                 }
         }
     }
+    if constexpr (APART)
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[t][e] += low[t][e];
 }
 
 // this thread's values of T column tiles as planes: rows row, row + 8
@@ -375,10 +384,10 @@ __global__ void __launch_bounds__(BlockCfg<KP, NP, PL>::kThreads) ortho_block_ke
         __syncthreads();
         const uint32_t X = smem_u32(Xs) + (C::kXBufs > 1 ? it & 1 : 0) * (PL * C::kXPlane * 2);
         float s[C::kS][4] = {}, p[C::kS][4] = {};
-        plane_mma<PL, NP / 16, C::kS, false>(s, X + row0 * C::kLdX * 2, C::kXPlane * 2, C::kLdX, X + half * (KP / 2) * C::kLdX * 2, C::kXPlane * 2, C::kLdX);
+        plane_mma<PL, NP / 16, C::kS, false, true>(s, X + row0 * C::kLdX * 2, C::kXPlane * 2, C::kLdX, X + half * (KP / 2) * C::kLdX * 2, C::kXPlane * 2, C::kLdX);
         put_tiles<PL>(s, Ss + s_at, C::kSPlane, C::kLdS);
         __syncthreads();
-        plane_mma<PL, KP / 16, C::kS, false>(p, s_a, C::kSPlane * 2, C::kLdS, s_b, C::kSPlane * 2, C::kLdS);
+        plane_mma<PL, KP / 16, C::kS, false, true>(p, s_a, C::kSPlane * 2, C::kLdS, s_b, C::kSPlane * 2, C::kLdS);
 #pragma unroll
         for (int t = 0; t < C::kS; ++t)
 #pragma unroll

@@ -1132,11 +1132,12 @@ PlaneGemm gemm(unsigned *status)
     return g;
 }
 
-// Logits.  An error of z is a relative error of g, so their sums in tensor memory end after 64 (bf16) or 24 (fp32) steps
-// (pg_seg); the loss alone takes less harm (bf16, d = 1024: 3.4e-7 of lse).
-template <int SCHEME, class Epi> int logits(const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mc, PlaneGemm p, const typename Epi::Args &e, bool exact, cudaStream_t s)
+// Logits.  An error of z is a relative error of g, so their sums in tensor memory end after 64 (bf16) or 24 (fp32) steps (pg_seg), for
+// few tokens, where time is not the matter, after 16; the loss takes less harm: 96 (bf16, 64 steps: 3.4e-7 of lse; 241 steps: 2e-6).
+template <int SCHEME, class Epi>
+int logits(const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mc, PlaneGemm p, const typename Epi::Args &e, int seg, bool exact, cudaStream_t s)
 {
-    p.seg = pg_seg(SCHEME);
+    p.seg = seg < pg_seg(SCHEME) ? seg : pg_seg(SCHEME);
     if (exact && p.kdim > p.seg * kPgChunk) return launch_plane_gemm<0, 0, SCHEME, true, Epi>(ma, mb, mc, p, e, s);
     return launch_plane_gemm<0, 0, SCHEME, false, Epi>(ma, mb, mc, p, e, s);
 }
@@ -1272,8 +1273,8 @@ int xent_fwd(const void *x, const void *W, const int64_t *targets, float *loss, 
             }
             const EpiStats::Args e = {part, tlogit, tgt, count, (int)row0, cols, v0, l.halves, half0};
             half0 += 2 * ceil_div(cols, l.tn);
-            if (dtype == MONARCH_F32) MONARCH_TRY((logits<kP3x3, EpiStats>(ma, mb, mb, p, e, true, s)));
-            else MONARCH_TRY((logits<kP1, EpiStats>(ma, mb, mb, p, e, d > 8192, s)));
+            if (dtype == MONARCH_F32) MONARCH_TRY((logits<kP3x3, EpiStats>(ma, mb, mb, p, e, 16, true, s)));
+            else MONARCH_TRY((logits<kP1, EpiStats>(ma, mb, mb, p, e, 16, d > 1536, s)));
         }
         const int ctas = ceil_div(rows, 8) < 148 * 8 ? ceil_div(rows, 8) : 148 * 8;
         MONARCH_TRY(launch_serialized(xent_join_kernel, dim3((unsigned)ctas), 256, 0, s, (const float2 *)part, (const float *)tlogit,
@@ -1330,7 +1331,7 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
         p.count = count; p.rows = (int)tokens; p.cols = cols; p.kdim = d; p.tn = l.tn;
         p.b_n0 = l.direct ? v0 : 0;
         const typename EpiGrad<GP, HALF>::Args eg = {cols, v0, tgt, count, clse, cdl, exponent, largest};
-        MONARCH_TRY((logits<LOGITS, EpiGrad<GP, HALF>>(x_k, w_k, g_to, p, eg, true, s)));
+        MONARCH_TRY((logits<LOGITS, EpiGrad<GP, HALF>>(x_k, w_k, g_to, p, eg, tokens <= kFewTokens ? 4 : 16, true, s)));
         // dW = g^T x
         p = gemm(status);
         p.count = count; p.count_is_k = 1; p.rows = cols; p.cols = d; p.kdim = (int)tokens; p.tn = l.tn_dw;
