@@ -1133,7 +1133,9 @@ PlaneGemm gemm(unsigned *status)
 }
 
 // Logits.  An error of z is a relative error of g, so their sums in tensor memory end after 64 (bf16) or 24 (fp32) steps (pg_seg), for
-// few tokens, where time is not the matter, after 16; the loss takes less harm: 96 (bf16, 64 steps: 3.4e-7 of lse; 241 steps: 2e-6).
+// few tokens, where time is not the matter, after 16, and up to 512 tokens after 32 (100 tokens: dW 1.01e-6 -> 5.8e-7 off; of 1000 on
+// dW's own sums weigh as much, 1.07e-6 -> 1.01e-6, and 4096 tokens would take 4 % longer).  The loss takes less harm: 96 (bf16, 64 steps:
+// 3.4e-7 of lse; 241 steps: 2e-6).
 template <int SCHEME, class Epi>
 int logits(const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mc, PlaneGemm p, const typename Epi::Args &e, int seg, bool exact, cudaStream_t s)
 {
@@ -1331,7 +1333,7 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
         p.count = count; p.rows = (int)tokens; p.cols = cols; p.kdim = d; p.tn = l.tn;
         p.b_n0 = l.direct ? v0 : 0;
         const typename EpiGrad<GP, HALF>::Args eg = {cols, v0, tgt, count, clse, cdl, exponent, largest};
-        MONARCH_TRY((logits<LOGITS, EpiGrad<GP, HALF>>(x_k, w_k, g_to, p, eg, tokens <= kFewTokens ? 4 : 16, true, s)));
+        MONARCH_TRY((logits<LOGITS, EpiGrad<GP, HALF>>(x_k, w_k, g_to, p, eg, tokens <= kFewTokens ? 4 : tokens <= 512 ? 8 : 16, true, s)));
         // dW = g^T x
         p = gemm(status);
         p.count = count; p.count_is_k = 1; p.rows = cols; p.cols = d; p.kdim = (int)tokens; p.tn = l.tn_dw;
