@@ -397,6 +397,7 @@ struct EpiStoreF32 {
         int rows, cols, add;
         int y0;                    // of these rows in the map that TMA writes by; -1: none
         const int *largest;        // E of fp16 parts, or null
+        size_t part;               // values of a part of the tokens, where there are several
     };
     int e;
     __device__ __forceinline__ void begin(const Args &a, const PgTile &) { e = a.largest != nullptr ? *a.largest - kBias - 13 : 0; }
@@ -409,11 +410,11 @@ struct EpiStoreF32 {
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] = v[i] * f1 * f2;
         if (a.y0 >= 0) {
-            if ((t.row & ~31) < a.rows && t.col + c < a.cols) st.tile(v, t.col + c, a.y0 + (t.row & ~31), 0, a.add);
+            if ((t.row & ~31) < a.rows && t.col + c < a.cols) st.tile(v, t.col + c, a.y0 + (t.row & ~31), t.z, a.add);
             return;
         }
         const int col = t.col + c + st.lane, row0 = t.row & ~31, rows = col < a.cols ? a.rows - row0 : 0;
-        float *out = a.out + (size_t)row0 * a.cols + col;
+        float *out = a.out + t.z * a.part + (size_t)row0 * a.cols + col;
         st.rows(
             v, [&](int r) { return a.add && r < rows ? out[(size_t)r * a.cols] : 0.0f; },
             [&](int r, float x, float w) {
@@ -510,6 +511,31 @@ __global__ void __launch_bounds__(256) xent_dx_kernel(const float *__restrict__ 
 #pragma unroll 8
             for (int q = 0; q < parts; ++q) v += in[q * part + c];
             elem<T>::store(out + c, v);
+        }
+    }
+}
+
+// the parts of dW, added up (and to what is there); n values, V of them a thread
+template <int V>
+__global__ void __launch_bounds__(256) xent_dw_kernel(const float *__restrict__ acc, size_t part, const int *__restrict__ splits, float *dW, long long n, int add)
+{
+    depend_wait();
+    depend_launch();
+    const int parts = *splits;
+    for (long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * V; i < n; i += (long long)gridDim.x * 256 * V) {
+        if constexpr (V == 4) {
+            float4 v = add ? *reinterpret_cast<const float4 *>(dW + i) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+            for (int q = 0; q < parts; ++q) {
+                const float4 w = *reinterpret_cast<const float4 *>(acc + q * part + i);
+                v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+            }
+            *reinterpret_cast<float4 *>(dW + i) = v;
+        } else {
+            float v = add ? dW[i] : 0.0f;
+#pragma unroll 8
+            for (int q = 0; q < parts; ++q) v += acc[q * part + i];
+            dW[i] = v;
         }
     }
 }
@@ -1011,9 +1037,9 @@ struct Layout {
     int planes, gplanes, dp, piece;             // planes of x and W, of g; padded row; vocabulary entries per piece
     int chunk, halves, trows;
     int tn, tn_dw, tn_dx;                       // columns of a tile: logits, dW, dx
-    int dx_parts;                               // most parts of the vocabulary in dx; 1: no parts
+    int dx_parts, dw_parts;                     // most parts of the vocabulary in dx, of the tokens in dW; 1: no parts
     bool half;                                  // dW from fp16 parts
-    size_t count, splits, largest, exponent, xh, map, tgt, lse, dl, tlogit, x, w, part, g, dx, total;
+    size_t count, splits, largest, exponent, xh, map, tgt, lse, dl, tlogit, x, w, part, g, dx, dw_splits, dw, total;
 };
 
 // Vocabulary entries per piece of the backward pass: whole 256-entry tiles, a plane of g within 160 MB, and
@@ -1072,6 +1098,15 @@ Layout layout(int64_t tokens, int d, int vocab, int dtype, bool bwd)
     if (parts > l.piece / 256) parts = l.piece / 256;
     if (parts > kPgPairs) parts = kPgPairs;
     l.dx_parts = tiles >= 4 * kPgPairs || parts < 1 ? 1 : (int)parts;
+    // dW of a small vocabulary is a few tiles, long ones: split along the tokens, 512 at least (whole calls, fp32 / bf16: 16384 tokens, d 512,
+    // vocabulary 100: 457 -> 150 / 178 -> 103 us; 9065, 220, 451: 238 -> 88 / 104 -> 68)
+    l.dw_parts = 1;
+    if (bwd && 2 * (int64_t)ceil_div(l.piece, 256) * ceil_div(d, l.tn_dw) <= kPgPairs) {
+        int64_t n = ((int64_t)64 << 20) / ((int64_t)l.piece * d * 4);
+        if (n > tokens / 512) n = tokens / 512;
+        if (n > kPgPairs) n = kPgPairs;
+        if (n > 1) l.dw_parts = (int)n;
+    }
     size_t at = kHead;
     auto take = [&](size_t bytes) { const size_t o = at; at += up(bytes); return o; };
     const size_t t = (size_t)tokens;
@@ -1093,6 +1128,8 @@ Layout layout(int64_t tokens, int d, int vocab, int dtype, bool bwd)
     if (bwd) {
         l.g = take((size_t)l.trows * l.piece * 2 * l.gplanes);
         l.dx = take(t * d * 4 * l.dx_parts);
+        l.dw_splits = take(4);
+        l.dw = l.dw_parts > 1 ? take((size_t)l.piece * d * 4 * l.dw_parts) : 0;
     } else {
         l.part = take((size_t)l.chunk * l.halves * sizeof(float2));
     }
@@ -1303,7 +1340,8 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
 
     CUtensorMap x_k, x_n, w_k, w_n, g_m, g_k, g_to, dw_to, dx_to, x_h;
     if (d % 4 == 0) {
-        MONARCH_TRY(tile_target(&dw_to, dW, vocab, d, (int64_t)vocab * d, 1));
+        if (l.dw_parts > 1) MONARCH_TRY(tile_target(&dw_to, base + l.dw, l.piece, d, (int64_t)l.piece * d, l.dw_parts));
+        else MONARCH_TRY(tile_target(&dw_to, dW, vocab, d, (int64_t)vocab * d, 1));
         MONARCH_TRY(tile_target(&dx_to, acc, tokens, d, tokens * d, l.dx_parts));
     } else {
         MONARCH_TRY(plane_map(&dw_to, xp, 0, tokens, l.dp, l.dp, tokens * l.dp, l.planes));                    // not used
@@ -1339,9 +1377,23 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
         p.count = count; p.count_is_k = 1; p.rows = cols; p.cols = d; p.kdim = (int)tokens; p.tn = l.tn_dw;
         p.n_fastest = 1;
         p.seg = pg_seg(DW);
-        const EpiStoreF32::Args ew = {dW + (size_t)v0 * d, cols, d, accumulate, d % 4 == 0 ? v0 : -1, HALF ? largest : nullptr};
         p.half = HALF;
+        float *to = dW + (size_t)v0 * d, *parts = (float *)(base + l.dw);
+        int *dw_splits = (int *)(base + l.dw_splits);
+        const size_t part = (size_t)l.piece * d;
+        const bool tma = d % 4 == 0;
+        EpiStoreF32::Args ew = {to, cols, d, accumulate, tma ? v0 : -1, HALF ? largest : nullptr, 0};
+        if (l.dw_parts > 1) {
+            p.splits = l.dw_parts;
+            p.splits_out = dw_splits;
+            ew.out = parts; ew.add = 0; ew.y0 = tma ? 0 : -1; ew.part = part;
+        }
         MONARCH_TRY((launch_plane_gemm<1, 1, DW, true, EpiStoreF32>(g_m, x_h, dw_to, p, ew, s)));
+        if (l.dw_parts > 1) {
+            const long long n = (long long)cols * d, want = (n / (tma ? 4 : 1) + 255) / 256;
+            MONARCH_TRY(launch_serialized(tma ? xent_dw_kernel<4> : xent_dw_kernel<1>, dim3((unsigned)(want < 148 * 8 ? want : 148 * 8)), 256, 0, s, (const float *)parts, part,
+                                          (const int *)dw_splits, to, n, accumulate));
+        }
         // dx += g W
         p = gemm(status);
         p.count = count; p.rows = (int)tokens; p.cols = d; p.kdim = cols; p.tn = l.tn_dx;

@@ -268,6 +268,28 @@ def test_gradient_of_few_tokens(T, d, V, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d,V,ignored", [(4704, 491, 65, 0.0), (1024, 64, 10, 0.0), (1023, 64, 10, 0.0), (3000, 300, 700, 0.9), (2500, 136, 1, 0.0), (5000, 33, 257, 1.1)])
+def test_gradient_of_a_small_vocabulary(T, d, V, ignored, dtype):
+    """dW in parts of the tokens (1024 of them and more): few tiles, most or all tokens left out, added to what is there."""
+    x, W, y, dloss = make(T, d, V, dtype, ignored, seed=T + V)
+    before = torch.randn(V, d, device="cuda")
+    if ignored > 1.0:
+        dx, dW = backward(x, W, y, torch.zeros(T, device="cuda"), dloss)
+        assert (dx == 0).all() and (dW == 0).all()
+        _, dW = backward(x, W, y, torch.zeros(T, device="cuda"), dloss, dW0=before)
+        assert torch.equal(dW, before)
+        return
+    e = exact(x, W, y, dloss)
+    dx, dW = backward(x, W, y, e["lse"].float(), dloss)
+    within(dx, e["dx"], e["dx_err"], "dx")
+    within(dW, e["dW"], e["dW_err"], "dW")
+    _, again = backward(x, W, y, e["lse"].float(), dloss)
+    assert torch.equal(dW, again)
+    _, dW = backward(x, W, y, e["lse"].float(), dloss, dW0=before)
+    within(dW, e["dW"] + before.double(), e["dW_err"] + (before.double().abs() + e["dW"].abs()) * 2.0 ** -23, "dW")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_accumulate_adds(dtype):
     T, d, V = 150, 80, 900
     x, W, y, dloss = make(T, d, V, dtype, 0.0, seed=5)
