@@ -726,7 +726,7 @@ __global__ void __launch_bounds__(few_threads(PL, NT), 1) xent_few_kernel(const 
     float *sums = reinterpret_cast<float *>(xs + PL * xplane) + team * 2 * kFewTeam * NT * 128;      // [2][team][NT][4][32 lanes]
     int turn = 0;
     for (int grp = 0; grp < groups; ++grp, ++turn) {
-        float z[NT][4] = {}, sum[NT][4] = {};
+        float z[NT][4] = {}, low[NT][4] = {}, sum[NT][4] = {};          // low: the products of other than the first planes (fp32)
         for (int step = 0; step < steps; ++step) {
 #pragma unroll
             for (int u = 0; u < kStep; ++u) {
@@ -746,13 +746,14 @@ __global__ void __launch_bounds__(few_threads(PL, NT), 1) xent_few_kernel(const 
 #pragma unroll
                         for (int q = o; q >= 0; --q) {
                             const uint32_t f0[4] = {a0[q][0], a1[q][0], a0[q][1], a1[q][1]}, f1[4] = {a0[q][2], a1[q][2], a0[q][3], a1[q][3]};
-                            mma(z[n], f0, b[o - q].x, b[o - q].y);
-                            mma(z[n], f1, b[o - q].z, b[o - q].w);
+                            float(&to)[4] = o > 0 ? low[n] : z[n];
+                            mma(to, f0, b[o - q].x, b[o - q].y);
+                            mma(to, f1, b[o - q].z, b[o - q].w);
                         }
                 }
             }
             fetch(step + 1 < steps ? grp : grp + 1, step + 1 < steps ? step + 1 : 0);
-            if (step % 8 == 7)                                                    // runs of at most 96 steps (plane_gemm.cuh)
+            if (step % 4 == 3)                                                    // runs of at most 32 products (plane_gemm.cuh)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -762,7 +763,7 @@ __global__ void __launch_bounds__(few_threads(PL, NT), 1) xent_few_kernel(const 
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) mine[((member * NT + n) * 4 + e) * 32 + lane] = sum[n][e] + z[n][e];
+            for (int e = 0; e < 4; ++e) mine[((member * NT + n) * 4 + e) * 32 + lane] = sum[n][e] + z[n][e] + low[n][e];
         asm volatile("bar.sync %0, 256;" ::"r"(team + 1) : "memory");
         // this buffer is written again two groups on, behind the next barrier, which its reader reaches when it has read
         if (turn % kFewTeam != member) continue;
