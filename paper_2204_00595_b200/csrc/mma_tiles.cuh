@@ -76,7 +76,8 @@ int launch_serialized(void (*kern)(Ts...), dim3 grid, int threads, int smem, cud
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (smem > 48 * 1024) MONARCH_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    // without it 48 KB at most, the kernel's static arrays (up to 8 KB) among them
+    if (smem > 40 * 1024) MONARCH_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     MONARCH_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, args...));
     note_launch();
     return MONARCH_OK;
