@@ -15,7 +15,8 @@
 // are near 1.  Tokens are what dW sums over, so each may have a power of two of its own: x' = x 2^-a[t] with the row's largest value
 // in [1, 2), g' = g 2^(a[t] - E + 13), E the same for all, so that every |g'| is below 2^14 where exp(z - lse) <= 1; dW = 2^(E - 13) sum g' x'.
 // What fp16 cannot hold of them is 2^-25 of the row's largest x and 2^-39 of the largest g.  Up to kFewTokens tokens take three bf16
-// planes, which cost nothing there: the time goes into reading W and writing dW.
+// planes: the time goes into reading W and writing dW (64 tokens of d 1024, vocabulary 50257: nothing more; 128: 160 -> 182 us, and dx,
+// of so few tokens up to 2.5e-3 off with one plane, is as exact as its type, 1.7e-3).
 #include <cuda_fp16.h>
 
 #include "plane_gemm.cuh"
@@ -25,7 +26,7 @@ namespace tc {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kFewTokens = 64, kBias = 1024;
+constexpr int kFewTokens = 128, kBias = 1024;
 constexpr int kTokenChunk = 32768;              // tokens whose partial sums are in memory at a time (forward)
 
 __device__ __forceinline__ float ex2(float x)
@@ -1170,10 +1171,13 @@ PlaneGemm gemm(unsigned *status)
     return g;
 }
 
-// Logits.  An error of z is a relative error of g, so their sums in tensor memory end after 64 (bf16) or 24 (fp32) steps (pg_seg), for
-// few tokens, where time is not the matter, after 16, and up to 512 tokens after 32 (100 tokens: dW 1.01e-6 -> 5.8e-7 off; of 1000 on
-// dW's own sums weigh as much, 1.07e-6 -> 1.01e-6, and 4096 tokens would take 4 % longer).  The loss takes less harm: 96 (bf16, 64 steps:
-// 3.4e-7 of lse; 241 steps: 2e-6).
+// Sums in tensor memory.  An error of z is a relative error of g, so the logits' sums end there after 64 (bf16) or 24 (fp32) steps
+// (pg_seg).  Of few tokens or a small vocabulary, where time is not the matter, they end after 16 and those of dW after 32: 3857 tokens,
+// d 824, vocabulary 220: dW 2.2e-6 -> below 1e-6 off.  Up to 512 tokens the logits' end after 32 (100 tokens: 1.01e-6 -> 5.8e-7; of 1000 on
+// dW's own sums weigh as much, and 4096 tokens would take 4 % longer).  The loss takes less harm: 96 (64 steps: 3.4e-7 of lse; 241: 2e-6).
+constexpr int kSmallVocab = 16384;
+bool short_runs(int64_t tokens, int vocab) { return tokens <= kFewTokens || vocab <= kSmallVocab; }
+
 template <int SCHEME, class Epi>
 int logits(const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mc, PlaneGemm p, const typename Epi::Args &e, int seg, bool exact, cudaStream_t s)
 {
@@ -1372,12 +1376,12 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
         p.count = count; p.rows = (int)tokens; p.cols = cols; p.kdim = d; p.tn = l.tn;
         p.b_n0 = l.direct ? v0 : 0;
         const typename EpiGrad<GP, HALF>::Args eg = {cols, v0, tgt, count, clse, cdl, exponent, largest};
-        MONARCH_TRY((logits<LOGITS, EpiGrad<GP, HALF>>(x_k, w_k, g_to, p, eg, tokens <= kFewTokens ? 4 : tokens <= 512 ? 8 : 16, true, s)));
+        MONARCH_TRY((logits<LOGITS, EpiGrad<GP, HALF>>(x_k, w_k, g_to, p, eg, short_runs(tokens, vocab) ? 4 : tokens <= 512 ? 8 : 16, true, s)));
         // dW = g^T x
         p = gemm(status);
         p.count = count; p.count_is_k = 1; p.rows = cols; p.cols = d; p.kdim = (int)tokens; p.tn = l.tn_dw;
         p.n_fastest = 1;
-        p.seg = pg_seg(DW);
+        p.seg = short_runs(tokens, vocab) && pg_seg(DW) > 4 ? 4 : pg_seg(DW);
         p.half = HALF;
         float *to = dW + (size_t)v0 * d, *parts = (float *)(base + l.dw);
         int *dw_splits = (int *)(base + l.dw_splits);
