@@ -263,9 +263,11 @@ template <int KP, int NP, int PL> struct BlockCfg {
 };
 
 // acc[t] += A B for T column tiles of 8.  A: planes at `a` (row-major, 16 rows of this warp), B: planes at `b`, TRANS: stored [k][n].
-// An MMA adds without rounding to nearest, so what a sum loses goes by the number of its products; APART: those of the first planes have a
-// sum of their own, which takes a sixth of them (fp32; bf16: a third), and the small ones are added to it at the end.
-template <int PL, int KSTEPS, int T, bool TRANS, bool APART = false>
+// An MMA adds without rounding to nearest, so what a sum loses goes by the number of its products when it is large.  kApart: those of the
+// first planes have a sum of their own, which takes a sixth of them (fp32; bf16: a third), and the small ones are added to it at the end;
+// kTwice (no registers for that): all the small ones come first, then K once more for the first planes.
+enum Sums { kOne, kApart, kTwice };
+template <int PL, int KSTEPS, int T, bool TRANS, Sums SUMS = kOne>
 __device__ __forceinline__ void plane_mma(float (&acc)[T][4], uint32_t a, uint32_t aplane, int lda, uint32_t b, uint32_t bplane, int ldb)
 {
     const int lane = threadIdx.x & 31, mtx = lane >> 3, r = lane & 7;
@@ -275,24 +277,26 @@ __device__ __forceinline__ void plane_mma(float (&acc)[T][4], uint32_t a, uint32
     // alone, twice: what would be the other one's rows may lie behind the planes
     const uint32_t b_at = TRANS ? b + ((mtx & 1) * 8 + r) * ldb * 2 : b + r * ldb * 2 + (mtx & 1) * 16;
     const uint32_t second = TRANS ? (mtx >> 1) * 16 : (mtx >> 1) * 8 * ldb * 2;
+    constexpr bool APART = SUMS == kApart;
     float low[APART ? T : 1][4] = {};
 #pragma unroll
-    for (int k = 0; k < KSTEPS; ++k) {
+    for (int i = 0; i < (SUMS == kTwice ? 2 : 1) * KSTEPS; ++i) {
+        const int k = i % KSTEPS, first = SUMS == kTwice && i < KSTEPS ? 1 : 0, last = SUMS == kTwice && i >= KSTEPS ? 0 : PL - 1;      // of these orders
         uint32_t fa[PL][4];
 #pragma unroll
-        for (int q = 0; q < PL; ++q) ldm4(fa[q], a_at + q * aplane + k * 32);
+        for (int q = 0; q <= last; ++q) ldm4(fa[q], a_at + q * aplane + k * 32);
 #pragma unroll
         for (int t = 0; t < T; t += 2) {
             const uint32_t at = b_at + (t + 1 < T ? second : 0);
             uint32_t fb[PL][4];
 #pragma unroll
-            for (int q = 0; q < PL; ++q) {
+            for (int q = 0; q <= last; ++q) {
                 if constexpr (TRANS) ldm4t(fb[q], at + q * bplane + k * 16 * ldb * 2 + t * 16);
                 else ldm4(fb[q], at + q * bplane + t * 8 * ldb * 2 + k * 32);
             }
             // the small products first
 #pragma unroll
-            for (int o = PL - 1; o >= 0; --o)
+            for (int o = last; o >= first; --o)
 #pragma unroll
                 for (int q = o; q >= 0; --q) {
                     float (*to)[4] = APART && o > 0 ? low : acc;
@@ -384,10 +388,10 @@ __global__ void __launch_bounds__(BlockCfg<KP, NP, PL>::kThreads) ortho_block_ke
         __syncthreads();
         const uint32_t X = smem_u32(Xs) + (C::kXBufs > 1 ? it & 1 : 0) * (PL * C::kXPlane * 2);
         float s[C::kS][4] = {}, p[C::kS][4] = {};
-        plane_mma<PL, NP / 16, C::kS, false, true>(s, X + row0 * C::kLdX * 2, C::kXPlane * 2, C::kLdX, X + half * (KP / 2) * C::kLdX * 2, C::kXPlane * 2, C::kLdX);
+        plane_mma<PL, NP / 16, C::kS, false, kApart>(s, X + row0 * C::kLdX * 2, C::kXPlane * 2, C::kLdX, X + half * (KP / 2) * C::kLdX * 2, C::kXPlane * 2, C::kLdX);
         put_tiles<PL>(s, Ss + s_at, C::kSPlane, C::kLdS);
         __syncthreads();
-        plane_mma<PL, KP / 16, C::kS, false, true>(p, s_a, C::kSPlane * 2, C::kLdS, s_b, C::kSPlane * 2, C::kLdS);
+        plane_mma<PL, KP / 16, C::kS, false, kApart>(p, s_a, C::kSPlane * 2, C::kLdS, s_b, C::kSPlane * 2, C::kLdS);
 #pragma unroll
         for (int t = 0; t < C::kS; ++t)
 #pragma unroll
@@ -395,7 +399,7 @@ __global__ void __launch_bounds__(BlockCfg<KP, NP, PL>::kThreads) ortho_block_ke
         put_tiles<PL>(p, Ps + s_at, C::kSPlane, C::kLdS);
         __syncthreads();
         float y[C::kX][4] = {};
-        plane_mma<PL, KP / 16, C::kX, true>(y, p_a, C::kSPlane * 2, C::kLdS, X + half * NP, C::kXPlane * 2, C::kLdX);
+        plane_mma<PL, KP / 16, C::kX, true, (KP > 32 && PL > 2 ? kTwice : kOne)>(y, p_a, C::kSPlane * 2, C::kLdS, X + half * NP, C::kXPlane * 2, C::kLdX);
 #pragma unroll
         for (int t = 0; t < C::kX; ++t)
 #pragma unroll
