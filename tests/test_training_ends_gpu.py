@@ -371,6 +371,34 @@ def test_large_and_masked_logits():
     assert torch.isfinite(loss[rest]).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1, 5, 12])
+def test_masked_logits_of_few_tokens(T, dtype):
+    """Entries masked by the lowest value of the type have no part in the loss nor in dx, and dW = 0; a token that is not a number keeps to itself."""
+    d, V = 64, 500
+    x, W, y, dloss = make(T, d, V, dtype, 0.0, seed=17 + T)
+    y = y.clamp(min=200)
+    x[:, 0] = 1.0
+    W[:, 0] = 0.0
+    live = exact(x, W[200:].contiguous(), y - 200, dloss)
+    W[:200, 0] = torch.finfo(W.dtype).min
+    loss, lse = forward(x, W, y)
+    within(loss, live["loss"], live["loss_err"], "loss")
+    within(lse, live["lse"], live["lse_err"], "lse")
+    dx, dW = backward(x, W, y, live["lse"].float(), dloss)
+    within(dx[:, 1:], live["dx"][:, 1:], live["dx_err"][:, 1:], "dx")
+    assert (dW[:200] == 0).all()
+    within(dW[200:], live["dW"], live["dW_err"], "dW")
+    x[0, 3] = float("nan")
+    loss, lse = forward(x, W, y)
+    assert torch.isnan(loss[0]) and torch.isnan(lse[0])
+    if T > 1:
+        within(loss[1:], live["loss"][1:], live["loss_err"][1:], "loss of the others")
+        dx, _ = backward(x, W, y, live["lse"].float(), dloss)
+        assert torch.isnan(dx[0]).all()
+        within(dx[1:, 1:], live["dx"][1:, 1:], live["dx_err"][1:, 1:], "dx of the others")
+
+
 def test_shifted_labels_in_place_and_other_stream():
     """targets[1:] (8 bytes off a 16-byte boundary) and per-token outputs at odd offsets; a stream that is not the current one."""
     T, d, V = 90, 64, 500
