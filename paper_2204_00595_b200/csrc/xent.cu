@@ -588,16 +588,18 @@ int few_tiles(int tokens) { return tokens <= 8 ? 1 : 2; }                       
 size_t few_x(int tokens, int d, int planes) { return (size_t)tokens * few_row(d) * 2 * planes; }
 size_t few_smem(int tokens, int d, int planes) { return few_x(tokens, d, planes) + (size_t)few_teams(planes, few_tiles(tokens)) * 2 * kFewTeam * few_tiles(tokens) * 512; }
 // launches of few tokens that the call takes; 0: tiles.  fp32, d 1024 / 4096 (launches of 16 / 8 tokens), vocabularies of 50257 / 32768:
-// a launch 68 / 136 us forward and 184 / 365 backward, the tile kernels 245 / 826 and 455 / 950
+// a launch 68 / 136 us forward and 184 / 365 backward, the tile kernels 218 / 590 and 455 / 950.  Rows of other than 16-byte multiples are
+// read value by value, up to 16 tokens (us, on tiles in brackets; 5 tokens, d 1018, 50257: bf16 48 (109) and 188 (322), fp32 69 (273)
+// and 157 (554); 3 tokens, d 3661, 57446, fp32: 238 (1410) and 588 (2058))
 int few_launches(int64_t tokens, int d, int dtype, bool bwd)
 {
-    const bool f32 = dtype == MONARCH_F32;
-    if (d % 8 != 0 || tokens > (f32 ? 3 : 1) * kFewMost) return 0;
+    const bool f32 = dtype == MONARCH_F32, again = f32 && d % 8 == 0;
+    if (tokens > (again ? 3 : 1) * kFewMost) return 0;
     int most = kFewMost;                                                        // 227 KB of shared memory, 4 of them static
     while (most > 0 && few_smem(most, d, f32 ? 3 : 1) > 223 * 1024) --most;
     if (most == 0) return 0;
     const bool all = most == kFewMost;
-    const int n = ((int)tokens + most - 1) / most, limit = !f32 ? 1 : bwd ? (all ? 2 : 1) : (all ? 3 : 6);
+    const int n = ((int)tokens + most - 1) / most, limit = !f32 ? 1 : bwd || !again ? 2 : all ? 3 : 6;
     return n <= limit ? n : 0;
 }
 
@@ -625,6 +627,14 @@ template <typename T> struct FewRaw;
 template <> struct FewRaw<__nv_bfloat16> {
     uint4 v;
     __device__ __forceinline__ void load(const __nv_bfloat16 *p, bool in) { v = in ? __ldcs(reinterpret_cast<const uint4 *>(p)) : make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void load_some(const __nv_bfloat16 *p, int n)                       // the first n of them, at any address
+    {
+        const uint16_t *q = reinterpret_cast<const uint16_t *>(p);
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = (2 * i < n ? (uint32_t)__ldg(q + 2 * i) : 0u) | (2 * i + 1 < n ? (uint32_t)__ldg(q + 2 * i + 1) << 16 : 0u);
+        v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
     __device__ __forceinline__ void planes(uint32_t (&o)[1][4]) const { o[0][0] = v.x; o[0][1] = v.y; o[0][2] = v.z; o[0][3] = v.w; }
 };
 template <> struct FewRaw<float> {
@@ -636,6 +646,14 @@ template <> struct FewRaw<float> {
             a = __ldcs(reinterpret_cast<const float4 *>(p));
             b = __ldcs(reinterpret_cast<const float4 *>(p + 4));
         }
+    }
+    __device__ __forceinline__ void load_some(const float *p, int n)
+    {
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = i < n ? __ldg(p + i) : 0.0f;
+        a = make_float4(f[0], f[1], f[2], f[3]);
+        b = make_float4(f[4], f[5], f[6], f[7]);
     }
     __device__ __forceinline__ void planes(uint32_t (&o)[3][4]) const
     {
@@ -654,7 +672,8 @@ template <> struct FewRaw<float> {
     }
 };
 
-template <typename T, int PL, int NT, bool BWD>
+// ODD: rows of W are not 16-byte multiples
+template <typename T, int PL, int NT, bool BWD, bool ODD>
 __global__ void __launch_bounds__(few_threads(PL, NT), 1) xent_few_kernel(const FewArgs p)
 {
     constexpr int kFewThreads = few_threads(PL, NT), kFewTeams = few_teams(PL, NT);
@@ -680,8 +699,13 @@ __global__ void __launch_bounds__(few_threads(PL, NT), 1) xent_few_kernel(const 
         for (int u = 0; u < kStep; ++u) {
             const int k = k0 + step * kStep + u, at = k * 32 + c * 8;
             const bool in = k < k1 && at < p.d;
-            raw[u][0].load(w + at, in && r < row1);
-            raw[u][1].load(w + (size_t)8 * p.d + at, in && r + 8 < row1);
+            if constexpr (ODD) {
+                raw[u][0].load_some(w + at, in && r < row1 ? p.d - at : 0);
+                raw[u][1].load_some(w + (size_t)8 * p.d + at, in && r + 8 < row1 ? p.d - at : 0);
+            } else {
+                raw[u][0].load(w + at, in && r < row1);
+                raw[u][1].load(w + (size_t)8 * p.d + at, in && r + 8 < row1);
+            }
         }
     };
     depend_wait();
@@ -876,6 +900,12 @@ template <int C> struct FewCols<__nv_bfloat16, C> {
             v[0] = in ? __ldcs(reinterpret_cast<const uint32_t *>(p)) : 0u;
         }
     }
+    __device__ __forceinline__ void load_apart(const __nv_bfloat16 *p, int n)          // value i at p + 32 i, where that is below n
+    {
+        const uint16_t *q = reinterpret_cast<const uint16_t *>(p);
+#pragma unroll
+        for (int i = 0; i < C; i += 2) v[i / 2] = (32 * i < n ? (uint32_t)__ldg(q + 32 * i) : 0u) | (32 * (i + 1) < n ? (uint32_t)__ldg(q + 32 * (i + 1)) << 16 : 0u);
+    }
     __device__ __forceinline__ float at(int i) const { return __uint_as_float(i & 1 ? v[i / 2] & 0xffff0000u : v[i / 2] << 16); }
 };
 template <int C> struct FewCols<float, C> {
@@ -889,17 +919,24 @@ template <int C> struct FewCols<float, C> {
             v[0] = in ? __ldcs(reinterpret_cast<const float2 *>(p)) : make_float2(0.0f, 0.0f);
         }
     }
+    __device__ __forceinline__ void load_apart(const float *p, int n)
+    {
+#pragma unroll
+        for (int i = 0; i < C; i += 2) v[i / 2] = make_float2(32 * i < n ? __ldg(p + 32 * i) : 0.0f, 32 * (i + 1) < n ? __ldg(p + 32 * (i + 1)) : 0.0f);
+    }
     __device__ __forceinline__ float at(int i) const { return i & 1 ? v[i / 2].y : v[i / 2].x; }
 };
 
-template <typename T, int TP>
+// ODD: rows are not 16-byte multiples; a lane's columns are 32 apart, its loads and stores single values
+template <typename T, int TP, bool ODD>
 __global__ void __launch_bounds__(256, 2) xent_few_grad_kernel(const FewGradArgs p)
 {
     constexpr int R = kFewRows<T>, C = 32 / TP, G = R * TP / 32;               // columns of a lane, values of g it fetches
     __shared__ __align__(16) float s_g[8][R][TP];
     __shared__ float s_dx[TP][32 * C];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = blockIdx.x * 32 * C + lane * C;
-    const bool live = col < p.d;                                               // d % 8 == 0
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, apart = ODD ? 32 : 1, at0 = ODD ? lane : lane * C;
+    const int col = blockIdx.x * 32 * C + at0;                                 // this lane's first column, the others `apart`
+    const bool live = col < p.d;                                               // not ODD: d % 8 == 0
     const int row0 = blockIdx.y * p.rows, row1 = min(row0 + p.rows, p.vocab);
     depend_wait();
     depend_launch();
@@ -919,7 +956,11 @@ __global__ void __launch_bounds__(256, 2) xent_few_grad_kernel(const FewGradArgs
             g[0] = v.x; g[1] = v.y;
         }
     };
-    auto fetch_w = [&](int r, int u) { w[u].load((const T *)p.W + (size_t)(r + u) * p.d + col, live && r + u < row1); };
+    auto fetch = [&](FewCols<T, C> &v, const T *row, bool in) {
+        if constexpr (ODD) v.load_apart(row + col, in ? p.d - col : 0);
+        else v.load(row + col, in && live);
+    };
+    auto fetch_w = [&](int r, int u) { fetch(w[u], (const T *)p.W + (size_t)(r + u) * p.d, r + u < row1); };
     int r = row0 + warp * R;
 #pragma unroll
     for (int u = 0; u < R; ++u) fetch_w(r, u);
@@ -930,7 +971,7 @@ __global__ void __launch_bounds__(256, 2) xent_few_grad_kernel(const FewGradArgs
         FewCols<T, C> v[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k)
-            v[k].load((const T *)p.x + (size_t)(t + k) * p.d + col, live && t + k < p.tokens && p.targets[t + k < p.tokens ? t + k : 0] != p.ignore);
+            fetch(v[k], (const T *)p.x + (size_t)(t + k) * p.d, t + k < p.tokens && p.targets[t + k < p.tokens ? t + k : 0] != p.ignore);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             x[t / 2][c] = pack2(v[0].at(c), v[1].at(c));
@@ -972,7 +1013,14 @@ __global__ void __launch_bounds__(256, 2) xent_few_grad_kernel(const FewGradArgs
                     const float2 h = unpack2(o[c]);
                     f[c] = h.x + h.y;
                 }
-                if (p.accumulate) {                                            // one addition of one thread to each value; nothing waits for it
+                if constexpr (ODD) {
+#pragma unroll
+                    for (int c = 0; c < C; ++c)
+                        if (col + 32 * c < p.d) {
+                            if (p.accumulate) atomicAdd(to + 32 * c, f[c]);
+                            else __stcs(to + 32 * c, f[c]);
+                        }
+                } else if (p.accumulate) {                                     // one addition of one thread to each value; nothing waits for it
                     if constexpr (C == 4)
                         asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(to), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]) : "memory");
                     else
@@ -992,7 +1040,7 @@ __global__ void __launch_bounds__(256, 2) xent_few_grad_kernel(const FewGradArgs
 #pragma unroll
                 for (int c = 0; c < C; ++c) {
                     float2 v = unpack2(dx[t / 2][c]);
-                    float *to = &s_dx[t][lane * C + c];
+                    float *to = &s_dx[t][at0 + apart * c];
                     if (q > 0) { v.x += to[0]; v.y += to[32 * C]; }
                     to[0] = v.x;
                     to[32 * C] = v.y;
@@ -1207,7 +1255,7 @@ constexpr int kFewCtas = 148;
 
 template <typename T, int PL, int NT, bool BWD> int few_launch(const FewArgs &a, cudaStream_t s)
 {
-    return launch_serialized(xent_few_kernel<T, PL, NT, BWD>, dim3(kFewCtas), few_threads(PL, NT), (int)few_smem(a.tokens, a.d, PL), s, a);
+    return launch_serialized(a.d % 8 == 0 ? xent_few_kernel<T, PL, NT, BWD, false> : xent_few_kernel<T, PL, NT, BWD, true>, dim3(kFewCtas), few_threads(PL, NT), (int)few_smem(a.tokens, a.d, PL), s, a);
 }
 template <typename T, int PL, bool BWD> int few_any(const FewArgs &a, cudaStream_t s)
 {
@@ -1247,7 +1295,7 @@ template <typename T, int TP> int few_grad_launch(FewGradArgs a, T *dx, cudaStre
     const int parts = few_parts(a.d, a.vocab, TP / 8);
     a.rows = ceil_div(a.vocab, parts);
     const int used = ceil_div(a.vocab, a.rows);
-    MONARCH_TRY(launch_serialized(xent_few_grad_kernel<T, TP>, dim3(ceil_div(a.d, 1024 / TP), used), 256, 0, s, a));
+    MONARCH_TRY(launch_serialized(a.d % 8 == 0 ? xent_few_grad_kernel<T, TP, false> : xent_few_grad_kernel<T, TP, true>, dim3(ceil_div(a.d, 1024 / TP), used), 256, 0, s, a));
     return launch_serialized(xent_few_dx_kernel<T>, dim3(ceil_div(a.d, 32), a.tokens), 256, 0, s, a.part, a.targets, a.ignore, dx, a.tokens, a.d, used);
 }
 

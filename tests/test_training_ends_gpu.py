@@ -224,11 +224,15 @@ def test_every_token_ignored_and_no_tokens():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("T,d,V", [(1, 8, 1), (1, 520, 70), (3, 136, 4097), (8, 1024, 3001), (9, 1032, 600), (13, 40, 20000), (16, 64, 63), (16, 2048, 900)])
+@pytest.mark.parametrize("T,d,V", [(1, 8, 1), (1, 520, 70), (3, 136, 4097), (8, 1024, 3001), (9, 1032, 600), (13, 40, 20000), (16, 64, 63), (16, 2048, 900),
+                                   (1, 1, 1), (1, 313, 3001), (2, 7, 40), (5, 1018, 700), (8, 129, 9), (8, 33, 2000), (9, 65, 1000), (16, 1001, 300), (12, 4, 77)])
 def test_gradient_of_few_tokens(T, d, V, dtype):
     """Up to 16 tokens: masked rows that are not numbers, targets out of range, added to what is there, the same bits again and replayed."""
     x, W, y, dloss = make(T, d, V, dtype, 0.3, seed=T * d)
     e = exact(x, W, y, dloss)
+    got, lse = forward(x, W, y)
+    within(got, e["loss"], e["loss_err"], "loss")
+    within(lse, e["lse"], e["lse_err"], "lse")
     lse = e["lse"].float()
     out = y == IGNORE
     x[out] = float("nan")
