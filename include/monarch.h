@@ -283,8 +283,10 @@ size_t monarch_xent_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab, in
  * lse, dloss: float32 [tokens].  Tokens left out (ignore_index) have dx = 0 and no part in dW;
  * a target out of range makes the gradients that it enters NaN.  g is held to 2^-24 in dW for
  * float32 and up to 128 tokens, else to 2^-22 (fp16 parts, scaled per token by the largest value
- * of x[t] and by dloss[t]: exp(z - lse) has to stay below 4, as it does with the lse of the same
- * x and W), and of more than 128 tokens to bf16 in a bf16 dx.  The order of all sums is fixed.
+ * of x[t] and by dloss[t], at any size of these: exp(z - lse) has to stay below 4, as it does with
+ * the lse of the same x and W), and of more than 128 tokens to bf16 in a bf16 dx.  Those parts leave
+ * out what is below 2^-25 of the largest value of a row of x, and of a token's share in dW what is
+ * below 2^-39 of the largest |dloss[t]| max |x[t]| of the call.  The order of all sums is fixed.
  * Workspace: monarch_xent_bwd_workspace_bytes (0 for invalid arguments). */
 int monarch_xent_bwd(const void *x, const void *W, const int64_t *targets, const float *lse,
                      const float *dloss, void *dx, float *dW, int accumulate,

@@ -13,8 +13,9 @@
 // rounding), of up to kFewTokens tokens two.  dW is a float32 result: two bf16 planes leave 2^-16 of a term (2.7e-6 of dW's norm at
 // 2900 tokens), a third costs a quarter of the call's time.  Two FP16 parts leave 2^-22, and x, bf16, fits fp16 once its exponents
 // are near 1.  Tokens are what dW sums over, so each may have a power of two of its own: x' = x 2^-a[t] with the row's largest value
-// in [1, 2), g' = g 2^(a[t] - E + 13), E the same for all, so that every |g'| is below 2^14 where exp(z - lse) <= 1; dW = 2^(E - 13) sum g' x'.
-// What fp16 cannot hold of them is 2^-25 of the row's largest x and 2^-39 of the largest g.  Up to kFewTokens tokens take three bf16
+// in [1, 2) (2^126 and more: [1, 4)), g' = g 2^(a[t] - E + 13), E the largest a[t] + exponent of dloss[t], so that every |g'| is below
+// 2^14 where exp(z - lse) <= 1; dW = 2^(E - 13) sum g' x'.  What fp16 cannot hold of them is 2^-25 of the row's largest x and 2^-39 of the
+// largest |dloss| times the largest x of its row.  Up to kFewTokens tokens take three bf16
 // planes: the time goes into reading W and writing dW (64 tokens of d 1024, vocabulary 50257: nothing more; 128: 160 -> 182 us, and dx,
 // of so few tokens up to 2.5e-3 off with one plane, is as exact as its type, 1.7e-3).
 #include <cuda_fp16.h>
@@ -108,8 +109,14 @@ __device__ __forceinline__ void copy_row(const T *__restrict__ src, __nv_bfloat1
     }
 }
 
-// exponent of a value by its bits; zeros, values below the normal range and infinities take the ends of the scale
-__device__ __forceinline__ int exponent_of(float v) { return min(max((int)(__float_as_uint(v) >> 23) - 127, -100), 100); }
+// exponent of |v| by its bits: -127 for zero and values below the normal range, 128 for infinities
+__device__ __forceinline__ int exponent_of(float v) { return (int)(__float_as_uint(v) >> 23) - 127; }
+// v 2^e in two steps, of which each is in the normal range where 2^e need not be
+__device__ __forceinline__ float scaled(float v, int e)
+{
+    const int e1 = max(-126, min(127, e / 2)), e2 = max(-126, min(127, e - e / 2));
+    return v * __uint_as_float((uint32_t)(127 + e1) << 23) * __uint_as_float((uint32_t)(127 + e2) << 23);
+}
 
 // x' of a row (one warp), its exponent, and its part in E
 __device__ __forceinline__ void scaled_row(const __nv_bfloat16 *__restrict__ src, __half *to, int d, int dp, float dl, int *exponent, int *largest, int lane)
@@ -128,7 +135,7 @@ __device__ __forceinline__ void scaled_row(const __nv_bfloat16 *__restrict__ src
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-    const int a = exponent_of(top);
+    const int a = max(-126, min(126, exponent_of(top)));       // 2^-a is in the normal range; x' of the largest rows is below 4
     const float down = __uint_as_float((uint32_t)(127 - a) << 23);
     if (d == dp) {
 #pragma unroll 4
@@ -313,7 +320,7 @@ template <int PL, bool HALF> struct EpiGrad {
         const float *lse, *dl;
         const int *exponent, *largest;
     };
-    float r_hi, r_lo, dl, up;
+    float r_hi, r_lo, dl, dlh;      // dlh: dl 2^(a[t] - E + 13)
     int y, e;
     bool live;
     __device__ __forceinline__ void begin(const Args &a, const PgTile &t)
@@ -331,9 +338,7 @@ template <int PL, bool HALF> struct EpiGrad {
         r_lo = fmaf(l, kLog2e, -r_hi);
         y -= a.v0 + t.col;
         if (HALF) {
-            // 2^(a[t] - E + 13); below the normal range of fp32 the whole row is below 2^-100 of the largest
-            const int x = e + kBias + 13;
-            up = x < -126 ? 0.0f : __uint_as_float((uint32_t)(127 + min(x, 127)) << 23);
+            dlh = scaled(dl, e + kBias + 13);
         }
     }
     __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<kStage> &st)
@@ -342,18 +347,18 @@ template <int PL, bool HALF> struct EpiGrad {
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
             const float e = ex2(fmaf(v[i], kLog2e, -r_hi) - r_lo);
-            v[i] = i >= left ? 0.0f : dl * (at == i ? e - 1.0f : e);
+            v[i] = i >= left ? 0.0f : (HALF ? 1.0f : dl) * (at == i ? e - 1.0f : e);
         }
         st.begin();
         if constexpr (HALF) {
             uint32_t w[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+            for (int i = 0; i < 16; ++i) w[i] = pack_bf16(dl * v[2 * i], dl * v[2 * i + 1]);
             st.row(0, w);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                v[2 * i] *= up;
-                v[2 * i + 1] *= up;
+                v[2 * i] *= dlh;
+                v[2 * i + 1] *= dlh;
                 const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
                 const float2 f = __half22float2(h);
                 v[2 * i] -= f.x;
@@ -405,11 +410,9 @@ struct EpiStoreF32 {
     __device__ __forceinline__ void start(const Args &, const PgTile &) {}
     __device__ __forceinline__ void chunk(const Args &a, const PgTile &t, int c, float (&v)[32], PgStage<kStage> &st)
     {
-        // times 2^(E - 13), in two steps: it need not be in the normal range itself (no weights at all: E is far below)
-        const int e1 = max(-126, min(127, e / 2)), e2 = max(-126, min(127, e - e / 2));
-        const float f1 = __uint_as_float((uint32_t)(127 + e1) << 23), f2 = __uint_as_float((uint32_t)(127 + e2) << 23);
+        // times 2^(E - 13); without any weights E is far below
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = v[i] * f1 * f2;
+        for (int i = 0; i < 32; ++i) v[i] = scaled(v[i], e);
         if (a.y0 >= 0) {
             if ((t.row & ~31) < a.rows && t.col + c < a.cols) st.tile(v, t.col + c, a.y0 + (t.row & ~31), t.z, a.add);
             return;
