@@ -264,7 +264,8 @@ int monarch_project(const void *A, void *L, void *R, int32_t n, int32_t m, int d
  * [0, vocab) that is not ignore_index gives loss = NaN for its token.  ignore_index may be
  * any value, one inside [0, vocab) included.  A row with a logit of +infinity or NaN gives
  * loss = lse = NaN, and so does, in float32, an infinity among the operands of any of its
- * logits (mask with the lowest finite value).  No reduction over tokens: a mean is dloss[t] = 1 / count below.
+ * logits (mask with the lowest finite value; a token with every word masked that way has finite
+ * loss, lse and gradients).  No reduction over tokens: a mean is dloss[t] = 1 / count below.
  * targets need 8-byte, loss, lse and dloss 4-byte alignment (so that shifted labels can be
  * passed in place); tokens and vocab up to 2^24, d up to 65536: beyond, MONARCH_ERR_UNSUPPORTED.
  * Sums over d, the maximum and the sum of exponentials are fp32 in both dtypes (float32

@@ -37,6 +37,10 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
+__device__ __forceinline__ float exp_of(float x) { return ex2(x * kLog2e); }
+// maximum and sum of exp(z - maximum) -> log of the sum of exponentials
+__device__ __forceinline__ float log_sum(float m, float s) { return fmaf(log2f(s), kLn2, m); }
+
 // ------------------------------------------------------------------------------------------------ preparation
 struct PrepArgs {
     const void *x;
@@ -254,8 +258,8 @@ __global__ void __launch_bounds__(256) split_rows_kernel(const T *__restrict__ W
 }
 
 // ------------------------------------------------------------------------------------------------ epilogues
-// Per row and half tile: r = log2(e) times the maximum, rounded, and s = sum 2^(z log2 e - r).  Exponents are formed by one FMA
-// from z and r, so the rounding of r cancels in r + log2 s.
+// Per row and half tile: the maximum m and s = sum exp(z - m).  The difference is taken first: it is exact where z is near m, off by
+// 2^-24 of itself where it weighs little, and z log2 e leaves fp32 from 2.36e38 on, where masks by the type's lowest value are.
 struct EpiStats {
     static constexpr int kStage = 0;
     struct Args {
@@ -287,12 +291,11 @@ struct EpiStats {
         float top[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
         for (int i = 4; i < 32; ++i) top[i & 3] = fmaxf(top[i & 3], v[i]);
-        const float cm = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * kLog2e;
-        const float nm = fmaxf(m, cm);
+        const float nm = fmaxf(fmaxf(m, fmaxf(top[0], top[1])), fmaxf(top[2], top[3]));
         const float base = nm == __int_as_float(0xff800000) ? 0.0f : nm;
-        float sum[4] = {s * ex2(m - base), 0.0f, 0.0f, 0.0f};
+        float sum[4] = {s * exp_of(m - base), 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < 32; ++i) sum[i & 3] += ex2(fmaf(v[i], kLog2e, -base));
+        for (int i = 0; i < 32; ++i) sum[i & 3] += exp_of(v[i] - base);
         s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
         m = nm;
         const int at = y - c;
@@ -320,22 +323,19 @@ template <int PL, bool HALF> struct EpiGrad {
         const float *lse, *dl;
         const int *exponent, *largest;
     };
-    float r_hi, r_lo, dl, dlh;      // dlh: dl 2^(a[t] - E + 13)
+    float l, dl, dlh;               // dlh: dl 2^(a[t] - E + 13)
     int y, e;
     bool live;
     __device__ __forceinline__ void begin(const Args &a, const PgTile &t)
     {
         live = t.row < *a.count;
-        r_hi = live ? a.lse[t.row] : 0.0f;
+        l = live ? a.lse[t.row] : 0.0f;
         dl = live ? a.dl[t.row] : 0.0f;
         y = live ? a.tgt[t.row] : -1;
         if (HALF) e = live ? a.exponent[t.row] - *a.largest : 0;
     }
     __device__ __forceinline__ void start(const Args &a, const PgTile &t)
     {
-        const float l = r_hi;
-        r_hi = l * kLog2e;
-        r_lo = fmaf(l, kLog2e, -r_hi);
         y -= a.v0 + t.col;
         if (HALF) {
             dlh = scaled(dl, e + kBias + 13);
@@ -346,7 +346,7 @@ template <int PL, bool HALF> struct EpiGrad {
         const int left = live ? a.cols - t.col - c : 0, at = y - c;
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-            const float e = ex2(fmaf(v[i], kLog2e, -r_hi) - r_lo);
+            const float e = exp_of(v[i] - l);
             v[i] = i >= left ? 0.0f : (HALF ? 1.0f : dl) * (at == i ? e - 1.0f : e);
         }
         st.begin();
@@ -560,11 +560,11 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const float2 *__restrict
         for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
         const float base = m == __int_as_float(0xff800000) ? 0.0f : m;
         float s = 0.0f;
-        for (int i = lane; i < halves; i += 32) s += q[i].y * ex2(q[i].x - base);
+        for (int i = lane; i < halves; i += 32) s += q[i].y * exp_of(q[i].x - base);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
         if (lane == 0) {
-            const float l = (base + log2f(s)) * kLn2;
+            const float l = log_sum(m, s);
             const int to = map[row];
             lse[to] = l;
             loss[to] = tgt[row] >= 0 ? l - tlogit[row] : __int_as_float(0x7fffffff);
@@ -621,7 +621,7 @@ struct FewArgs {
 __device__ __forceinline__ void join(float &m, float &s, float m2, float s2)
 {
     const float n = fmaxf(m, m2), base = n == __int_as_float(0xff800000) ? 0.0f : n;
-    s = s * ex2(m - base) + s2 * ex2(m2 - base);
+    s = s * exp_of(m - base) + s2 * exp_of(m2 - base);
     m = n;
 }
 
@@ -806,10 +806,10 @@ __global__ void __launch_bounds__(few_threads(PL, NT), 1) xent_few_kernel(const 
 #pragma unroll
             for (int e = 0; e < 2 && BWD; ++e) {
                 const int at = n * 8 + 2 * c + e;
-                const float l = s_lse[at], hi = l * kLog2e, lo = fmaf(l, kLog2e, -hi), dl = s_dl[at];
+                const float l = s_lse[at], dl = s_dl[at];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const float x = ex2(fmaf(t[e + 2 * h], kLog2e, -hi) - lo);
+                    const float x = exp_of(t[e + 2 * h] - l);
                     t[e + 2 * h] = tgt[n][e] == -2 ? 0.0f : dl * (tgt[n][e] == r0 + 8 * h ? x - 1.0f : x);
                 }
             }
@@ -825,8 +825,8 @@ __global__ void __launch_bounds__(few_threads(PL, NT), 1) xent_few_kernel(const 
                 if (r0 == tgt[n][e] && r0 < row1) p.tlogit[n * 8 + 2 * c + e] = z0;
                 if (r1 == tgt[n][e] && r1 < row1) p.tlogit[n * 8 + 2 * c + e] = z1;
                 const float v0 = r0 < row1 ? z0 : __int_as_float(0xff800000), v1 = r1 < row1 ? z1 : __int_as_float(0xff800000);
-                const float top = fmaxf(m[n][e], fmaxf(v0, v1) * kLog2e), base = top == __int_as_float(0xff800000) ? 0.0f : top;
-                s[n][e] = s[n][e] * ex2(m[n][e] - base) + ex2(fmaf(v0, kLog2e, -base)) + ex2(fmaf(v1, kLog2e, -base));
+                const float top = fmaxf(m[n][e], fmaxf(v0, v1)), base = top == __int_as_float(0xff800000) ? 0.0f : top;
+                s[n][e] = s[n][e] * exp_of(m[n][e] - base) + exp_of(v0 - base) + exp_of(v1 - base);
                 m[n][e] = top;
             }
         }
@@ -865,7 +865,7 @@ __global__ void __launch_bounds__(few_threads(PL, NT), 1) xent_few_kernel(const 
         for (int o = 16; o > 0; o >>= 1) join(mm, ss, __shfl_xor_sync(~0u, mm, o), __shfl_xor_sync(~0u, ss, o));
         if (lane == 0) {
             const int y = s_tgt[t];
-            const float l = (mm + log2f(ss)) * kLn2;
+            const float l = log_sum(mm, ss);
             p.lse[t] = y == -2 ? 0.0f : l;
             p.loss[t] = y == -2 ? 0.0f : y >= 0 ? l - __ldcg(p.tlogit + t) : __int_as_float(0x7fffffff);
         }

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2204_00595_b200 as P
-from tests.test_training_ends_gpu import backward, exact, make, near, within
+from tests.test_training_ends_gpu import IGNORE, backward, exact, forward, make, near, within
 
 pytestmark = pytest.mark.gpu
 
@@ -70,3 +70,58 @@ def test_weights_and_rows_at_opposite_ends():
     e = exact(x, W, y, dloss)
     _, dW = backward(x, W, y, e["lse"].float(), dloss)
     within(dW, e["dW"], e["dW_err"], "dW")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [5, 40, 300])
+def test_rows_whose_mask_leaves_nothing(T, dtype):
+    """Tokens all of whose words are masked by the type's lowest value: finite results, and nothing of them reaches the others."""
+    d, V = 64, 500
+    x, W, y, _ = make(T, d, V, dtype, 0.0, seed=44)
+    lowest = torch.finfo(W.dtype).min
+    masked = torch.arange(T, device="cuda") % 2 == 0
+    x[:, 0] = 0.0
+    W[:, 0] = 0.0
+    e = exact(x, W, y)
+    x[masked] = 0.0
+    x[masked, 0] = 1.0
+    W[:, 0] = lowest
+    loss, lse = forward(x, W, y)
+    within(loss[~masked], e["loss"][~masked], e["loss_err"][~masked], "loss of the others")
+    within(lse[~masked], e["lse"][~masked], e["lse_err"][~masked], "lse of the others")
+    # z = lowest for every word: lse = lowest + log V, which is lowest in float32 (half a step of it is 1e31)
+    assert torch.isfinite(loss[masked]).all() and torch.isfinite(lse[masked]).all()
+    assert bool(((lse[masked].double() - lowest).abs() <= 2.0 ** -22 * -lowest).all())
+    assert bool((loss[masked].double().abs() <= 2.0 ** -22 * -lowest).all())
+    # exp(z - lse) = 1 for the lse that is given: g = dloss (1 - [v == target]), of the others as it was
+    dloss = torch.full((T,), 2.0 ** -20, device="cuda")
+    given = torch.where(masked, torch.full_like(lse, lowest), e["lse"].float())
+    xo = torch.where(masked[:, None], torch.zeros_like(x), x)
+    o = exact(xo, torch.cat([torch.zeros_like(W[:, :1]), W[:, 1:]], 1), torch.where(masked, IGNORE, y), dloss)
+    dx, dW = backward(x, W, y, given, dloss)
+    within(dx[~masked][:, 1:], o["dx"][~masked][:, 1:], o["dx_err"][~masked][:, 1:], "dx of the others")
+    assert torch.isfinite(dx).all()
+    within(dW[:, 1:], o["dW"][:, 1:], o["dW_err"][:, 1:] + 2.0 ** -37 * 2.0 ** -19 * T, "dW")
+    hits = torch.bincount(y[masked], minlength=V).double()
+    within(dW[:, 0], 2.0 ** -20 * (float(masked.sum()) - hits), torch.full((V,), 2.0 ** -20 * T * 2.0 ** -20, device="cuda", dtype=torch.float64), "dW of the mask")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [3, 200])
+def test_logits_of_3e38(T, dtype):
+    d, V = 64, 300
+    x, W, y, _ = make(T, d, V, dtype, 0.0, seed=45)
+    x[:, 0] = 0.0
+    W[:, 0] = 0.0
+    e = exact(x, W, y)
+    top = float(torch.tensor(3e38).to(W.dtype))
+    x[1] = 0.0
+    x[1, 0] = 1.0
+    W[7, 0] = top
+    W[8, 0] = -top
+    for target, want in ((7, 0.0), (9, top)):
+        y[1] = target
+        loss, lse = forward(x, W, y)
+        assert float(lse[1]) == pytest.approx(top, rel=2.0 ** -22) and float(loss[1]) == pytest.approx(want, rel=2.0 ** -22)
+        rest = torch.arange(T, device="cuda") != 1
+        within(loss[rest], e["loss"][rest], e["loss_err"][rest], "loss of the others")
