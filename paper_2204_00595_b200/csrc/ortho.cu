@@ -753,13 +753,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) ortho_tc_kernel(const Io<T> io,
             }
         }
         phase ^= 1;
-        if (stop) {
-            let_copies_land(dead);             // nor do MMAs outlive their shared memory
-            break;
-        }
+        if (stop) break;
     }
     tc_fence_before();
-    __syncthreads();
+    if (__syncthreads_or(!ok)) let_copies_land(dead);      // nor do MMAs outlive their shared and tensor memory, the last product's among them
     if (warp == 0) tmem_dealloc(tmem, 512);
     if (holds)
 #pragma unroll
@@ -1024,7 +1021,6 @@ ortho_run_kernel(const __grid_constant__ OrthoMaps maps, const __grid_constant__
                     }
                 }
             }
-            let_copies_land(dead);
         }
     } else if (warp == 9) {
         if (rank == 0 && elect_one()) {
@@ -1087,7 +1083,7 @@ ortho_run_kernel(const __grid_constant__ OrthoMaps maps, const __grid_constant__
                 for (int i = 0; i < 32; ++i) acc[h][i] = 0.0f;
             for (int c0 = t.c0; c0 < t.c1; c0 += kSeg, ++it) {
                 const uint32_t buf = it & 1;
-                if (!pg_wait(accf0 + buf * 8, (it >> 1) & 1, p.status, dead, kErrMmaWait)) { ok = false; break; }
+                if (!pg_wait_warp(accf0 + buf * 8, (it >> 1) & 1, p.status, dead, kErrMmaWait)) { ok = false; break; }
                 tc_fence_after();
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
@@ -1201,6 +1197,7 @@ ortho_run_kernel(const __grid_constant__ OrthoMaps maps, const __grid_constant__
 
     tc_fence_before();
     __syncthreads();
+    let_copies_land(dead);                                                     // as in plane_gemm.cuh
     cluster_arrive_release();
     cluster_wait_acquire();
     if (warp == 0) tmem_dealloc_pair(tmem_base, 512);

@@ -272,6 +272,11 @@ __device__ __forceinline__ bool pg_wait(uint32_t bar, uint32_t parity, unsigned 
 {
     return mbar_try_wait_cluster_acquire(bar, parity) || pg_wait_on(bar, parity, status, dead, code);
 }
+// The same by a whole warp, which goes on or gives up together: what follows takes all lanes
+__device__ __forceinline__ bool pg_wait_warp(uint32_t bar, uint32_t parity, unsigned *status, volatile int *dead, unsigned code)
+{
+    return __all_sync(~0u, pg_wait(bar, parity, status, dead, code));
+}
 
 // Epi: struct with  begin(const Epi::Args &, const PgTile &) (a tile ahead: loads),  start(args, tile),  chunk(args, tile, c, float (&v)[32], stage)  for c = 0, 32, .. < tn / 2,
 // end(args, tile); kStage: pieces in `stage`, its warp's PgStage (0: none).  PROMOTE: at most p.seg chunks are accumulated in tensor memory, sums of those in fp32 registers.
@@ -401,7 +406,6 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
                     }
                 }
             }
-            let_copies_land(dead);
         }
     } else if (warp == 9) {
         if (rank == 0 && elect_one()) {
@@ -481,7 +485,7 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
             if constexpr (!PROMOTE) {
                 uint32_t buf = it & 1;
                 if (!t.zero) {
-                    if (!pg_wait(accf0 + buf * 8, (it >> 1) & 1, p.status, dead, kErrMmaWait)) { ok = false; break; }
+                    if (!pg_wait_warp(accf0 + buf * 8, (it >> 1) & 1, p.status, dead, kErrMmaWait)) { ok = false; break; }
                     tc_fence_after();
                     ++it;
                 }
@@ -509,7 +513,7 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
                     for (int i = 0; i < 32; ++i) acc[h][i] = 0.0f;
                 for (int c0 = at.c0; c0 < at.c1; c0 = (at.c1 - c0 > seg) ? c0 + seg : at.c1, ++it) {
                     const uint32_t buf = it & 1;
-                    if (!pg_wait(accf0 + buf * 8, (it >> 1) & 1, p.status, dead, kErrMmaWait)) { ok = false; break; }
+                    if (!pg_wait_warp(accf0 + buf * 8, (it >> 1) & 1, p.status, dead, kErrMmaWait)) { ok = false; break; }
                     tc_fence_after();
 #pragma unroll
                     for (int h = 0; h < 4; ++h) {
@@ -542,9 +546,11 @@ plane_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
         if (Epi::kStage > 0 && lane == 0) tma_store_wait_all<0>();
     }
 
-    // the even CTA's barriers receive arrivals from the odd CTA until it is done: leave together
+    // the even CTA's barriers receive arrivals from the odd CTA until it is done: leave together.  After a wait that ran out no load,
+    // which lands here, and no MMA, which reads here and writes tensor memory, may outlive this CTA, whichever warp gave up
     tc_fence_before();
     __syncthreads();
+    let_copies_land(dead);
     cluster_arrive_release();
     cluster_wait_acquire();
     if (warp == 0) tmem_dealloc_pair(tmem_base, 512);

@@ -1,12 +1,13 @@
 """The vocabulary loss and the orthogonalised update at the ends of the ranges that their documentation allows: values near the ends
 of the types' range, tokens without any word left, several host threads, workspaces of other sizes, waits that run out, and the
 precision that the results are promised up to 128 tokens."""
+import time
 
 import pytest
 import torch
 
 import paper_2204_00595_b200 as P
-from tests.test_training_ends_gpu import IGNORE, backward, exact, forward, make, near, within
+from tests.test_training_ends_gpu import DT, IGNORE, backward, exact, forward, gradient, make, near, within
 
 pytestmark = pytest.mark.gpu
 
@@ -125,3 +126,53 @@ def test_logits_of_3e38(T, dtype):
         assert float(lse[1]) == pytest.approx(top, rel=2.0 ** -22) and float(loss[1]) == pytest.approx(want, rel=2.0 ** -22)
         rest = torch.arange(T, device="cuda") != 1
         within(loss[rest], e["loss"][rest], e["loss_err"][rest], "loss of the others")
+
+
+# ------------------------------------------------------------------------------------------------ waits that run out
+def after_a_time_out(ws, call, outputs, must=True):
+    """The call under a limit of 1 us gives up instead of hanging and says so; the workspace, made anew, then serves the same call as before."""
+    def run():
+        for t in outputs:
+            t.zero_()
+        call()
+        torch.cuda.synchronize()
+        return [t.clone() for t in outputs]
+
+    want = run()
+    assert P.monarch_last_device_status(ws) == 0
+    P.monarch_debug_set_wait_limit(ws, 1)
+    t0 = time.perf_counter()
+    run()
+    assert time.perf_counter() - t0 < 5.0
+    status = P.monarch_last_device_status(ws)
+    assert status == 5 if must else status in (0, 5)       # MONARCH_ERR_TIMEOUT
+    P.monarch_workspace_init(ws)
+    assert all(torch.equal(a, b) for a, b in zip(run(), want))
+    assert P.monarch_last_device_status(ws) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("blocks,rows,cols", [(1, 300, 520), (3, 520, 300), (1, 1024, 1024)])
+def test_waits_of_large_blocks_run_out(blocks, rows, cols, dtype):
+    """Products wait for the ones before them, several microseconds each: every pair gives up at one place or another."""
+    G = gradient(blocks, rows, cols, 60).to(DT[dtype][0])
+    O = torch.empty_like(G)
+    ws = P.Workspace(P.monarch_ortho_workspace_bytes(blocks, rows, cols, DT[dtype][1]))
+    after_a_time_out(ws, lambda: P.monarch_orthogonalize(G, O, blocks, rows, cols, 5, ws), [O])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_short_waits_of_the_other_kernels(dtype):
+    """Whether a wait on chip takes longer than a microsecond is up to the device: where one does, the call ends all the same."""
+    G = gradient(4, 100, 120, 61).to(DT[dtype][0])
+    O = torch.empty_like(G)
+    ws = P.Workspace(P.monarch_ortho_workspace_bytes(4, 100, 120, DT[dtype][1]))
+    after_a_time_out(ws, lambda: P.monarch_orthogonalize(G, O, 4, 100, 120, 5, ws), [O], must=False)
+    T, d, V = 300, 512, 3000
+    x, W, y, dloss = make(T, d, V, dtype, 0.1, seed=62)
+    loss, lse, dx, dW = torch.empty(T, device="cuda"), torch.empty(T, device="cuda"), torch.empty_like(x), torch.empty(V, d, device="cuda")
+    ws = P.Workspace(P.monarch_xent_workspace_bytes(T, d, V, DT[dtype][1]))
+    after_a_time_out(ws, lambda: P.monarch_xent_fwd(x, W, y, loss, lse, T, d, V, IGNORE, ws), [loss, lse], must=False)
+    given = lse.clone()
+    ws = P.Workspace(P.monarch_xent_bwd_workspace_bytes(T, d, V, DT[dtype][1]))
+    after_a_time_out(ws, lambda: P.monarch_xent_bwd(x, W, y, given, dloss, dx, dW, 0, T, d, V, IGNORE, ws), [dx, dW], must=False)
