@@ -63,8 +63,10 @@ __device__ __forceinline__ void let_copies_land(volatile int *dead)
 __device__ __forceinline__ void depend_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void depend_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// `most`: the dynamic shared memory that any call of this kernel takes.  The limit belongs to the kernel on its device, not to the
+// launch: it is the same in every call, so that no thread lowers it under another one's launch.
 template <typename... Ts, typename... As>
-int launch_serialized(void (*kern)(Ts...), dim3 grid, int threads, int smem, cudaStream_t s, As... args)
+int launch_serialized_up_to(int most, void (*kern)(Ts...), dim3 grid, int threads, int smem, cudaStream_t s, As... args)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
@@ -77,10 +79,16 @@ int launch_serialized(void (*kern)(Ts...), dim3 grid, int threads, int smem, cud
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     // without it 48 KB at most, the kernel's static arrays (up to 8 KB) among them
-    if (smem > 40 * 1024) MONARCH_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    if (smem > 40 * 1024) MONARCH_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
     MONARCH_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, args...));
     note_launch();
     return MONARCH_OK;
+}
+// kernels that take the same amount in every call
+template <typename... Ts, typename... As>
+int launch_serialized(void (*kern)(Ts...), dim3 grid, int threads, int smem, cudaStream_t s, As... args)
+{
+    return launch_serialized_up_to(smem, kern, grid, threads, smem, s, args...);
 }
 
 }  // namespace tc

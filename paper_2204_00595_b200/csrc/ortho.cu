@@ -1478,7 +1478,7 @@ int ortho_any(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, in
             return launch_tc<T, PL, 64, 64>(io, blocks, rows, cols, steps, ws, s);
         case kWarpMma: return ortho_block<T, PL>(io, blocks, rows, cols, steps, s);
         case kFma:
-            return launch_serialized(ortho_small_kernel<T>, dim3((unsigned)blocks), kSmallThreads, (int)(small_floats(k, n) * 4), s, io, rows, cols, steps);
+            return launch_serialized_up_to((int)kSmallMax, ortho_small_kernel<T>, dim3((unsigned)blocks), kSmallThreads, (int)(small_floats(k, n) * 4), s, io, rows, cols, steps);
         default: return ortho_large<T, PL, SCHEME>(io, blocks, rows, cols, steps, dtype, ws, s);
     }
 }

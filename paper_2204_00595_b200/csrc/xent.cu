@@ -584,6 +584,7 @@ constexpr int kFewMost = 16, kFewTeam = 8;
 // 24 warps have 96 KB under way, 16 have 64; fp32 and a second column tile need the registers
 __host__ __device__ constexpr int few_threads(int planes, int tiles) { return planes == 1 && tiles == 1 ? 768 : 512; }
 __host__ __device__ constexpr int few_teams(int planes, int tiles) { return few_threads(planes, tiles) / 32 / kFewTeam; }
+constexpr size_t kFewSmem = 223 * 1024;         // of 227 KB, 4 of them static
 constexpr int kFewTicket = 16;                  // word of the status area, zero between calls
 
 int few_row(int d) { return ((d * 2 + 127) / 128 * 128 + 64) / 2; }             // rows 64 bytes apart in their banks
@@ -598,8 +599,8 @@ int few_launches(int64_t tokens, int d, int dtype, bool bwd)
 {
     const bool f32 = dtype == MONARCH_F32, again = f32 && d % 8 == 0;
     if (tokens > (again ? 3 : 1) * kFewMost) return 0;
-    int most = kFewMost;                                                        // 227 KB of shared memory, 4 of them static
-    while (most > 0 && few_smem(most, d, f32 ? 3 : 1) > 223 * 1024) --most;
+    int most = kFewMost;
+    while (most > 0 && few_smem(most, d, f32 ? 3 : 1) > kFewSmem) --most;
     if (most == 0) return 0;
     const bool all = most == kFewMost;
     const int n = ((int)tokens + most - 1) / most, limit = !f32 ? 1 : bwd || !again ? 2 : all ? 3 : 6;
@@ -1258,7 +1259,8 @@ constexpr int kFewCtas = 148;
 
 template <typename T, int PL, int NT, bool BWD> int few_launch(const FewArgs &a, cudaStream_t s)
 {
-    return launch_serialized(a.d % 8 == 0 ? xent_few_kernel<T, PL, NT, BWD, false> : xent_few_kernel<T, PL, NT, BWD, true>, dim3(kFewCtas), few_threads(PL, NT), (int)few_smem(a.tokens, a.d, PL), s, a);
+    return launch_serialized_up_to((int)kFewSmem, a.d % 8 == 0 ? xent_few_kernel<T, PL, NT, BWD, false> : xent_few_kernel<T, PL, NT, BWD, true>, dim3(kFewCtas),
+                                   few_threads(PL, NT), (int)few_smem(a.tokens, a.d, PL), s, a);
 }
 template <typename T, int PL, bool BWD> int few_any(const FewArgs &a, cudaStream_t s)
 {

@@ -1,6 +1,8 @@
 """The vocabulary loss and the orthogonalised update at the ends of the ranges that their documentation allows: values near the ends
 of the types' range, tokens without any word left, several host threads, workspaces of other sizes, waits that run out, and the
 precision that the results are promised up to 128 tokens."""
+import ctypes
+import subprocess
 import time
 
 import pytest
@@ -126,6 +128,64 @@ def test_logits_of_3e38(T, dtype):
         assert float(lse[1]) == pytest.approx(top, rel=2.0 ** -22) and float(loss[1]) == pytest.approx(want, rel=2.0 ** -22)
         rest = torch.arange(T, device="cuda") != 1
         within(loss[rest], e["loss"][rest], e["loss_err"][rest], "loss of the others")
+
+
+# ------------------------------------------------------------------------------------------------ several host threads
+HAMMER = r"""
+#include <pthread.h>
+#include <stdint.h>
+#include <stddef.h>
+typedef int (*fwd_fn)(const void *, const void *, const int64_t *, float *, float *, int64_t, int32_t, int32_t, int64_t, int, void *, size_t, void *);
+struct job { fwd_fn fn; void *p[7]; int64_t tokens; int64_t d, vocab; size_t bytes; int calls, status; };
+static void *work(void *arg)
+{
+    struct job *j = arg;
+    for (int i = 0; i < j->calls && j->status == 0; ++i)
+        j->status = j->fn(j->p[0], j->p[1], j->p[2], j->p[3], j->p[4], j->tokens, j->d, j->vocab, -100, 0, j->p[5], j->bytes, j->p[6]);
+    return 0;
+}
+int hammer(struct job *jobs, int n)
+{
+    pthread_t t[8];
+    for (int i = 0; i < n; ++i) if (pthread_create(&t[i], 0, work, &jobs[i])) return -1;
+    for (int i = 0; i < n; ++i) pthread_join(t[i], 0);
+    return 0;
+}
+"""
+
+
+class Job(ctypes.Structure):
+    _fields_ = [("fn", ctypes.c_void_p), ("p", ctypes.c_void_p * 7), ("tokens", ctypes.c_int64), ("d", ctypes.c_int64), ("vocab", ctypes.c_int64),
+                ("bytes", ctypes.c_size_t), ("calls", ctypes.c_int), ("status", ctypes.c_int)]
+
+
+def test_host_threads_with_calls_of_different_size(tmp_path):
+    """Host threads, each with its stream, tensors and workspace, whose calls take different amounts of shared memory of one kernel:
+    none lowers the limit under another's launch.  Threads of C: those of Python take turns."""
+    src, so = tmp_path / "hammer.c", tmp_path / "hammer.so"
+    src.write_text(HAMMER)
+    subprocess.run(["gcc", "-O2", "-shared", "-fPIC", "-pthread", "-o", str(so), str(src)], check=True)
+    V, T = 40, 6
+    jobs, keep = (Job * 4)(), []
+    for j, d in zip(jobs, (1032, 4096, 1536, 3200)):
+        x, W, y, _ = make(T, d, V, "f32", 0.0, seed=d)
+        loss, lse = torch.zeros(T, device="cuda"), torch.zeros(T, device="cuda")
+        ws = P.Workspace(P.monarch_xent_workspace_bytes(T, d, V, P.F32))
+        stream = torch.cuda.Stream()
+        j.fn = ctypes.cast(P.lib().monarch_xent_fwd, ctypes.c_void_p).value
+        for i, p in enumerate((x.data_ptr(), W.data_ptr(), y.data_ptr(), loss.data_ptr(), lse.data_ptr(), ws.ptr, stream.cuda_stream)):
+            j.p[i] = p
+        j.tokens, j.d, j.vocab, j.bytes, j.calls = T, d, V, ws.nbytes, 20000
+        keep.append((x, W, y, loss, lse, ws, stream))
+    torch.cuda.synchronize()
+    hammer = ctypes.CDLL(str(so)).hammer
+    hammer.argtypes = [ctypes.POINTER(Job), ctypes.c_int]
+    assert hammer(jobs, 4) == 0
+    torch.cuda.synchronize()
+    assert [j.status for j in jobs] == [0, 0, 0, 0]
+    for x, W, y, loss, lse, _, _ in keep:
+        e = exact(x, W, y)
+        within(loss, e["loss"], e["loss_err"], "loss")
 
 
 # ------------------------------------------------------------------------------------------------ waits that run out
