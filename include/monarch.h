@@ -270,7 +270,9 @@ int monarch_project(const void *A, void *L, void *R, int32_t n, int32_t m, int d
  * passed in place); tokens and vocab up to 2^24, d up to 65536: beyond, MONARCH_ERR_UNSUPPORTED.
  * Sums over d, the maximum and the sum of exponentials are fp32 in both dtypes (float32
  * operands enter the tensor cores as three bf16 parts each, 24 bits).
- * Workspace: monarch_xent_workspace_bytes (0 for invalid arguments). */
+ * Workspace: monarch_xent_workspace_bytes (0 for invalid arguments); what it gives for some number
+ * of tokens serves every smaller one of the same d, vocab and dtype as well, in smaller pieces of
+ * the vocabulary where it is less than what the smaller number would be given. */
 int monarch_xent_fwd(const void *x, const void *W, const int64_t *targets, float *loss, float *lse,
                      int64_t tokens, int32_t d, int32_t vocab, int64_t ignore_index, int dtype,
                      void *workspace, size_t workspace_bytes, void *stream);
@@ -287,8 +289,9 @@ size_t monarch_xent_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab, in
  * of x[t] and by dloss[t], at any size of these: exp(z - lse) has to stay below 4, as it does with
  * the lse of the same x and W), and of more than 128 tokens to bf16 in a bf16 dx.  Those parts leave
  * out what is below 2^-25 of the largest value of a row of x, and of a token's share in dW what is
- * below 2^-39 of the largest |dloss[t]| max |x[t]| of the call.  The order of all sums is fixed.
- * Workspace: monarch_xent_bwd_workspace_bytes (0 for invalid arguments). */
+ * below 2^-39 of the largest |dloss[t]| max |x[t]| of the call.  The order of all sums
+ * is fixed by the sizes and workspace_bytes.
+ * Workspace: monarch_xent_bwd_workspace_bytes (0 for invalid arguments); it serves fewer tokens as above. */
 int monarch_xent_bwd(const void *x, const void *W, const int64_t *targets, const float *lse,
                      const float *dloss, void *dx, float *dW, int accumulate,
                      int64_t tokens, int32_t d, int32_t vocab, int64_t ignore_index, int dtype,

@@ -182,11 +182,11 @@ int tc_staged_mlp_fwd(const void *x, const void *L1, const void *R1, const void 
 
 
 // ---- the vocabulary loss (xent.cu) and the orthogonalised update (ortho.cu) ----
-size_t xent_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab, int dtype, int bwd);
+size_t xent_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab, int dtype, int bwd, bool least = false);
 int xent_fwd(const void *x, const void *W, const int64_t *targets, float *loss, float *lse, int64_t tokens, int32_t d, int32_t vocab,
-             int64_t ignore_index, int dtype, void *ws, cudaStream_t s);
+             int64_t ignore_index, int dtype, void *ws, size_t ws_bytes, cudaStream_t s);
 int xent_bwd(const void *x, const void *W, const int64_t *targets, const float *lse, const float *dloss, void *dx, float *dW, int accumulate,
-             int64_t tokens, int32_t d, int32_t vocab, int64_t ignore_index, int dtype, void *ws, cudaStream_t s);
+             int64_t tokens, int32_t d, int32_t vocab, int64_t ignore_index, int dtype, void *ws, size_t ws_bytes, cudaStream_t s);
 size_t ortho_workspace_bytes(int64_t blocks, int32_t rows, int32_t cols, int dtype);
 int orthogonalize(const void *G, void *O, int64_t blocks, int32_t rows, int32_t cols, int32_t steps, int dtype, void *ws, cudaStream_t s);
 int muon_step(void *W, const float *dW, float *V, int64_t blocks, int32_t rows, int32_t cols, float keep, float step, float beta, int nesterov,

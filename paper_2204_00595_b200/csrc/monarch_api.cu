@@ -455,8 +455,8 @@ int monarch_xent_fwd(const void *x, const void *W, const int64_t *targets, float
     const size_t es = esize(dtype), t = (size_t)tokens;
     const Range in[] = {{x, t * d * es, 16, true}, {W, (size_t)vocab * d * es}, {targets, t * 8, 8, true}};
     const Range out[] = {{loss, t * 4, 4, true}, {lse, t * 4, 4, true}};
-    MONARCH_TRY(check_buffers(in, 3, out, 2, workspace, workspace_bytes, xent_workspace_bytes(tokens, d, vocab, dtype, 0)));
-    return xent_fwd(x, W, targets, loss, lse, tokens, d, vocab, ignore_index, dtype, workspace, (cudaStream_t)stream);
+    MONARCH_TRY(check_buffers(in, 3, out, 2, workspace, workspace_bytes, xent_workspace_bytes(tokens, d, vocab, dtype, 0, true)));
+    return xent_fwd(x, W, targets, loss, lse, tokens, d, vocab, ignore_index, dtype, workspace, workspace_bytes, (cudaStream_t)stream);
 }
 
 int monarch_xent_bwd(const void *x, const void *W, const int64_t *targets, const float *lse, const float *dloss, void *dx, float *dW,
@@ -468,8 +468,9 @@ int monarch_xent_bwd(const void *x, const void *W, const int64_t *targets, const
     const size_t es = esize(dtype), t = (size_t)tokens;
     const Range in[] = {{x, t * d * es, 16, true}, {W, (size_t)vocab * d * es}, {targets, t * 8, 8, true}, {lse, t * 4, 4, true}, {dloss, t * 4, 4, true}};
     const Range out[] = {{dx, t * d * es, 16, true}, {dW, (size_t)vocab * d * 4}};
-    MONARCH_TRY(check_buffers(in, 5, out, 2, workspace, workspace_bytes, xent_workspace_bytes(tokens, d, vocab, dtype, 1)));
-    return xent_bwd(x, W, targets, lse, dloss, dx, dW, accumulate, tokens, d, vocab, ignore_index, dtype, workspace, (cudaStream_t)stream);
+    MONARCH_TRY(check_buffers(in, 5, out, 2, workspace, workspace_bytes, xent_workspace_bytes(tokens, d, vocab, dtype, 1, true)));
+    return xent_bwd(x, W, targets, lse, dloss, dx, dW, accumulate, tokens, d, vocab, ignore_index, dtype, workspace, workspace_bytes,
+                    (cudaStream_t)stream);
 }
 
 size_t monarch_ortho_workspace_bytes(int64_t blocks, int32_t rows, int32_t cols, int dtype)

@@ -1121,6 +1121,41 @@ int bwd_piece(int64_t tokens, int d, int vocab)
     return best * 256;
 }
 
+// Where everything stands, by the choices in `l`
+void place(Layout &l, int64_t tokens, int d, int vocab, bool bwd)
+{
+    // half tiles of all pieces
+    l.halves = 2 * (vocab / l.piece * ceil_div(l.piece, l.tn) + ceil_div(vocab % l.piece, l.tn));
+    size_t at = kHead;
+    auto take = [&](size_t bytes) { const size_t o = at; at += up(bytes); return o; };
+    const size_t t = (size_t)tokens;
+    l.count = take(4);
+    l.splits = take(4);
+    l.largest = take(4);
+    l.exponent = l.xh = 0;
+    if (l.half) {
+        l.exponent = take(t * 4);
+        l.xh = take(t * l.dp * 2);
+    }
+    l.map = take(t * 4);
+    l.tgt = take(t * 4);
+    l.lse = l.dl = l.tlogit = l.part = l.g = l.dx = 0;
+    if (bwd) { l.lse = take(t * 4); l.dl = take(t * 4); }
+    else l.tlogit = take(t * 4);
+    l.x = take(t * l.dp * 2 * l.planes);
+    l.w = l.direct ? 0 : take((size_t)l.piece * l.dp * 2 * l.planes);
+    if (bwd) {
+        l.g = take((size_t)l.trows * l.piece * 2 * l.gplanes);
+        l.dx = take(t * d * 4 * l.dx_parts);
+        l.dw_splits = take(4);
+        l.dw = l.dw_parts > 1 ? take((size_t)l.piece * d * 4 * l.dw_parts) : 0;
+    } else {
+        l.part = take((size_t)l.chunk * l.halves * sizeof(float2));
+    }
+    l.total = at;
+}
+
+// What takes the least time
 Layout layout(int64_t tokens, int d, int vocab, int dtype, bool bwd)
 {
     Layout l;
@@ -1153,8 +1188,6 @@ Layout layout(int64_t tokens, int d, int vocab, int dtype, bool bwd)
     }
     const int64_t mt = ceil_div(tokens, 256);
     l.tn = pg_tile(mt, l.piece, !bwd);
-    // half tiles of all pieces
-    l.halves = 2 * (vocab / l.piece * ceil_div(l.piece, l.tn) + ceil_div(vocab % l.piece, l.tn));
     l.tn_dw = pg_tile(ceil_div(l.piece, 256), d, false);
     // dx of few tiles is split along the vocabulary, as far as the parts stay within L2; narrow tiles where there would be many parts
     l.tn_dx = mt * ceil_div(d, 256) >= 8 ? 256 : 128;
@@ -1172,34 +1205,47 @@ Layout layout(int64_t tokens, int d, int vocab, int dtype, bool bwd)
         if (n > kPgPairs) n = kPgPairs;
         if (n > 1) l.dw_parts = (int)n;
     }
-    size_t at = kHead;
-    auto take = [&](size_t bytes) { const size_t o = at; at += up(bytes); return o; };
-    const size_t t = (size_t)tokens;
-    l.count = take(4);
-    l.splits = take(4);
-    l.largest = take(4);
-    l.exponent = l.xh = 0;
-    if (l.half) {
-        l.exponent = take(t * 4);
-        l.xh = take(t * l.dp * 2);
-    }
-    l.map = take(t * 4);
-    l.tgt = take(t * 4);
-    l.lse = l.dl = l.tlogit = l.part = l.g = l.dx = 0;
-    if (bwd) { l.lse = take(t * 4); l.dl = take(t * 4); }
-    else l.tlogit = take(t * 4);
-    l.x = take(t * l.dp * 2 * l.planes);
-    l.w = l.direct ? 0 : take((size_t)l.piece * l.dp * 2 * l.planes);
-    if (bwd) {
-        l.g = take((size_t)l.trows * l.piece * 2 * l.gplanes);
-        l.dx = take(t * d * 4 * l.dx_parts);
-        l.dw_splits = take(4);
-        l.dw = l.dw_parts > 1 ? take((size_t)l.piece * d * 4 * l.dw_parts) : 0;
-    } else {
-        l.part = take((size_t)l.chunk * l.halves * sizeof(float2));
-    }
-    l.total = at;
+    place(l, tokens, d, vocab, bwd);
     return l;
+}
+
+// The same in pieces of `units` 256 vocabulary entries, without parts (parts: dx keeps its own).  With widest tiles in the forward pass: fewest
+// sums in memory.  Everything here grows with the tokens and the units.
+Layout smaller(const Layout &best, int64_t tokens, int d, int vocab, bool bwd, int units, bool parts)
+{
+    Layout l = best;
+    l.piece = units * 256 < best.piece ? units * 256 : best.piece;
+    if (!bwd) l.tn = 256;
+    l.tn_dw = pg_tile(ceil_div(l.piece, 256), d, false);
+    l.dw_parts = 1;
+    l.dx_parts = !parts ? 1 : best.dx_parts < units ? best.dx_parts : units;
+    place(l, tokens, d, vocab, bwd);
+    return l;
+}
+
+// What takes the least time within `bytes`.  Pieces and parts are chosen by the tokens, and fewer tokens may take more memory (gradient, bf16, d 1024,
+// vocabulary 50257: 4096 tokens 499 MB, 5000 tokens 470): a workspace that was asked for with more tokens serves fewer in smaller pieces.
+Layout layout_within(size_t bytes, int64_t tokens, int d, int vocab, int dtype, bool bwd)
+{
+    const Layout best = layout(tokens, d, vocab, dtype, bwd);
+    if (best.total <= bytes) return best;
+    const int most = ceil_div(best.piece, 256);
+    for (int parts = 1; parts >= 0; --parts) {
+        int units = 0;                                                        // the most that fit
+        for (int lo = 1, hi = most; lo <= hi;) {
+            const int mid = lo + (hi - lo) / 2;
+            if (smaller(best, tokens, d, vocab, bwd, mid, parts != 0).total <= bytes) { units = mid; lo = mid + 1; }
+            else hi = mid - 1;
+        }
+        // dx in parts only where they leave room for pieces of some size: each is four launches and its last round of tiles
+        if (units >= (parts ? (most < 8 ? most : 8) : 1)) return smaller(best, tokens, d, vocab, bwd, units, parts != 0);
+    }
+    return best;
+}
+// the least that a call takes
+size_t least_bytes(int64_t tokens, int d, int vocab, int dtype, bool bwd)
+{
+    return smaller(layout(tokens, d, vocab, dtype, bwd), tokens, d, vocab, bwd, 1, false).total;
 }
 
 template <typename T, int PL, bool BWD> int prep(PrepArgs a, cudaStream_t s)
@@ -1332,21 +1378,22 @@ int few_bwd(int launches, const T *x, const T *W, const int64_t *targets, const 
 }  // namespace
 }  // namespace tc
 
-size_t xent_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab, int dtype, int bwd)
+// A workspace sized for a batch serves every smaller one, on whichever kernels: also the few tokens' parts, whose size is the same for all.
+// `least`: what a call needs, else what it runs best with.
+size_t xent_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab, int dtype, int bwd, bool least)
 {
-    // a workspace sized for a batch serves every smaller one, on whichever kernels: also the few tokens' parts
     const size_t few = bwd ? tc::few_bwd_bytes(d, vocab) : tc::kHead + tc::kFewMost * (4 + 8 * tc::kFewCtas);
-    const size_t need = tc::layout(tokens, d, vocab, dtype, bwd != 0).total;
+    const size_t need = least ? tc::least_bytes(tokens, d, vocab, dtype, bwd != 0) : tc::layout(tokens, d, vocab, dtype, bwd != 0).total;
     return need > few ? need : few;
 }
 
 int xent_fwd(const void *x, const void *W, const int64_t *targets, float *loss, float *lse, int64_t tokens, int32_t d, int32_t vocab,
-             int64_t ignore_index, int dtype, void *ws, cudaStream_t s)
+             int64_t ignore_index, int dtype, void *ws, size_t ws_bytes, cudaStream_t s)
 {
     using namespace tc;
     if (tokens == 0) return MONARCH_OK;
     if (const int launches = few_launches(tokens, d, dtype, false)) return few(launches, x, W, targets, loss, lse, (int)tokens, d, vocab, ignore_index, dtype, ws, s);
-    const Layout l = layout(tokens, d, vocab, dtype, false);
+    const Layout l = layout_within(ws_bytes, tokens, d, vocab, dtype, false);
     char *base = (char *)ws;
     unsigned *status = (unsigned *)ws;
     int *count = (int *)(base + l.count), *map = (int *)(base + l.map), *tgt = (int *)(base + l.tgt);
@@ -1493,7 +1540,7 @@ int bwd_pieces(const Layout &l, const void *W, T *dx, float *dW, int accumulate,
 }  // namespace tc
 
 int xent_bwd(const void *x, const void *W, const int64_t *targets, const float *lse, const float *dloss, void *dx, float *dW, int accumulate,
-             int64_t tokens, int32_t d, int32_t vocab, int64_t ignore_index, int dtype, void *ws, cudaStream_t s)
+             int64_t tokens, int32_t d, int32_t vocab, int64_t ignore_index, int dtype, void *ws, size_t ws_bytes, cudaStream_t s)
 {
     using namespace tc;
     if (tokens == 0) {
@@ -1506,7 +1553,7 @@ int xent_bwd(const void *x, const void *W, const int64_t *targets, const float *
         return few_bwd<__nv_bfloat16, 1>(launches, (const __nv_bfloat16 *)x, (const __nv_bfloat16 *)W, targets, lse, dloss, (__nv_bfloat16 *)dx, dW, accumulate, (int)tokens, d, vocab,
                                          ignore_index, ws, s);
     }
-    const Layout l = layout(tokens, d, vocab, dtype, true);
+    const Layout l = layout_within(ws_bytes, tokens, d, vocab, dtype, true);
     char *base = (char *)ws;
     PrepArgs a = {};
     a.x = x; a.targets = targets; a.lse_in = lse; a.dloss = dloss; a.dx = dx;

@@ -236,3 +236,55 @@ def test_short_waits_of_the_other_kernels(dtype):
     given = lse.clone()
     ws = P.Workspace(P.monarch_xent_bwd_workspace_bytes(T, d, V, DT[dtype][1]))
     after_a_time_out(ws, lambda: P.monarch_xent_bwd(x, W, y, given, dloss, dx, dW, 0, T, d, V, IGNORE, ws), [dx, dW], must=False)
+
+
+# ------------------------------------------------------------------------------------------------ workspaces of other sizes
+def least(refused, most):
+    """The smallest workspace that a call is not refused for (tests/test_training_ends_workspaces.py: nothing is launched)."""
+    low, high = 0, most
+    while high - low > 1:
+        mid = (low + high) // 2
+        low, high = (mid, high) if refused(mid) else (low, mid)
+    return high
+
+
+class Guarded(P.Workspace):
+    """A workspace of exactly n bytes with a band behind it that no call may touch."""
+
+    def __init__(self, n):
+        super().__init__(n + 65536)
+        at = self.ptr - self.buf.data_ptr() + n
+        self.nbytes, self.band = n, self.buf[at:at + 65536]
+        self.band.fill_(0x5A)
+
+    def untouched(self):
+        return bool((self.band == 0x5A).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d,V", [(300, 136, 5000), (129, 250, 3000), (2100, 64, 700), (200, 520, 257), (50, 1000, 20000)])
+def test_loss_and_gradient_within_less_memory(T, d, V, dtype):
+    """From the workspace that the query reports down to the least that is taken: pieces of the vocabulary, results within their bounds."""
+    x, W, y, dloss = make(T, d, V, dtype, 0.1, seed=70)
+    e = exact(x, W, y, dloss)
+    code = DT[dtype][1]
+    need = P.monarch_xent_workspace_bytes(T, d, V, code)
+    p = [(i + 1) << 44 for i in range(8)]                  # never dereferenced: overlapping outputs are refused behind the workspace
+    low = least(lambda n: P.lib().monarch_xent_fwd(p[0], p[1], p[2], p[3], p[3], T, d, V, IGNORE, code, p[4], n, None) == 3, need)
+    for n in sorted({low, (low + need) // 2, max(low, need - 1), need, 2 * need}):
+        ws = Guarded(n)
+        loss, lse = forward(x, W, y, ws=ws)
+        within(loss, e["loss"], e["loss_err"], "loss")
+        within(lse, e["lse"], e["lse_err"], "lse")
+        assert ws.untouched(), n
+    need = P.monarch_xent_bwd_workspace_bytes(T, d, V, code)
+    low = least(lambda n: P.lib().monarch_xent_bwd(*p[:5], p[5], p[5], 0, T, d, V, IGNORE, code, p[6], n, None) == 3, need)
+    assert low < need or V != 5000
+    for n in sorted({low, low + (need - low) // 8, (low + need) // 2, max(low, need - 1), need, 2 * need}):
+        ws = Guarded(n)
+        dx, dW = backward(x, W, y, e["lse"].float(), dloss, ws=ws)
+        within(dx, e["dx"], e["dx_err"], "dx")
+        within(dW, e["dW"], e["dW_err"], "dW")
+        assert ws.untouched(), n
+        again, dW2 = backward(x, W, y, e["lse"].float(), dloss, ws=ws)
+        assert torch.equal(dx, again) and torch.equal(dW, dW2)
