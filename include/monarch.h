@@ -307,7 +307,8 @@ size_t monarch_xent_bwd_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab
  * [q][b][b1] or [b][r][q], a dense matrix one block.  A block of zeros gives zeros; one with an infinity
  * or NaN gives NaN, in that block alone.  rows, cols up to 32768, blocks up to 2^20, steps 1 to 32.
  * Products are held to fp32 (float32 O) or to 16 bits or more (bf16 O), sums are fp32, the norm is summed in fp64.
- * Workspace: monarch_ortho_workspace_bytes (0 for invalid arguments). */
+ * Workspace: monarch_ortho_workspace_bytes (0 for invalid arguments); what it gives for some number of
+ * blocks serves every smaller one of the same sides and dtype as well. */
 int monarch_orthogonalize(const void *G, void *O, int64_t blocks, int32_t rows, int32_t cols, int32_t steps,
                           int dtype, void *workspace, size_t workspace_bytes, void *stream);
 size_t monarch_ortho_workspace_bytes(int64_t blocks, int32_t rows, int32_t cols, int dtype);

@@ -187,10 +187,11 @@ int xent_fwd(const void *x, const void *W, const int64_t *targets, float *loss, 
              int64_t ignore_index, int dtype, void *ws, size_t ws_bytes, cudaStream_t s);
 int xent_bwd(const void *x, const void *W, const int64_t *targets, const float *lse, const float *dloss, void *dx, float *dW, int accumulate,
              int64_t tokens, int32_t d, int32_t vocab, int64_t ignore_index, int dtype, void *ws, size_t ws_bytes, cudaStream_t s);
-size_t ortho_workspace_bytes(int64_t blocks, int32_t rows, int32_t cols, int dtype);
-int orthogonalize(const void *G, void *O, int64_t blocks, int32_t rows, int32_t cols, int32_t steps, int dtype, void *ws, cudaStream_t s);
+size_t ortho_workspace_bytes(int64_t blocks, int32_t rows, int32_t cols, int dtype, bool least = false);
+int orthogonalize(const void *G, void *O, int64_t blocks, int32_t rows, int32_t cols, int32_t steps, int dtype, void *ws, size_t ws_bytes,
+                  cudaStream_t s);
 int muon_step(void *W, const float *dW, float *V, int64_t blocks, int32_t rows, int32_t cols, float keep, float step, float beta, int nesterov,
-              int32_t steps, int dtype, void *ws, cudaStream_t s);
+              int32_t steps, int dtype, void *ws, size_t ws_bytes, cudaStream_t s);
 
 // m = 128 as chains of block GEMMs on token-innermost planes (chain_m128.cu)
 size_t chain_fwd_m128_workspace_bytes(int64_t tokens);

@@ -485,8 +485,8 @@ int monarch_orthogonalize(const void *G, void *O, int64_t blocks, int32_t rows, 
     const size_t bytes = (size_t)blocks * rows * cols * esize(dtype);
     const Range in[] = {{G, bytes, 16, true}};
     const Range out[] = {{O, bytes, 16, true}};
-    MONARCH_TRY(check_buffers(in, 1, out, 1, workspace, workspace_bytes, ortho_workspace_bytes(blocks, rows, cols, dtype)));
-    return orthogonalize(G, O, blocks, rows, cols, steps, dtype, workspace, (cudaStream_t)stream);
+    MONARCH_TRY(check_buffers(in, 1, out, 1, workspace, workspace_bytes, ortho_workspace_bytes(blocks, rows, cols, dtype, true)));
+    return orthogonalize(G, O, blocks, rows, cols, steps, dtype, workspace, workspace_bytes, (cudaStream_t)stream);
 }
 
 int monarch_muon_step(void *W, const float *dW, float *V, int64_t blocks, int32_t rows, int32_t cols, double lr, double weight_decay,
@@ -499,9 +499,9 @@ int monarch_muon_step(void *W, const float *dW, float *V, int64_t blocks, int32_
     const size_t n = (size_t)blocks * rows * cols;
     const Range in[] = {{dW, n * 4, 16, true}};
     const Range out[] = {{W, n * esize(dtype), 16, true}, {V, n * 4, 16, true}};
-    MONARCH_TRY(check_buffers(in, 1, out, 2, workspace, workspace_bytes, ortho_workspace_bytes(blocks, rows, cols, dtype)));
+    MONARCH_TRY(check_buffers(in, 1, out, 2, workspace, workspace_bytes, ortho_workspace_bytes(blocks, rows, cols, dtype, true)));
     return muon_step(W, dW, V, blocks, rows, cols, (float)(1.0 - lr * weight_decay), (float)(lr * scale), (float)beta, nesterov, steps, dtype,
-                     workspace, (cudaStream_t)stream);
+                     workspace, workspace_bytes, (cudaStream_t)stream);
 }
 
 size_t monarch_rect_workspace_bytes(int64_t tokens, int32_t q, int32_t b1, int32_t b, int32_t r, int dtype)

@@ -863,7 +863,7 @@ struct Product {
     int rows, cols, kchunks;
     int a_mn, b_mn;                // operands stored with K along their rows
     int tn, sub, lower;            // columns of a tile; tiles in 256 columns; symmetric result
-    int mtiles, ntiles, tiles;     // of a block
+    int ntiles, tiles;             // of a block
     int splits, per_split;         // parts of K, chunks in one
     int publishers;                // warps that publish something of a tile
     float scale, diagonal;         // of the result
@@ -1286,15 +1286,15 @@ __global__ void __launch_bounds__(256) start_kernel(const Planes x, const Io<T> 
 }
 
 // Tiles and parts of a product by the time they take on a block's share of the CTA pairs, in cycles: `products` MMAs of 512 cycles per
-// K chunk (narrow tiles load more per MMA), 4000 for a tile's start and end, 6000 and 1000 each for parts.
-Product cut(int64_t blocks, int m, int n, int kdim, int products, bool lower)
+// K chunk (narrow tiles load more per MMA), 4000 for a tile's start and end, 6000 and 1000 each for parts, `most` of them.
+Product cut(int64_t blocks, int m, int n, int kdim, int products, bool lower, int most)
 {
     Product best = {};
     double best_cost = 1e300;
     const int64_t mt = ceil_div(m, 256), chunks = ceil_div(kdim, kPgChunk), share = blocks >= kPgPairs ? 1 : kPgPairs / (blocks > 0 ? blocks : 1);
     for (int tn = 256; tn >= 128; tn /= 2) {
         const int64_t tiles = lower ? mt * (mt + 1) / 2 * (256 / tn) : mt * ceil_div(n, tn);
-        for (int s = 1; s <= 16 && s <= chunks; ++s) {
+        for (int s = 1; s <= most && s <= chunks; ++s) {
             if (s > 1 && tiles * s > share) break;
             const int64_t rounds = (tiles * s + share - 1) / share, per = (chunks + s - 1) / s;
             const double chunk = 512.0 * products * tn / 256 * (tn == 128 ? 1.2 : 1.0);
@@ -1314,7 +1314,6 @@ Product cut(int64_t blocks, int m, int n, int kdim, int products, bool lower)
     best.publishers = best.splits == 1 ? 16 : 16 * (best.splits < best.tn / 64 ? best.splits : best.tn / 64);
     best.sub = 256 / best.tn;
     best.lower = lower;
-    best.mtiles = (int)mt;
     best.ntiles = ceil_div(n, best.tn);
     best.scale = 1.0f;
     return best;
@@ -1327,7 +1326,9 @@ struct Large {
     size_t norm, count, xp[2], sp, pp, part, total;
 };
 
-Large large_layout(int64_t blocks, int rows, int cols, int dtype)
+constexpr int kMostParts = 16;
+
+Large large_layout(int64_t blocks, int rows, int cols, int dtype, int most = kMostParts)
 {
     Large l;
     l.k = rows < cols ? rows : cols;
@@ -1337,9 +1338,9 @@ Large large_layout(int64_t blocks, int rows, int cols, int dtype)
     l.planes = dtype == MONARCH_F32 ? 3 : 2;
     const int products = dtype == MONARCH_F32 ? 6 : 3;
     const bool wide = rows <= cols;
-    l.prod[0] = cut(blocks, l.k, l.k, l.n, products, true);
-    l.prod[1] = cut(blocks, l.k, l.k, l.k, products, true);
-    l.prod[2] = cut(blocks, rows, cols, l.k, products, false);
+    l.prod[0] = cut(blocks, l.k, l.k, l.n, products, true, most);
+    l.prod[1] = cut(blocks, l.k, l.k, l.k, products, true, most);
+    l.prod[2] = cut(blocks, rows, cols, l.k, products, false, most);
     l.prod[0].a_mn = l.prod[0].b_mn = !wide;
     l.prod[2].b_mn = wide;
     l.prod[0].diagonal = kBeta;
@@ -1368,10 +1369,19 @@ Large large_layout(int64_t blocks, int rows, int cols, int dtype)
     return l;
 }
 
-template <typename T, int PL, int SCHEME>
-int ortho_large(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, int dtype, void *ws, cudaStream_t s)
+// Fewer blocks are cut into more parts and may take more memory (512 x 512, fp32: 4 blocks 42 MB, 5 blocks 30): a workspace that was asked for
+// with more blocks serves fewer in as many parts as it has room for.
+Large large_within(size_t bytes, int64_t blocks, int rows, int cols, int dtype)
 {
-    const Large l = large_layout(blocks, rows, cols, dtype);
+    Large l = large_layout(blocks, rows, cols, dtype);
+    for (int most = kMostParts - 1; l.total > bytes && most >= 1; --most) l = large_layout(blocks, rows, cols, dtype, most);
+    return l;
+}
+
+template <typename T, int PL, int SCHEME>
+int ortho_large(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, int dtype, void *ws, size_t ws_bytes, cudaStream_t s)
+{
+    const Large l = large_within(ws_bytes, blocks, rows, cols, dtype);
     char *base = (char *)ws;
     const bool wide = rows <= cols;
     double *norm = (double *)(base + l.norm);
@@ -1457,7 +1467,7 @@ int ortho_large(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, 
 }
 
 // Which kernel serves blocks whose smaller side is k and larger side n; not by their number, so that a workspace for many blocks
-// serves fewer.
+// serves fewer (large_within).
 enum Kernel { kWarpMma, kTcgen05, kFma, kRun };
 Kernel kernel_for(int k, int n)
 {
@@ -1467,7 +1477,7 @@ Kernel kernel_for(int k, int n)
 }
 
 template <typename T, int PL, int SCHEME>
-int ortho_any(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, int dtype, void *ws, cudaStream_t s)
+int ortho_any(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, int dtype, void *ws, size_t ws_bytes, cudaStream_t s)
 {
     if (blocks == 0) return MONARCH_OK;
     const int k = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
@@ -1479,38 +1489,39 @@ int ortho_any(const Io<T> &io, int64_t blocks, int rows, int cols, int steps, in
         case kWarpMma: return ortho_block<T, PL>(io, blocks, rows, cols, steps, s);
         case kFma:
             return launch_serialized_up_to((int)kSmallMax, ortho_small_kernel<T>, dim3((unsigned)blocks), kSmallThreads, (int)(small_floats(k, n) * 4), s, io, rows, cols, steps);
-        default: return ortho_large<T, PL, SCHEME>(io, blocks, rows, cols, steps, dtype, ws, s);
+        default: return ortho_large<T, PL, SCHEME>(io, blocks, rows, cols, steps, dtype, ws, ws_bytes, s);
     }
 }
 
 }  // namespace
 }  // namespace tc
 
-size_t ortho_workspace_bytes(int64_t blocks, int32_t rows, int32_t cols, int dtype)
+// `least`: what a call needs, else what it runs best with
+size_t ortho_workspace_bytes(int64_t blocks, int32_t rows, int32_t cols, int dtype, bool least)
 {
     const int k = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
-    return tc::kernel_for(k, n) != tc::kRun ? (size_t)MONARCH_STATUS_BYTES : tc::large_layout(blocks, rows, cols, dtype).total;
+    return tc::kernel_for(k, n) != tc::kRun ? (size_t)MONARCH_STATUS_BYTES : tc::large_layout(blocks, rows, cols, dtype, least ? 1 : tc::kMostParts).total;
 }
 
-int orthogonalize(const void *G, void *O, int64_t blocks, int32_t rows, int32_t cols, int32_t steps, int dtype, void *ws, cudaStream_t s)
+int orthogonalize(const void *G, void *O, int64_t blocks, int32_t rows, int32_t cols, int32_t steps, int dtype, void *ws, size_t ws_bytes, cudaStream_t s)
 {
     if (dtype == MONARCH_F32) {
         const tc::Io<float> io = {G, nullptr, (float *)O, 0.0f, 0.0f, 0.0f, 0};
-        return tc::ortho_any<float, 3, tc::kP3x3>(io, blocks, rows, cols, steps, dtype, ws, s);
+        return tc::ortho_any<float, 3, tc::kP3x3>(io, blocks, rows, cols, steps, dtype, ws, ws_bytes, s);
     }
     const tc::Io<__nv_bfloat16> io = {G, nullptr, (__nv_bfloat16 *)O, 0.0f, 0.0f, 0.0f, 0};
-    return tc::ortho_any<__nv_bfloat16, 2, tc::kP2x2>(io, blocks, rows, cols, steps, dtype, ws, s);
+    return tc::ortho_any<__nv_bfloat16, 2, tc::kP2x2>(io, blocks, rows, cols, steps, dtype, ws, ws_bytes, s);
 }
 
 int muon_step(void *W, const float *dW, float *V, int64_t blocks, int32_t rows, int32_t cols, float keep, float step, float beta, int nesterov,
-              int32_t steps, int dtype, void *ws, cudaStream_t s)
+              int32_t steps, int dtype, void *ws, size_t ws_bytes, cudaStream_t s)
 {
     if (dtype == MONARCH_F32) {
         const tc::Io<float> io = {dW, V, (float *)W, keep, step, beta, nesterov};
-        return tc::ortho_any<float, 3, tc::kP3x3>(io, blocks, rows, cols, steps, dtype, ws, s);
+        return tc::ortho_any<float, 3, tc::kP3x3>(io, blocks, rows, cols, steps, dtype, ws, ws_bytes, s);
     }
     const tc::Io<__nv_bfloat16> io = {dW, V, (__nv_bfloat16 *)W, keep, step, beta, nesterov};
-    return tc::ortho_any<__nv_bfloat16, 2, tc::kP2x2>(io, blocks, rows, cols, steps, dtype, ws, s);
+    return tc::ortho_any<__nv_bfloat16, 2, tc::kP2x2>(io, blocks, rows, cols, steps, dtype, ws, ws_bytes, s);
 }
 
 }  // namespace monarch

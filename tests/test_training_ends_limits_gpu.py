@@ -9,7 +9,7 @@ import pytest
 import torch
 
 import paper_2204_00595_b200 as P
-from tests.test_training_ends_gpu import DT, IGNORE, backward, exact, forward, gradient, make, near, within
+from tests.test_training_ends_gpu import DT, IGNORE, backward, exact, forward, gradient, make, near, newton_schulz, ortho, within
 
 pytestmark = pytest.mark.gpu
 
@@ -288,3 +288,18 @@ def test_loss_and_gradient_within_less_memory(T, d, V, dtype):
         assert ws.untouched(), n
         again, dW2 = backward(x, W, y, e["lse"].float(), dloss, ws=ws)
         assert torch.equal(dx, again) and torch.equal(dW, dW2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("blocks,rows,cols", [(2, 1030, 260), (1, 1024, 1024), (12, 63, 897), (1, 200, 3000)])
+def test_update_within_less_memory(blocks, rows, cols, dtype):
+    G = gradient(blocks, rows, cols, 71).to(DT[dtype][0])
+    want = newton_schulz(G.double())
+    need = P.monarch_ortho_workspace_bytes(blocks, rows, cols, DT[dtype][1])
+    p = [1 << 44, 2 << 44]
+    low = least(lambda n: P.lib().monarch_orthogonalize(p[0], p[0], blocks, rows, cols, 5, DT[dtype][1], p[1], n, None) == 3, need)
+    assert low < need
+    for n in (low, low + (need - low) // 3, need - 1, need, 2 * need):
+        ws = Guarded(n)
+        near(ortho(G, ws=ws), want, dtype, "O")
+        assert ws.untouched(), n

@@ -61,3 +61,29 @@ def test_fewer_tokens_with_the_workspace_of_more_at_any_sizes(lib, call):
         assert run(lib, t, d, V, code, large) == INVALID, (code, d, V, t, T)
         assert run(lib, t, d, V, code, 1 << 16) == WORKSPACE
     assert more > 20                             # the sizes met are not all of the plain kind
+
+
+def update(lib, blocks, rows, cols, code, nbytes):
+    out, ws = ADDRESS[:2]
+    return lib.monarch_orthogonalize(out, out, blocks, rows, cols, 5, code, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("code,rows,cols,few,many", [(B.BF16, 63, 897, 12, 16), (B.F32, 512, 512, 4, 5), (B.F32, 512, 512, 4, 6)])
+def test_fewer_blocks_with_the_workspace_of_more(lib, code, rows, cols, few, many):
+    need = B.monarch_ortho_workspace_bytes
+    assert need(few, rows, cols, code) > need(many, rows, cols, code)
+    assert update(lib, few, rows, cols, code, need(many, rows, cols, code)) == INVALID
+
+
+def test_fewer_blocks_with_the_workspace_of_more_at_any_sizes(lib):
+    rng = random.Random(8)
+    more = 0
+    for _ in range(4000):
+        code, rows, cols = rng.choice([B.F32, B.BF16]), log_int(rng, 1, 4096), log_int(rng, 1, 4096)
+        most = log_int(rng, 1, 300)
+        blocks = rng.randint(1, most)
+        large = B.monarch_ortho_workspace_bytes(most, rows, cols, code)
+        more += B.monarch_ortho_workspace_bytes(blocks, rows, cols, code) > large
+        assert update(lib, blocks, rows, cols, code, large) == INVALID, (code, rows, cols, blocks, most)
+        assert update(lib, blocks, rows, cols, code, 128) == WORKSPACE
+    assert more > 20
