@@ -584,6 +584,7 @@ constexpr int kFewMost = 16, kFewTeam = 8;
 // 24 warps have 96 KB under way, 16 have 64; fp32 and a second column tile need the registers
 __host__ __device__ constexpr int few_threads(int planes, int tiles) { return planes == 1 && tiles == 1 ? 768 : 512; }
 __host__ __device__ constexpr int few_teams(int planes, int tiles) { return few_threads(planes, tiles) / 32 / kFewTeam; }
+constexpr int64_t kPieceBytes = (int64_t)128 << 20;         // planes of W in a piece of the vocabulary (forward)
 constexpr size_t kFewSmem = 223 * 1024;         // of 227 KB, 4 of them static
 constexpr int kFewTicket = 16;                  // word of the status area, zero between calls
 
@@ -591,19 +592,25 @@ int few_row(int d) { return ((d * 2 + 127) / 128 * 128 + 64) / 2; }             
 int few_tiles(int tokens) { return tokens <= 8 ? 1 : 2; }                       // column tiles of 8 tokens: what the kernels are built for
 size_t few_x(int tokens, int d, int planes) { return (size_t)tokens * few_row(d) * 2 * planes; }
 size_t few_smem(int tokens, int d, int planes) { return few_x(tokens, d, planes) + (size_t)few_teams(planes, few_tiles(tokens)) * 2 * kFewTeam * few_tiles(tokens) * 512; }
-// launches of few tokens that the call takes; 0: tiles.  fp32, d 1024 / 4096 (launches of 16 / 8 tokens), vocabularies of 50257 / 32768:
-// a launch 68 / 136 us forward and 184 / 365 backward, the tile kernels 218 / 590 and 455 / 950.  Rows of other than 16-byte multiples are
-// read value by value, up to 16 tokens (us, on tiles in brackets; 5 tokens, d 1018, 50257: bf16 48 (109) and 188 (322), fp32 69 (273)
-// and 157 (554); 3 tokens, d 3661, 57446, fp32: 238 (1410) and 588 (2058))
-int few_launches(int64_t tokens, int d, int dtype, bool bwd)
+// Launches of few tokens that the call takes; 0: tiles.  fp32, us of n launches (on tiles):
+//   forward   two always: d 1024, vocabulary 50257 144 (224), 512, 2000 27 (29), 4096, 32768 282 (590), 8192, 16384 306 (565)
+//             three where a launch holds up to 8 tokens: 4096, 32768 419 (589), 4096, 2000 91 (98), 8192, 1000 139 (168)
+//             or where W is more than one piece of the tile kernels: 1024, 50257 212 (226), 2048, 32768 269 (316), 2560, 20000 245 (278);
+//             else not: 1024, 16000 102 (83), 512, 8000 49 (36), 2048, 4000 76 (65)
+//             four: 4096, 32768 557 (589), but 4096, 4000 129 (123), 8192, 16384 604 (565), 2048, 32768 342 (314)
+//   backward  two: 1024, 50257 381 (473), 512, 2000 42 (60), 4096, 32768 764 (973), 8192, 16384 805 (975)
+//             three: 1024, 50257 571 (473), 4096, 32768 1135 (979)
+// Rows of other than 16-byte multiples are read value by value, up to 16 tokens (5 tokens, d 1018, 50257: bf16 48 (109) and 188 (322), fp32
+// 69 (273) and 157 (554); 3 tokens, d 3661, 57446, fp32: 238 (1410) and 588 (2058))
+int few_launches(int64_t tokens, int d, int vocab, int dtype, bool bwd)
 {
     const bool f32 = dtype == MONARCH_F32, again = f32 && d % 8 == 0;
     if (tokens > (again ? 3 : 1) * kFewMost) return 0;
     int most = kFewMost;
     while (most > 0 && few_smem(most, d, f32 ? 3 : 1) > kFewSmem) --most;
     if (most == 0) return 0;
-    const bool all = most == kFewMost;
-    const int n = ((int)tokens + most - 1) / most, limit = !f32 ? 1 : bwd || !again ? 2 : all ? 3 : 6;
+    const bool pieces = (int64_t)vocab * d * 6 > kPieceBytes;
+    const int n = ((int)tokens + most - 1) / most, limit = !f32 ? 1 : bwd || !again ? 2 : most <= 8 || pieces ? 3 : 2;
     return n <= limit ? n : 0;
 }
 
@@ -1174,7 +1181,7 @@ Layout layout(int64_t tokens, int d, int vocab, int dtype, bool bwd)
             // planes of W within 128 MB, or whole rounds of the pairs over tiles of 128 columns, one at least, where that takes fewer
             // column rounds for an entry (fp32, 128 tokens: d 1024, vocabulary 50257: 249 -> 218 us; d 4096, 32768: 840 -> 597)
             const int mt = ceil_div(tokens > 0 ? tokens : 1, 256), half = kPgPairs / mt / 2, unit = (half > 0 ? half : 1) * 256;
-            const int64_t most = ((int64_t)128 << 20) / ((int64_t)l.dp * 2 * l.planes);
+            const int64_t most = kPieceBytes / ((int64_t)l.dp * 2 * l.planes);
             auto cost = [&](int piece) {
                 const int tn = pg_tile(mt, piece, true);
                 return (double)ceil_div((int64_t)mt * ceil_div(piece, tn), kPgPairs) * tn * (tn == 256 ? 10 : tn == 192 ? 11 : 12) / piece;
@@ -1392,7 +1399,7 @@ int xent_fwd(const void *x, const void *W, const int64_t *targets, float *loss, 
 {
     using namespace tc;
     if (tokens == 0) return MONARCH_OK;
-    if (const int launches = few_launches(tokens, d, dtype, false)) return few(launches, x, W, targets, loss, lse, (int)tokens, d, vocab, ignore_index, dtype, ws, s);
+    if (const int launches = few_launches(tokens, d, vocab, dtype, false)) return few(launches, x, W, targets, loss, lse, (int)tokens, d, vocab, ignore_index, dtype, ws, s);
     const Layout l = layout_within(ws_bytes, tokens, d, vocab, dtype, false);
     char *base = (char *)ws;
     unsigned *status = (unsigned *)ws;
@@ -1547,7 +1554,7 @@ int xent_bwd(const void *x, const void *W, const int64_t *targets, const float *
         if (!accumulate) MONARCH_CUDA_TRY(cudaMemsetAsync(dW, 0, (size_t)vocab * d * sizeof(float), s));
         return MONARCH_OK;
     }
-    if (const int launches = few_launches(tokens, d, dtype, true)) {
+    if (const int launches = few_launches(tokens, d, vocab, dtype, true)) {
         if (dtype == MONARCH_F32)
             return few_bwd<float, 3>(launches, (const float *)x, (const float *)W, targets, lse, dloss, (float *)dx, dW, accumulate, (int)tokens, d, vocab, ignore_index, ws, s);
         return few_bwd<__nv_bfloat16, 1>(launches, (const __nv_bfloat16 *)x, (const __nv_bfloat16 *)W, targets, lse, dloss, (__nv_bfloat16 *)dx, dW, accumulate, (int)tokens, d, vocab,

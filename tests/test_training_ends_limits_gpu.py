@@ -188,6 +188,25 @@ def test_host_threads_with_calls_of_different_size(tmp_path):
         within(loss, e["loss"], e["loss_err"], "loss")
 
 
+# ------------------------------------------------------------------------------------------------ the choice of kernels
+@pytest.mark.parametrize("d,V,most,limit", [(4096, 600, 8, 3), (8192, 600, 4, 3), (1024, 600, 16, 2), (1024, 22000, 16, 3)])
+def test_fp32_loss_of_few_tokens_reads_the_vocabulary_while_that_takes_less(d, V, most, limit):
+    """Launches of few tokens (`most` at these sizes) read all of W each: beyond `limit` of them the tile kernels take less time."""
+    def launches(T):
+        x, W, y, _ = make(T, d, V, "f32", 0.0, seed=T)
+        e = exact(x, W, y)
+        before = P.monarch_launch_count()
+        loss, _ = forward(x, W, y)
+        count = P.monarch_launch_count() - before
+        within(loss, e["loss"], e["loss_err"], "loss")
+        return count
+
+    tiles = launches(64)
+    for n in range(1, min(6, 64 // most) + 1):
+        assert launches(n * most) == (n if n <= limit else tiles), n
+    assert launches(limit * most + 1) == tiles
+
+
 # ------------------------------------------------------------------------------------------------ waits that run out
 def after_a_time_out(ws, call, outputs, must=True):
     """The call under a limit of 1 us gives up instead of hanging and says so; the workspace, made anew, then serves the same call as before."""
