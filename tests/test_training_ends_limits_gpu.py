@@ -9,7 +9,7 @@ import pytest
 import torch
 
 import paper_2204_00595_b200 as P
-from tests.test_training_ends_gpu import DT, IGNORE, backward, exact, forward, gradient, make, near, newton_schulz, ortho, within
+from tests.test_training_ends_gpu import DT, IGNORE, acc, backward, exact, forward, gen, gradient, make, near, newton_schulz, ortho, within
 
 pytestmark = pytest.mark.gpu
 
@@ -322,3 +322,92 @@ def test_update_within_less_memory(blocks, rows, cols, dtype):
         ws = Guarded(n)
         near(ortho(G, ws=ws), want, dtype, "O")
         assert ws.untouched(), n
+
+
+# ------------------------------------------------------------------------------------------------ what is promised of the precision
+@pytest.mark.parametrize("T", [9, 17, 40, 65, 100, 128])
+def test_gradients_of_up_to_128_bf16_tokens_are_as_exact_as_their_types(T):
+    """g in three parts in dW and two in dx (2^-24 and 2^-16 of a term).  The words share a component 16 times as large as what tells them
+    apart: the sum of a token's g is zero, so in dx that component cancels, and what g loses does not."""
+    d, V = 64, 5000
+    g = gen(80 + T)
+    W = ((torch.randn(1, d, generator=g, device="cuda") * 16 + torch.randn(V, d, generator=g, device="cuda")) / 64).bfloat16()
+    x = torch.randn(T, d, generator=g, device="cuda").bfloat16()
+    y = torch.randint(0, V, (T,), generator=g, device="cuda")
+    dloss = torch.rand(T, generator=g, device="cuda") + 0.1
+    xd, Wd, w = x.double(), W.double(), dloss.double()[:, None]
+    z = xd @ Wd.T
+    lse = torch.logsumexp(z, 1).float()
+    p = torch.exp(z - lse.double()[:, None])
+    gr = w * (p - torch.zeros_like(p).scatter_(1, y[:, None], 1.0))
+    dz = (xd.abs() @ Wd.abs().T) * acc(d)
+    dg = w * p * (dz + 2.0 ** -20 * (1.0 + z.abs() / 16)) + gr.abs() * (2.0 ** -24 + 2.0 ** -23)
+    dx, dW = backward(x, W, y, lse, dloss)
+    want = gr.T @ xd
+    within(dW, want, dg.T @ xd.abs() + (gr.abs().T @ xd.abs()) * acc(T, 3) + want.abs() * 2.0 ** -23, "dW")
+    want = gr @ Wd
+    err = (dg + gr.abs() * 2.0 ** -16) @ Wd.abs() + (gr.abs() @ Wd.abs()) * acc(V, 2)
+    within(dx, want, err + want.abs() * 2.0 ** -8, "dx")
+    # one part alone could be off by 2^-8 of every term: twenty times the bound
+    assert float(((gr.abs() * 2.0 ** -8) @ Wd.abs()).mean()) > 20 * float((err + want.abs() * 2.0 ** -8).mean())
+
+
+@pytest.mark.parametrize("T", [129, 300])
+def test_masked_logits_and_tokens_that_are_not_numbers_among_many(T):
+    """The fp16 parts of dW: words masked by the lowest value of the type have no part in anything, a token that is not a number keeps
+    to itself in dx and makes dW NaN."""
+    d, V = 64, 500
+    x, W, y, dloss = make(T, d, V, "bf16", 0.0, seed=81 + T)
+    y = y.clamp(min=200)
+    x[:, 0] = 1.0
+    W[:, 0] = 0.0
+    live = exact(x, W[200:].contiguous(), y - 200, dloss)
+    W[:200, 0] = torch.finfo(W.dtype).min
+    loss, lse = forward(x, W, y)
+    within(loss, live["loss"], live["loss_err"], "loss")
+    within(lse, live["lse"], live["lse_err"], "lse")
+    given = live["lse"].float()
+    dx, dW = backward(x, W, y, given, dloss)
+    within(dx[:, 1:], live["dx"][:, 1:], live["dx_err"][:, 1:], "dx")
+    assert (dW[:200] == 0).all()
+    within(dW[200:], live["dW"], live["dW_err"], "dW")
+    rest = torch.arange(T, device="cuda") != 3
+    for bad in (float("nan"), float("inf")):
+        xb = x.clone()
+        xb[3, 5] = bad
+        loss, lse = forward(xb, W, y)
+        assert torch.isnan(loss[3]) and torch.isnan(lse[3])
+        within(loss[rest], live["loss"][rest], live["loss_err"][rest], "loss of the others")
+        dx, dW = backward(xb, W, y, lse, dloss)
+        assert torch.isnan(dx[3]).all() and torch.isnan(dW).all()
+    w = dloss.clone()
+    w[3] = float("nan")
+    dx, dW = backward(x, W, y, given, w)
+    assert torch.isnan(dx[3]).all() and torch.isnan(dW).all()
+    within(dx[rest][:, 1:], live["dx"][rest][:, 1:], live["dx_err"][rest][:, 1:], "dx of the others")
+
+
+@pytest.mark.parametrize("rows,cols", [(16, 16), (64, 64), (40, 60), (30, 200), (60, 200), (128, 128), (90, 128), (160, 200), (8, 600)])
+def test_bf16_blocks_stand_alone(rows, cols):
+    """Zeros give zeros; NaN and infinity stay in their block; norms beyond the range of fp32 squares, and tiny ones."""
+    G = gradient(8, rows, cols, seed=82)
+    G[1] = 0.0
+    G[2, 3, 5] = float("nan")
+    G[3, 0, 0] = float("inf")
+    G[4] *= 1e30
+    G[5] *= 1e-30
+    G[6] *= 1e-6
+    G = G.bfloat16()
+    O = ortho(G)
+    assert (O[1] == 0).all()
+    assert torch.isnan(O[2]).all() and torch.isnan(O[3]).all()
+    fine = [0, 4, 6, 7]
+    near(O[fine], newton_schulz(G[fine].double()), "bf16", "O")
+    near(O[5:6], newton_schulz(G[5:6].double()), "bf16", "O")
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 7])
+@pytest.mark.parametrize("blocks,rows,cols", [(3, 24, 40), (3, 60, 60), (2, 100, 120), (2, 8, 500), (2, 150, 140)])
+def test_other_numbers_of_steps_in_bf16(blocks, rows, cols, steps):
+    G = gradient(blocks, rows, cols, seed=83 + steps).bfloat16()
+    near(ortho(G, steps), newton_schulz(G.double(), steps), "bf16", "O", steps)
