@@ -286,9 +286,10 @@ size_t monarch_xent_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab, in
  * lse, dloss: float32 [tokens].  Tokens left out (ignore_index) have dx = 0 and no part in dW;
  * a target out of range makes the gradients that it enters NaN.  g is held to 2^-24 in dW for
  * float32 and up to 128 tokens, else to 2^-22 (fp16 parts, scaled per token by the largest value
- * of x[t] and by dloss[t], at any size of these: exp(z - lse) has to stay below 4, as it does with
- * the lse of the same x and W), and of more than 128 tokens to bf16 in a bf16 dx.  Those parts leave
- * out what is below 2^-25 of the largest value of a row of x, and of a token's share in dW what is
+ * of x[t] and by dloss[t], at any size of these: exp(z - lse) has to stay below 3.9, as it does with
+ * the lse of the same x and W), and of more than 128 tokens to bf16 in a bf16 dx (2^-8 of each term: beyond
+ * the result's own rounding where the rows of W share a large component).  The fp16 parts leave out
+ * what is below 2^-25 of the largest value of a row of x, and of a token's share in dW what is
  * below 2^-39 of the largest |dloss[t]| max |x[t]| of the call.  The order of all sums
  * is fixed by the sizes and workspace_bytes.
  * Workspace: monarch_xent_bwd_workspace_bytes (0 for invalid arguments); it serves fewer tokens as above. */
@@ -301,7 +302,8 @@ size_t monarch_xent_bwd_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab
 /* Orthogonalisation of every block of a stack by Newton-Schulz products (for the gradients of the
  * factors: M = P L P^T R with orthogonal blocks is orthogonal).  For each block X0 = G / (||G||_F + 1e-7),
  * then `steps` times, with S = X X^T (rows <= cols) or X^T X:
- *   X <- a X + (b S + c S^2) X   or   X (b S + c S^2),   a, b, c = 3.4445, -4.7750, 2.0315,
+ *   X <- a X + (b S + c S^2) X   or   a X + X (b S + c S^2),   a, b, c = 3.4445, -4.7750, 2.0315
+ * (published with the Muon optimiser, K. Jordan and others, 2024),
  * which takes the singular values near 1 (five steps: to about 0.7 .. 1.2) and keeps the singular vectors.
  * G, O: [blocks][rows][cols] in the storage dtype; a factor of monarch_fwd is [m][m][m], of monarch_rect_fwd
  * [q][b][b1] or [b][r][q], a dense matrix one block.  A block of zeros gives zeros; one with an infinity

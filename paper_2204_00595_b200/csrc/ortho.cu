@@ -9,6 +9,7 @@ namespace monarch {
 namespace tc {
 namespace {
 
+// published with the Muon optimiser (K. Jordan and others, 2024)
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr float kEps = 1e-7f;
 
